@@ -450,6 +450,83 @@ int eesd_time_projection(eesd_ctx *ctx, int which, int M, float *ms_per_launch, 
 int eesd_sample_rows(void *cuda_stream, const float *logits, const float *u, int B, int V,
                      float temperature, int32_t *out);
 
+/* ---- 4-bit weights ------------------------------------------------------------------------------
+ * A matrix [R][K] (out, in) held in 4 bits per weight, in groups of `group` neighbours along K that share a scale
+ * and, optionally, a zero point (the last group of a row may be short):
+ *   value(r, k) = (c - z) * s,  c = 0..15,  z = the group's zero point (0..15), or 8 without zero points.
+ * The paper stores 16-bit weights; this is an extension for models whose weight stream bounds a pass. */
+typedef struct eesd_w4 {
+    int32_t R, K;         /* at most 2^28 each                                                   */
+    int32_t group;        /* 32, 64 or 128 (UNSUPPORTED otherwise)                               */
+    int32_t scale_dtype;  /* EESD_F32 or EESD_BF16                                               */
+    int32_t zero_point;   /* 1: zero points are stored, 0: symmetric (z = 8)                     */
+} eesd_w4;
+
+/* Byte offsets inside the one device buffer (16-byte aligned) that holds such a matrix, rows padded to 16 and columns to
+ * 64 (padding stands for 0):
+ *   codes  [R/16][K/64] tiles of 16 x 64 codes, 512 bytes each: element (r, k) of a tile sits in 32-bit word
+ *          ((r % 8) * 4 + (k % 8) / 2) * 4 + k / 16 at bits 4 * (r / 8 + 2 * (k / 8 % 2) + 4 * (k % 2)) and up
+ *   scales [groups][16 * row_blocks] in scale_dtype;  zeros the same in bytes (zero_point only). */
+typedef struct eesd_w4_layout {
+    size_t codes, scales, zeros, total_bytes;
+    int32_t row_blocks, k_tiles, groups;
+} eesd_w4_layout;
+int eesd_w4_layout_of(const eesd_w4 *m, eesd_w4_layout *out);
+
+/* The calls below are asynchronous on `cuda_stream`; all buffers are device memory; `packed` holds at least
+ * eesd_w4_layout.total_bytes (NOMEM otherwise).  Errors: BADARG, NOMEM, UNSUPPORTED, CUDA.
+ *
+ * eesd_w4_quantize: W [R][K] in w_dtype, rows ldw >= K elements apart.  Quotients are rounded to the nearest integer, ties to
+ * even, as if computed exactly; scales to the nearest value of scale_dtype.
+ *   symmetric:   s = max|w| / 7;  c = clamp(w / s, -8, 7) + 8
+ *   zero points: lo = min(w, 0), hi = max(w, 0), s = (hi - lo) / 15, z = clamp(-lo / s, 0, 15), c = clamp(w / s + z, 0, 15)
+ * A group of zeros (or one whose scale rounds to 0) reads back as zeros, a group that holds a NaN or an infinity as NaN.
+ * eesd_w4_pack: the same storage from codes [R][K] (one per byte, low 4 bits), scales [R][groups] in scale_dtype and zeros [R][groups]
+ * (bytes; NULL without zero points), all contiguous: how a model that comes quantised is brought in.
+ * eesd_w4_dequantize: the values, out [R][K] in out_dtype with rows ldo >= K apart. */
+int eesd_w4_quantize(void *cuda_stream, const eesd_w4 *m, int w_dtype, const void *W, int64_t ldw, void *packed, size_t packed_bytes);
+int eesd_w4_pack(void *cuda_stream, const eesd_w4 *m, const uint8_t *codes, const void *scales, const uint8_t *zeros, void *packed,
+                 size_t packed_bytes);
+int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int out_dtype, void *out, int64_t ldo);
+
+/* eesd_project_rows for a 4-bit matrix: out[r'][r] = sum_k A[r'][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A [M] rows of a_dtype lda >= K elements
+ * apart, out [M] fp32 rows ldo >= R apart.  No scratch, one launch, the same bits on every call.  Sums are fp32; an activation
+ * below 2^-39 of the largest of its row (among neighbouring columns, 512 at least) counts as 0 (bf16 rows: below 2^-40).  A row of
+ * A that holds a NaN or an infinity gives NaN or infinities; the other rows are not touched by it. */
+int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,
+                         float *out, int64_t ldo, int M);
+
+/* ---- logit rules -----------------------------------------------------------------------------------
+ * Penalties for repeated tokens, biases and grammar masks on logit rows, before they are sampled or tested.  For lossless
+ * acceptance the draft's rows and the target's are both processed, with the same rules: row i of a sequence (0-based) is the one
+ * that follows its drafts x_1..x_i, so it counts them as generated.
+ *   n    = times v was generated: in history[n_prompt .. n_history), or among drafted[0 .. i)
+ *   l1   = v generated or in history[0 .. n_prompt) ? (l > 0 ? l / repetition : l * repetition) : l
+ *   l2   = l1 - (frequency * n + (n > 0 ? presence : 0));   l3 = l2 + bias(v);   out = allowed ? l3 : -inf
+ * Everything is optional (NULL: off).  Token ids outside [0, V) are ignored everywhere.  A masked entry is -inf whatever the
+ * logit was (NaN and infinities included).  A row whose mask leaves nothing is -inf throughout; eesd_sample_rows and
+ * eesd_accept_resample answer -1 for a row without any logit above -inf. */
+#define EESD_MAX_RULE_ROWS 256
+typedef struct eesd_logit_rules {              /* device pointers */
+    const int32_t *history;                    /* [B] rows of history_len tokens, history_stride apart          */
+    int64_t history_stride;
+    int32_t history_len;
+    int32_t n_bias;                            /* entries of bias_ids / bias_values (0: no biases)              */
+    const int32_t *n_history, *n_prompt;       /* [B]; NULL: history_len tokens / no prompt; cut to the range   */
+    const int32_t *drafted;                    /* [B] rows of rows - 1 tokens, drafted_stride apart             */
+    int64_t drafted_stride;
+    const float *repetition, *frequency, *presence;   /* [B]; repetition > 0                                    */
+    const int32_t *bias_start;                 /* [B + 1]: sequence b's biases are bias_start[b] .. bias_start[b + 1] - 1 */
+    const int32_t *bias_ids;
+    const float *bias_values;                  /* an id given twice takes its last value                        */
+    const int32_t *mask;                       /* [B * rows] rows of words, mask_stride apart; bit v % 32 of word v / 32: allowed */
+    int64_t mask_stride;
+} eesd_logit_rules;
+/* logits: B * rows rows of V fp32, ld_logits apart; out likewise.  out may be logits (same ld); any other overlap is BADARG.
+ * rows <= EESD_MAX_RULE_ROWS.  Asynchronous, one launch, no scratch. */
+int eesd_process_logits(void *cuda_stream, const float *logits, int64_t ld_logits, float *out, int64_t ld_out, int B, int rows, int V,
+                        const eesd_logit_rules *rules);
+
 #ifdef __cplusplus
 }
 #endif

@@ -76,6 +76,22 @@ class Stats(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class W4Desc(C.Structure):
+    _fields_ = [("R", C.c_int32), ("K", C.c_int32), ("group", C.c_int32), ("scale_dtype", C.c_int32), ("zero_point", C.c_int32)]
+
+
+class W4Layout(C.Structure):
+    _fields_ = [("codes", C.c_size_t), ("scales", C.c_size_t), ("zeros", C.c_size_t), ("total_bytes", C.c_size_t),
+                ("row_blocks", C.c_int32), ("k_tiles", C.c_int32), ("groups", C.c_int32)]
+
+
+class RulesStruct(C.Structure):
+    _fields_ = [("history", C.c_void_p), ("history_stride", C.c_int64), ("history_len", C.c_int32), ("n_bias", C.c_int32),
+                ("n_history", C.c_void_p), ("n_prompt", C.c_void_p), ("drafted", C.c_void_p), ("drafted_stride", C.c_int64),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("bias_start", C.c_void_p),
+                ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p), ("mask", C.c_void_p), ("mask_stride", C.c_int64)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -139,6 +155,13 @@ def lib():
         L.eesd_time_projection.argtypes = [vp, C.c_int, C.c_int, C.POINTER(C.c_float), C.POINTER(C.c_size_t)]
         L.eesd_accept_resample_static.argtypes = [vp, vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, vp]
         L.eesd_sample_rows.argtypes = [vp, vp, vp, C.c_int, C.c_int, C.c_float, vp]
+        i64, sz = C.c_int64, C.c_size_t
+        L.eesd_w4_layout_of.argtypes = [C.POINTER(W4Desc), C.POINTER(W4Layout)]
+        L.eesd_w4_quantize.argtypes = [vp, vp, C.c_int, vp, i64, vp, sz]
+        L.eesd_w4_pack.argtypes = [vp, vp, vp, vp, vp, vp, sz]
+        L.eesd_w4_dequantize.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64]
+        L.eesd_w4_project_rows.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64, vp, i64, C.c_int]
+        L.eesd_process_logits.argtypes = [vp, vp, i64, vp, i64, C.c_int, C.c_int, C.c_int, vp]
         _lib = L
     return _lib
 
@@ -543,8 +566,11 @@ def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: fl
     return out
 
 
-def project_rows(A: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """eesd_project_rows: A [M, K] fp32 times W [R, K]^T (fp32 or bf16) -> [M, R] fp32."""
+def project_rows(A: torch.Tensor, W, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """eesd_project_rows: A [M, K] fp32 times W [R, K]^T (fp32 or bf16) -> [M, R] fp32.  With a W4Matrix in
+    the place of W eesd_w4_project_rows (A fp32 or bf16; needs no scratch)."""
+    if isinstance(W, W4Matrix):
+        return W.project_rows(A)
     _need_cuda()
     M, K = A.shape
     R = W.shape[0]
@@ -558,4 +584,257 @@ def project_rows(A: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tenso
                                  scratch.data_ptr(), scratch.numel())
     if st:
         raise EesdError(st, "eesd_project_rows")
+    return out
+
+
+# ---- 4-bit weights, logit rules
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _raw_stream(device: torch.device) -> int:
+    """The current stream of the tensors' device."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+class _on:
+    """Makes the tensors' device the current one for a call (the library launches on the current device)."""
+
+    def __init__(self, device: torch.device):
+        self.want = device.index
+
+    def __enter__(self):
+        self.was = torch._C._cuda_getDevice()
+        if self.was != self.want:
+            torch.cuda.set_device(self.want)
+
+    def __exit__(self, *_):
+        if self.was != self.want:
+            torch.cuda.set_device(self.was)
+
+
+def _cuda_tensor(t, name: str, dtypes, device=None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes:
+        raise ValueError(f"{name}: wanted a CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the other tensors are on {device}")
+    return t
+
+
+class W4Matrix:
+    """A weight matrix [R, K] in 4 bits per weight with a scale (and optionally a zero point) per group of `group`
+    neighbours along K (eesd_w4): `W4Matrix.quantize(w)` or `W4Matrix.from_codes(codes, scales, zeros)`, then
+    `project_rows(A, m)`.  Storage: one buffer laid out by eesd_w4_layout_of."""
+
+    def __init__(self, R: int, K: int, group: int = 128, scale_dtype: torch.dtype = torch.bfloat16, zero_point: bool = False, device="cuda"):
+        if scale_dtype not in _DTYPES:
+            raise ValueError("scale_dtype: torch.float32 or torch.bfloat16")
+        self.desc, self.layout = W4Desc(R, K, group, _DTYPES[scale_dtype], int(zero_point)), W4Layout()
+        st = lib().eesd_w4_layout_of(C.byref(self.desc), C.byref(self.layout))
+        if st:
+            raise EesdError(st, "eesd_w4_layout_of")
+        _need_cuda()
+        self.shape, self.group, self.scale_dtype, self.zero_point = (R, K), group, scale_dtype, bool(zero_point)
+        self.buffer = torch.empty(self.layout.total_bytes, dtype=torch.uint8, device=device)
+        self.device = self.buffer.device
+        self._desc_ptr, self._ptr, self._bytes = C.addressof(self.desc), self.buffer.data_ptr(), self.buffer.numel()
+
+    @classmethod
+    def quantize(cls, w: torch.Tensor, group: int = 128, scale_dtype: torch.dtype = torch.bfloat16, zero_point: bool = False) -> "W4Matrix":
+        """eesd_w4_quantize: w [R, K] fp32 or bf16 (rows may be strided)."""
+        _need_cuda()
+        _cuda_tensor(w, "w", _DTYPES)
+        if w.dim() != 2 or w.shape[1] < 1 or w.shape[0] < 1 or (w.stride(1) != 1 and w.shape[1] > 1):
+            raise ValueError("w: wanted [R, K] with neighbouring columns next to each other")
+        m = cls(w.shape[0], w.shape[1], group, scale_dtype, zero_point, w.device)
+        ld = w.stride(0) if w.shape[0] > 1 else w.shape[1]
+        with _on(m.device):
+            st = lib().eesd_w4_quantize(_raw_stream(m.device), m._desc_ptr, _DTYPES[w.dtype], w.data_ptr(), ld, m._ptr, m._bytes)
+        if st:
+            raise EesdError(st, "eesd_w4_quantize")
+        return m
+
+    @classmethod
+    def from_codes(cls, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, group: int = 128) -> "W4Matrix":
+        """eesd_w4_pack: codes uint8 [R, K] (0..15), scales [R, ceil(K / group)] fp32 or bf16, zeros uint8 of the scales' shape or
+        None (symmetric: zero point 8)."""
+        _need_cuda()
+        _cuda_tensor(codes, "codes", (torch.uint8,))
+        _cuda_tensor(scales, "scales", _DTYPES, codes.device)
+        if codes.dim() != 2 or codes.numel() == 0:
+            raise ValueError("codes: wanted [R, K]")
+        R, K = codes.shape
+        m = cls(R, K, group, scales.dtype, zeros is not None, codes.device)
+        if tuple(scales.shape) != (R, m.layout.groups):
+            raise ValueError(f"scales: wanted [{R}, {m.layout.groups}]")
+        if zeros is not None and tuple(_cuda_tensor(zeros, "zeros", (torch.uint8,), codes.device).shape) != (R, m.layout.groups):
+            raise ValueError(f"zeros: wanted [{R}, {m.layout.groups}]")
+        with _on(m.device):
+            codes, scales = codes.contiguous(), scales.contiguous()
+            zeros = None if zeros is None else zeros.contiguous()
+            st = lib().eesd_w4_pack(_raw_stream(m.device), m._desc_ptr, codes.data_ptr(), scales.data_ptr(),
+                                    None if zeros is None else zeros.data_ptr(), m._ptr, m._bytes)
+        if st:
+            raise EesdError(st, "eesd_w4_pack")
+        return m
+
+    def _group_view(self, off: int, dtype: torch.dtype) -> torch.Tensor:
+        r16, g = self.layout.row_blocks * 16, self.layout.groups
+        n = r16 * g * torch.empty((), dtype=dtype).element_size()
+        return self.buffer[off:off + n].view(dtype).view(g, r16)[:, :self.shape[0]].t()
+
+    def scales(self) -> torch.Tensor:
+        """[R, groups] view of the scales."""
+        return self._group_view(self.layout.scales, self.scale_dtype)
+
+    def zeros(self) -> Optional[torch.Tensor]:
+        """[R, groups] view of the zero points (None: symmetric, 8)."""
+        return self._group_view(self.layout.zeros, torch.uint8) if self.zero_point else None
+
+    def codes(self) -> torch.Tensor:
+        """The codes, uint8 [R, K] (a copy)."""
+        rb, kt = self.layout.row_blocks, self.layout.k_tiles
+        b = self.buffer[:rb * kt * 512].view(rb, kt, 8, 4, 4, 2, 2, 1)   # [.., row % 8, pair, step, byte pair e, q, h]
+        c = torch.cat((b & 15, b >> 4), -1)                              # low nibble: rows 0..7, high nibble: rows 8..15
+        # -> [row block, h, row % 8, tile, step, q, pair, e]
+        return c.permute(0, 7, 2, 1, 4, 6, 3, 5).reshape(rb * 16, kt * 64)[:self.shape[0], :self.shape[1]]
+
+    def dense(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        """eesd_w4_dequantize: the values, [R, K] fp32 or bf16."""
+        if dtype not in _DTYPES:
+            raise ValueError("dtype: torch.float32 or torch.bfloat16")
+        out = torch.empty(self.shape, dtype=dtype, device=self.device)
+        with _on(self.device):
+            st = lib().eesd_w4_dequantize(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, _DTYPES[dtype], out.data_ptr(), self.shape[1])
+        if st:
+            raise EesdError(st, "eesd_w4_dequantize")
+        return out
+
+    def project_rows(self, A: torch.Tensor) -> torch.Tensor:
+        """eesd_w4_project_rows: A [M, K] fp32 or bf16, M <= MAX_ROWS (rows may be strided), times the matrix's transpose -> [M, R] fp32."""
+        _cuda_tensor(A, "A", _DTYPES, self.device)
+        R, K = self.shape
+        if A.dim() != 2 or A.shape[1] != K or (A.stride(1) != 1 and K > 1):
+            raise ValueError(f"A: wanted [M, {K}] with neighbouring columns next to each other")
+        M = A.shape[0]
+        if not 1 <= M <= MAX_ROWS:
+            raise ValueError(f"A: 1 to {MAX_ROWS} rows, not {M}")
+        out = torch.empty((M, R), dtype=torch.float32, device=self.device)
+        with _on(self.device):
+            st = lib().eesd_w4_project_rows(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, _DTYPES[A.dtype], A.data_ptr(),
+                                            A.stride(0) if M > 1 else K, out.data_ptr(), R, M)
+        if st:
+            raise EesdError(st, "eesd_w4_project_rows")
+        return out
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements between the rows of [B, n] or [B, rows, n]; they have to lie evenly."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: neighbours of a row have to lie next to each other")
+    if t.dim() == 2:
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    B, rows, n = t.shape
+    ld = t.stride(1) if rows > 1 else t.stride(0) if B > 1 else n
+    if B > 1 and t.stride(0) != ld * rows:
+        raise ValueError(f"{name}: rows have to lie evenly")
+    return ld
+
+
+class LogitRules:
+    """Penalties, biases and a grammar mask for the logit rows of B sequences (eesd_logit_rules); what is left out is off.
+
+    history [B, H] int32 with n_history, n_prompt [B] int32: each sequence's tokens, its prompt first (without n_history all H; the
+    sizes are read on the device at each call, so a buffer of full length can be kept and filled in place)
+    drafted [B, rows - 1] int32: the round's draft tokens; row i of a sequence counts its first i
+    repetition, frequency, presence [B] fp32
+    bias_start [B + 1] int32, bias_ids [n] int32, bias_values [n] fp32: sequence b's biases are bias_start[b] .. bias_start[b + 1] - 1
+    mask [B, rows, words] int32 (or [B, words] for one row each): bit v % 32 of word v // 32 set: v is allowed
+
+    The tensors are kept and read at each process_logits call; none is copied."""
+
+    def __init__(self, *, history=None, n_history=None, n_prompt=None, drafted=None, repetition=None, frequency=None, presence=None,
+                 bias_start=None, bias_ids=None, bias_values=None, mask=None):
+        i32, f32 = (torch.int32,), (torch.float32,)
+        r, self._keep, self.device, self.B, self.rows, self.mask_words = RulesStruct(), [], None, None, None, None
+
+        def take(t, name, dtypes, dim):
+            _cuda_tensor(t, name, dtypes, self.device)
+            if t.dim() not in dim:
+                raise ValueError(f"{name}: {t.dim()} dimensions")
+            self.device = t.device
+            self._keep.append(t)
+            return t
+
+        def per_sequence(t, name, n=None, extra=0):
+            n = t.shape[0] - extra if n is None else n
+            if self.B is None:
+                self.B = n
+            if n != self.B:
+                raise ValueError(f"{name}: for {n} sequences, not {self.B}")
+
+        if history is not None:
+            take(history, "history", i32, (2,))
+            per_sequence(history, "history")
+            if history.shape[1]:
+                r.history, r.history_stride, r.history_len = history.data_ptr(), _row_stride(history, "history"), history.shape[1]
+        elif n_history is not None or n_prompt is not None:
+            raise ValueError("n_history / n_prompt without history")
+        for name, t, dtypes in (("n_history", n_history, i32), ("n_prompt", n_prompt, i32), ("repetition", repetition, f32),
+                                ("frequency", frequency, f32), ("presence", presence, f32)):
+            if t is not None:
+                per_sequence(take(t, name, dtypes, (1,)), name)
+                if not t.is_contiguous():
+                    raise ValueError(f"{name}: wanted contiguous")
+                setattr(r, name, t.data_ptr())
+        if drafted is not None:
+            take(drafted, "drafted", i32, (2,))
+            per_sequence(drafted, "drafted")
+            self.rows = drafted.shape[1] + 1
+            if drafted.shape[1]:
+                r.drafted, r.drafted_stride = drafted.data_ptr(), _row_stride(drafted, "drafted")
+        if (bias_start is None) != (bias_ids is None) or (bias_ids is None) != (bias_values is None):
+            raise ValueError("bias_start, bias_ids and bias_values go together")
+        if bias_ids is not None:
+            for name, t, dtypes in (("bias_start", bias_start, i32), ("bias_ids", bias_ids, i32), ("bias_values", bias_values, f32)):
+                if not take(t, name, dtypes, (1,)).is_contiguous():
+                    raise ValueError(f"{name}: wanted contiguous")
+                setattr(r, name, t.data_ptr())
+            per_sequence(bias_start, "bias_start", extra=1)
+            if bias_ids.shape != bias_values.shape:
+                raise ValueError("bias_ids and bias_values: one value for each id")
+            r.n_bias = bias_ids.shape[0]
+        if mask is not None:
+            take(mask, "mask", i32, (2, 3))
+            per_sequence(mask, "mask")
+            n = mask.shape[1] if mask.dim() == 3 else 1
+            if self.rows not in (None, n):
+                raise ValueError(f"mask: {n} rows a sequence, {self.rows} with its drafts")
+            self.rows, self.mask_words = n, mask.shape[-1]
+            r.mask, r.mask_stride = mask.data_ptr(), _row_stride(mask, "mask")
+        self._struct, self._ptr = r, C.addressof(r)
+
+
+def process_logits(logits: torch.Tensor, rules: LogitRules, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """eesd_process_logits: logits [B, rows, V] (or [B, V]: one row each) fp32, rows evenly spaced; returns the processed rows, in
+    `out` when given (which may be `logits` itself)."""
+    _need_cuda()
+    _cuda_tensor(logits, "logits", (torch.float32,))
+    if logits.dim() not in (2, 3) or logits.numel() == 0:
+        raise ValueError("logits: wanted [B, rows, V] or [B, V]")
+    B, rows, V = logits.shape[0], logits.shape[1] if logits.dim() == 3 else 1, logits.shape[-1]
+    if rules.B not in (None, B) or rules.rows not in (None, rows):
+        raise ValueError(f"rules for {rules.B} sequences of {rules.rows} rows, logits for {B} of {rows}")
+    if rules.device not in (None, logits.device):
+        raise ValueError(f"rules: on {rules.device}, logits on {logits.device}")
+    if rules.mask_words is not None and rules.mask_words < (V + 31) // 32:
+        raise ValueError(f"mask: {rules.mask_words} words for {V} entries")
+    if out is None:
+        out = torch.empty((B, rows, V) if logits.dim() == 3 else (B, V), dtype=torch.float32, device=logits.device)
+    elif _cuda_tensor(out, "out", (torch.float32,), logits.device).shape != logits.shape:
+        raise ValueError("out: wanted the shape of logits")
+    with _on(logits.device):
+        st = lib().eesd_process_logits(_raw_stream(logits.device), logits.data_ptr(), _row_stride(logits, "logits"), out.data_ptr(),
+                                       _row_stride(out, "out"), B, rows, V, rules._ptr)
+    if st:
+        raise EesdError(st, "eesd_process_logits")
     return out
