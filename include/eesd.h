@@ -462,14 +462,15 @@ typedef struct eesd_w4 {
     int32_t zero_point;   /* 1: zero points are stored, 0: symmetric (z = 8)                     */
 } eesd_w4;
 
-/* Byte offsets inside the one device buffer (16-byte aligned) that holds such a matrix, rows padded to 16 and columns to
- * 64 (padding stands for 0):
- *   codes  [R/16][K/64] tiles of 16 x 64 codes, 512 bytes each: element (r, k) of a tile sits in 32-bit word
- *          ((r % 8) * 4 + (k % 8) / 2) * 4 + k / 16 at bits 4 * (r / 8 + 2 * (k / 8 % 2) + 4 * (k % 2)) and up
- *   scales [groups][16 * row_blocks] in scale_dtype;  zeros the same in bytes (zero_point only). */
+/* The one device buffer (16-byte aligned) that holds such a matrix: blocks of 16 rows x 128 columns, block (r / 16, k / 128) at
+ * ((r / 16) * k_blocks + k / 128) * block_bytes.  Rows are padded to 16 and columns to 128 (padding stands for 0).  In a block:
+ *   at 0       two tiles of 16 x 64 codes, 512 bytes each: element (r, k) of a tile sits in 32-bit word
+ *              ((r % 8) * 4 + (k % 16) / 4) * 4 + k / 16 at bits 8 * (k % 4) + 4 * (r / 8) and up
+ *   at scales  [row % 8][row / 8][128 / group] scales in scale_dtype
+ *   at zeros   the same in bytes (zero_point only). */
 typedef struct eesd_w4_layout {
-    size_t codes, scales, zeros, total_bytes;
-    int32_t row_blocks, k_tiles, groups;
+    size_t scales, zeros, block_bytes, total_bytes;
+    int32_t row_blocks, k_blocks, groups;
 } eesd_w4_layout;
 int eesd_w4_layout_of(const eesd_w4 *m, eesd_w4_layout *out);
 
@@ -489,12 +490,16 @@ int eesd_w4_pack(void *cuda_stream, const eesd_w4 *m, const uint8_t *codes, cons
                  size_t packed_bytes);
 int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int out_dtype, void *out, int64_t ldo);
 
-/* eesd_project_rows for a 4-bit matrix: out[r'][r] = sum_k A[r'][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A [M] rows of a_dtype lda >= K elements
- * apart, out [M] fp32 rows ldo >= R apart.  No scratch, one launch, the same bits on every call.  Sums are fp32; an activation
- * below 2^-39 of the largest of its row (among neighbouring columns, 512 at least) counts as 0 (bf16 rows: below 2^-40).  A row of
- * A that holds a NaN or an infinity gives NaN or infinities; the other rows are not touched by it. */
+/* eesd_project_rows for a 4-bit matrix: out[m][r] = sum_k A[m][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A: M rows of a_dtype,
+ * lda >= K elements apart; out: M fp32 rows, ldo >= R apart.  scratch: device, 16-byte aligned, eesd_w4_project_scratch_bytes bytes
+ * (0 while M * ceil(K / 128) <= 32: then it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.  The same
+ * bits on every call.  Activations are taken as fixed-point numbers, one scale for the same 128 columns (128 i .. 128 i + 127) of a
+ * row: they are off by at most 2^-22.9 of the largest magnitude there (up to 4 rows: 2^-30.9), as the terms of a sum in fp32 are off by
+ * their share of its largest; where that largest is below 2^-96 by up to 2^-127.  The sums of a group are exact, those over groups fp32.
+ * A row of A that holds a NaN or an infinity gives NaN; the other rows are not touched by it. */
+size_t eesd_w4_project_scratch_bytes(const eesd_w4 *m, int M);
 int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,
-                         float *out, int64_t ldo, int M);
+                         float *out, int64_t ldo, int M, void *scratch, size_t scratch_bytes);
 
 /* ---- logit rules -----------------------------------------------------------------------------------
  * Penalties for repeated tokens, biases and grammar masks on logit rows, before they are sampled or tested.  For lossless

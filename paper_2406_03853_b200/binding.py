@@ -81,8 +81,8 @@ class W4Desc(C.Structure):
 
 
 class W4Layout(C.Structure):
-    _fields_ = [("codes", C.c_size_t), ("scales", C.c_size_t), ("zeros", C.c_size_t), ("total_bytes", C.c_size_t),
-                ("row_blocks", C.c_int32), ("k_tiles", C.c_int32), ("groups", C.c_int32)]
+    _fields_ = [("scales", C.c_size_t), ("zeros", C.c_size_t), ("block_bytes", C.c_size_t), ("total_bytes", C.c_size_t),
+                ("row_blocks", C.c_int32), ("k_blocks", C.c_int32), ("groups", C.c_int32)]
 
 
 class RulesStruct(C.Structure):
@@ -160,7 +160,9 @@ def lib():
         L.eesd_w4_quantize.argtypes = [vp, vp, C.c_int, vp, i64, vp, sz]
         L.eesd_w4_pack.argtypes = [vp, vp, vp, vp, vp, vp, sz]
         L.eesd_w4_dequantize.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64]
-        L.eesd_w4_project_rows.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64, vp, i64, C.c_int]
+        L.eesd_w4_project_scratch_bytes.restype = sz
+        L.eesd_w4_project_scratch_bytes.argtypes = [vp, C.c_int]
+        L.eesd_w4_project_rows.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64, vp, i64, C.c_int, vp, sz]
         L.eesd_process_logits.argtypes = [vp, vp, i64, vp, i64, C.c_int, C.c_int, C.c_int, vp]
         _lib = L
     return _lib
@@ -568,9 +570,9 @@ def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: fl
 
 def project_rows(A: torch.Tensor, W, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
     """eesd_project_rows: A [M, K] fp32 times W [R, K]^T (fp32 or bf16) -> [M, R] fp32.  With a W4Matrix in
-    the place of W eesd_w4_project_rows (A fp32 or bf16; needs no scratch)."""
+    the place of W eesd_w4_project_rows (A fp32 or bf16)."""
     if isinstance(W, W4Matrix):
-        return W.project_rows(A)
+        return W.project_rows(A, scratch)
     _need_cuda()
     M, K = A.shape
     R = W.shape[0]
@@ -677,26 +679,29 @@ class W4Matrix:
             raise EesdError(st, "eesd_w4_pack")
         return m
 
-    def _group_view(self, off: int, dtype: torch.dtype) -> torch.Tensor:
-        r16, g = self.layout.row_blocks * 16, self.layout.groups
-        n = r16 * g * torch.empty((), dtype=dtype).element_size()
-        return self.buffer[off:off + n].view(dtype).view(g, r16)[:, :self.shape[0]].t()
+    def _per_group(self, off: int, dtype: torch.dtype) -> torch.Tensor:
+        lay, n = self.layout, 128 // self.group
+        es = torch.empty((), dtype=dtype).element_size()
+        b = self.buffer.view(lay.row_blocks, lay.k_blocks, lay.block_bytes)[:, :, off:off + n * 16 * es].view(dtype)
+        b = b.view(lay.row_blocks, lay.k_blocks, 8, 2, n).permute(0, 3, 2, 1, 4)   # [row block, row / 8, row % 8, block, group]
+        return b.reshape(lay.row_blocks * 16, lay.k_blocks * n)[:self.shape[0], :lay.groups]
 
     def scales(self) -> torch.Tensor:
-        """[R, groups] view of the scales."""
-        return self._group_view(self.layout.scales, self.scale_dtype)
+        """The scales, [R, groups] (a copy)."""
+        return self._per_group(self.layout.scales, self.scale_dtype)
 
     def zeros(self) -> Optional[torch.Tensor]:
-        """[R, groups] view of the zero points (None: symmetric, 8)."""
-        return self._group_view(self.layout.zeros, torch.uint8) if self.zero_point else None
+        """The zero points, uint8 [R, groups] (a copy; None: symmetric, 8)."""
+        return self._per_group(self.layout.zeros, torch.uint8) if self.zero_point else None
 
     def codes(self) -> torch.Tensor:
         """The codes, uint8 [R, K] (a copy)."""
-        rb, kt = self.layout.row_blocks, self.layout.k_tiles
-        b = self.buffer[:rb * kt * 512].view(rb, kt, 8, 4, 4, 2, 2, 1)   # [.., row % 8, pair, step, byte pair e, q, h]
-        c = torch.cat((b & 15, b >> 4), -1)                              # low nibble: rows 0..7, high nibble: rows 8..15
-        # -> [row block, h, row % 8, tile, step, q, pair, e]
-        return c.permute(0, 7, 2, 1, 4, 6, 3, 5).reshape(rb * 16, kt * 64)[:self.shape[0], :self.shape[1]]
+        rb, kb = self.layout.row_blocks, self.layout.k_blocks
+        b = self.buffer.view(rb, kb, self.layout.block_bytes)[:, :, :1024]
+        b = b.reshape(rb, kb, 2, 8, 4, 4, 4, 1)   # [.., tile, row % 8, k % 16 / 4, k / 16, k % 4]: a byte holds rows r and r + 8
+        c = torch.cat((b & 15, b >> 4), -1)
+        # -> [row block, row / 8, row % 8, block, tile, k / 16, k % 16 / 4, k % 4]
+        return c.permute(0, 7, 3, 1, 2, 5, 4, 6).reshape(rb * 16, kb * 128)[:self.shape[0], :self.shape[1]]
 
     def dense(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """eesd_w4_dequantize: the values, [R, K] fp32 or bf16."""
@@ -709,8 +714,9 @@ class W4Matrix:
             raise EesdError(st, "eesd_w4_dequantize")
         return out
 
-    def project_rows(self, A: torch.Tensor) -> torch.Tensor:
-        """eesd_w4_project_rows: A [M, K] fp32 or bf16, M <= MAX_ROWS (rows may be strided), times the matrix's transpose -> [M, R] fp32."""
+    def project_rows(self, A: torch.Tensor, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """eesd_w4_project_rows: A [M, K] fp32 or bf16, M <= MAX_ROWS (rows may be strided), times the matrix's transpose -> [M, R]
+        fp32.  scratch: a CUDA tensor of eesd_w4_project_scratch_bytes bytes (made for the call when left out)."""
         _cuda_tensor(A, "A", _DTYPES, self.device)
         R, K = self.shape
         if A.dim() != 2 or A.shape[1] != K or (A.stride(1) != 1 and K > 1):
@@ -718,10 +724,17 @@ class W4Matrix:
         M = A.shape[0]
         if not 1 <= M <= MAX_ROWS:
             raise ValueError(f"A: 1 to {MAX_ROWS} rows, not {M}")
+        L, dt = lib(), _DTYPES[A.dtype]
+        need = L.eesd_w4_project_scratch_bytes(self._desc_ptr, M)
+        if scratch is not None:
+            _cuda_tensor(scratch, "scratch", (torch.uint8,), self.device)
+        elif need:
+            scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
         out = torch.empty((M, R), dtype=torch.float32, device=self.device)
         with _on(self.device):
-            st = lib().eesd_w4_project_rows(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, _DTYPES[A.dtype], A.data_ptr(),
-                                            A.stride(0) if M > 1 else K, out.data_ptr(), R, M)
+            st = L.eesd_w4_project_rows(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, dt, A.data_ptr(),
+                                        A.stride(0) if M > 1 else K, out.data_ptr(), R, M,
+                                        *((None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel())))
         if st:
             raise EesdError(st, "eesd_w4_project_rows")
         return out

@@ -4,12 +4,13 @@
 //   value(r, k) = (c(r, k) - z(r, k / g)) * s(r, k / g),   c = 0..15, z = 0..15 (8 without zero points)
 //   out[m][r]   = sum_G s(r, G) * sum_{k in G} (c(r, k) - z(r, G)) * A[m][k]
 //
-// Storage: codes are kept in the register order of the matrix instruction that consumes them (m16n8k16: 16 weight
-// rows, 16 columns).  A tile is 16 rows x 64 columns = 512 bytes, lane l's 16 bytes together (four k16 steps), so a warp's
-// load of a tile is one contiguous 16-byte-per-lane read that needs no shared memory and no shuffles; tiles of a row
-// block follow one another along K.  Scales (and zero points) are group-major, [group][rows padded to 16].
+// Storage: blocks of 16 rows x 128 columns, the blocks of a row block one after the other along K, so that a warp streams
+// contiguous memory.  A block holds its codes in the register order of the matrix instruction that consumes them (m16n8k32 on bytes: 16
+// weight rows, 32 columns; two tiles of 64 columns, lane l's 16 bytes of a tile together), then its groups' scales, then their zero
+// points, both [row % 8][row / 8][group]: what a lane needs of them lies together.  Element (r, k) of a tile: lane (r % 8) * 4 + (k %
+// 16) / 4, word k / 16, bits 8 * (k % 4) + 4 * (r / 8) of it: the low nibbles of a word are a fragment register of row r % 8,
+// the high ones that of row r % 8 + 8.
 #include <cooperative_groups.h>
-#include <cuda_fp16.h>
 
 #include <atomic>
 
@@ -22,9 +23,18 @@ namespace w4 {
 
 namespace cg = cooperative_groups;
 
-// Element (r, k) of a tile: lane (r % 8) * 4 + (k % 8) / 2, word k / 16, bits 4 * (r / 8 + 2 * (k / 8 % 2) + 4 * (k % 2)) of it.
-// The pair (k, k + 1) of a fragment register sits 16 bits apart and the word's four registers 4 bits apart, so one AND
-// takes a register's pair out of the word.
+struct Geom {   // where things are in a block
+    int group, scale_dtype, zp, R, K, KB, block_bytes, off_zeros;
+};
+
+__device__ __forceinline__ int scale_slot(int r, int g, int per_row) { return ((r & 7) * 2 + ((r >> 3) & 1)) * per_row + g; }   // per_row: 128 / group
+__device__ __forceinline__ float load_scale(const unsigned char *blk, const Geom &q, int slot) {
+    return q.scale_dtype == EESD_F32 ? reinterpret_cast<const float *>(blk + 1024)[slot] : to_f(reinterpret_cast<const __nv_bfloat16 *>(blk + 1024)[slot]);
+}
+__device__ __forceinline__ void store_scale(unsigned char *blk, const Geom &q, int slot, float s) {
+    if (q.scale_dtype == EESD_F32) reinterpret_cast<float *>(blk + 1024)[slot] = s;
+    else reinterpret_cast<__nv_bfloat16 *>(blk + 1024)[slot] = __float2bfloat16_rn(s);
+}
 
 // ------------------------------------------------------------------------------------ quantisation
 // float64 -> nearest bf16 (ties to even) without double rounding: towards zero in fp32, the lost part kept in the last bit
@@ -35,131 +45,135 @@ __device__ __forceinline__ float round_scale(double x, int scale_dtype) {
     return __bfloat162float(__float2bfloat16_rn(f));
 }
 
-// nearest integer (ties to even) to the exact quotient x / s, clamped to [lo, hi].  The rounded quotient can only be off by
-// one, and only when x / s is within rounding of a half: the exact remainder (one fused multiply-add) settles it.
-__device__ __forceinline__ int nearest_quotient(float x, float s, int lo, int hi) {
+// nearest integer (ties to even) to the exact quotient x / s.  The rounded quotient can only be off by one, and only when x / s
+// is within rounding of a half: the exact remainder (one fused multiply-add) settles it.
+__device__ __forceinline__ float nearest_quotient(float x, float s) {
     float q = rintf(__fdiv_rn(x, s));
-    q = fminf(fmaxf(q, (float)lo - 1.f), (float)hi + 1.f);   // (also ends a NaN or an infinite quotient; |q| <= 16, so the remainder is exact where it matters)
+    q = fminf(fmaxf(q, -17.f), 17.f);
     const float rem = __fmaf_rn(-q, s, x), twice = rem + rem;
     if (twice > s || (twice == s && ((int)q & 1))) q += 1.f;
     else if (-twice > s || (-twice == s && ((int)q & 1))) q -= 1.f;
-    return (int)fminf(fmaxf(q, (float)lo), (float)hi);
+    return q;
 }
 
 template <typename WT> __device__ __forceinline__ void load16(const WT *row, int k, int K, bool vec, float *v) {
     constexpr int N = Vec16<WT>::N;
     if (vec && k + 16 <= K) {
 #pragma unroll
-        for (int i = 0; i < 16; i += N) Vec16<WT>::load(row + k + i, v + i);
+        for (int i = 0; i < 16; i += N) Vec16<WT>::load_stream(row + k + i, v + i);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = k + i < K ? to_f(row[k + i]) : 0.f;
     }
 }
 
-// One warp: 16 rows x 128 columns (two tiles).  A unit is rows (g, g + 8) x one k16 step: its 32 codes are exactly four
-// words of the tile.  Lane l takes step l % 8 of rows l / 8 and l / 8 + 4 (mod 8), so eight neighbouring lanes read 128 contiguous columns of a
-// row, and a group's statistics are a butterfly over 2, 4 or 8 of them.
+// w[t] of four neighbouring lanes (steps 0..3 of a tile) <-> their 16 bytes in storage (lane t's words of steps 0..3)
+__device__ __forceinline__ uint4 transpose4(const uint32_t (&w)[4], int i) {
+    uint32_t o[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+        const int t = i ^ r;
+        const uint32_t send = t == 0 ? w[0] : t == 1 ? w[1] : t == 2 ? w[2] : w[3];
+        o[r] = r ? __shfl_xor_sync(0xffffffffu, send, r) : send;   // lane i ^ r's word i
+    }
+    uint4 v;
+    v.x = i == 0 ? o[0] : i == 1 ? o[1] : i == 2 ? o[2] : o[3];   // o[r] belongs at place i ^ r
+    v.y = i == 0 ? o[1] : i == 1 ? o[0] : i == 2 ? o[3] : o[2];
+    v.z = i == 0 ? o[2] : i == 1 ? o[3] : i == 2 ? o[0] : o[1];
+    v.w = i == 0 ? o[3] : i == 1 ? o[2] : i == 2 ? o[1] : o[0];
+    return v;
+}
+
+// One warp: one block.  A unit is rows (g, g + 8) x 16 columns (a step): its 32 codes are exactly four words.  Lane l takes step l % 8 of
+// rows l / 8 (+ 8), and of rows l / 8 + 4 (+ 8): eight neighbouring lanes read 128 contiguous columns of a row, and a group's
+// statistics are a butterfly over 2, 4 or 8 of them.
 template <typename WT>
-__global__ void __launch_bounds__(256) quantize_kernel(const WT *W, size_t ldw, int R, int K, int group, int scale_dtype, bool zp,
-                                                       uint32_t *codes, void *scales, uint8_t *zeros, int KT, int R16, bool vec) {
+__global__ void __launch_bounds__(256) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, step = lane & 7;
-    const int pairs = (KT + 1) / 2;
     const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (job >= (size_t)(R16 / 16) * pairs) return;
-    const int rb = (int)(job / pairs), kp = (int)(job % pairs);
-    const int k = kp * 128 + step * 16;
-    const int lanes = group / 16;   // lanes that share a group
+    if (job >= jobs) return;
+    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + step * 16;
+    unsigned char *blk = packed + job * q.block_bytes;
+    const int lanes = q.group / 16;   // lanes that share a group
 #pragma unroll
     for (int half = 0; half < 2; half++) {
         const int g8 = (lane >> 3) + 4 * half;
-        float s[2];
-        int z[2], c[2][16];
+        float v[2][16];
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int r = rb * 16 + g8 + 8 * h;
-            float v[16];
-            if (r < R) {
-                load16(W + (size_t)r * ldw, k, K, vec, v);
+            if (r < q.R) {
+                load16(W + (size_t)r * ldw, k, q.K, vec, v[h]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; i++) v[i] = 0.f;
+                for (int i = 0; i < 16; i++) v[h][i] = 0.f;
             }
+        }
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
             float lo = 0.f, hi = 0.f;
             bool bad = false;
 #pragma unroll
-            for (int i = 0; i < 16; i++) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); bad |= !(fabsf(v[i]) <= 3.402823466e38f); }
+            for (int i = 0; i < 16; i++) { lo = fminf(lo, v[h][i]); hi = fmaxf(hi, v[h][i]); bad |= v[h][i] != v[h][i]; }
+            bad |= hi > 3.402823466e38f || lo < -3.402823466e38f;
             for (int o = 1; o < lanes; o <<= 1) {
                 lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
                 hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
                 bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, o);
             }
-            s[h] = zp ? round_scale(((double)hi - (double)lo) / 15.0, scale_dtype) : round_scale((double)fmaxf(hi, -lo) / 7.0, scale_dtype);
-            if (bad) s[h] = __uint_as_float(0x7fc00000u);   // a NaN or infinity among the weights: the whole group reads back as NaN
-            const bool some = s[h] > 0.f && !bad;
-            z[h] = zp ? (some ? nearest_quotient(-lo, s[h], 0, 15) : 0) : 8;
+            float s = q.zp ? round_scale(((double)hi - (double)lo) / 15.0, q.scale_dtype) : round_scale((double)fmaxf(hi, -lo) / 7.0, q.scale_dtype);
+            if (bad) s = __uint_as_float(0x7fc00000u);   // a NaN or infinity among the weights: the whole group reads back as NaN
+            const bool some = s > 0.f;
+            const int z = q.zp ? (some ? (int)fminf(nearest_quotient(-lo, s), 15.f) : 0) : 8;
+            const float least = q.zp ? -(float)z : -8.f, most = q.zp ? 15.f - (float)z : 7.f;
 #pragma unroll
             for (int i = 0; i < 16; i++) {
-                const int lowest = -z[h];
                 // padding columns (and an all-zero group) hold the zero point's code: they stand for 0
-                c[h][i] = some && k + i < K ? (zp ? min(max(nearest_quotient(v[i], s[h], -15, 15), lowest), 15 - z[h]) : nearest_quotient(v[i], s[h], -8, 7)) + z[h] : z[h];
+                const int c = (some && k + i < q.K ? (int)fminf(fmaxf(nearest_quotient(v[h][i], s), least), most) : 0) + z;
+                w[i >> 2] |= (uint32_t)c << (8 * (i & 3) + 4 * h);
             }
-            if (step % lanes == 0 && k < K) {
-                const size_t at = (size_t)(k / group) * R16 + r;
-                if (scale_dtype == EESD_F32) ((float *)scales)[at] = s[h];
-                else ((__nv_bfloat16 *)scales)[at] = __float2bfloat16_rn(s[h]);
-                if (zp) zeros[at] = (uint8_t)z[h];
-            }
-        }
-        const int kt = kp * 2 + (step >> 2);
-        if (kt < KT) {
-#pragma unroll
-            for (int t = 0; t < 4; t++) {   // fragment columns 2t, 2t + 1 and 2t + 8, 2t + 9
-                uint32_t w = 0;
-#pragma unroll
-                for (int h = 0; h < 2; h++)
-#pragma unroll
-                    for (int q = 0; q < 2; q++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) w |= (uint32_t)c[h][q * 8 + 2 * t + e] << (4 * (h + 2 * q + 4 * e));
-                codes[(((size_t)rb * KT + kt) * 32 + g8 * 4 + t) * 4 + (step & 3)] = w;
+            if (step % lanes == 0) {
+                const int slot = scale_slot(g8 + 8 * h, step / lanes, 8 / lanes);
+                store_scale(blk, q, slot, s);
+                if (q.zp) blk[q.off_zeros + slot] = (unsigned char)z;
             }
         }
+        const uint4 o = transpose4(w, step & 3);
+        *reinterpret_cast<uint4 *>(blk + (step >> 2) * 512 + (g8 * 4 + (step & 3)) * 16) = o;
     }
 }
 
 template <typename OT>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint32_t *codes, const void *scales, const uint8_t *zeros, int R, int K, int group,
-                                                         int scale_dtype, OT *out, size_t ldo, int KT, int R16, bool vec) {
+__global__ void __launch_bounds__(256) dequantize_kernel(const unsigned char *packed, OT *out, size_t ldo, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, step = lane & 7;
-    const int pairs = (KT + 1) / 2;
     const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (job >= (size_t)(R16 / 16) * pairs) return;
-    const int rb = (int)(job / pairs), kp = (int)(job % pairs);
-    const int k = kp * 128 + step * 16, kt = kp * 2 + (step >> 2);
-    if (k >= K) return;
+    if (job >= jobs) return;
+    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + step * 16;
+    const unsigned char *blk = packed + job * q.block_bytes;
 #pragma unroll
     for (int half = 0; half < 2; half++) {
         const int g8 = (lane >> 3) + 4 * half;
-        uint32_t w[4];
-#pragma unroll
-        for (int t = 0; t < 4; t++) w[t] = __ldg(&codes[(((size_t)rb * KT + kt) * 32 + g8 * 4 + t) * 4 + (step & 3)]);
+        const uint4 raw = __ldcs(reinterpret_cast<const uint4 *>(blk + (step >> 2) * 512 + (g8 * 4 + (step & 3)) * 16));
+        const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
+        const uint4 tr = transpose4(in, step & 3);   // the transposition is its own inverse
+        const uint32_t w[4] = {tr.x, tr.y, tr.z, tr.w};
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int r = rb * 16 + g8 + 8 * h;
-            if (r >= R) continue;
-            const size_t at = (size_t)(k / group) * R16 + r;
-            const float s = scale_dtype == EESD_F32 ? ((const float *)scales)[at] : to_f(((const __nv_bfloat16 *)scales)[at]);
-            const int z = zeros ? zeros[at] : 8;
+            if (r >= q.R || k >= q.K) continue;
+            const int slot = scale_slot(r, step * 16 / q.group, 128 / q.group);
+            const float s = load_scale(blk, q, slot);
+            const int z = q.zp ? blk[q.off_zeros + slot] : 8;
             float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; i++) v[i] = __fmul_rn((float)((int)((w[(i & 7) >> 1] >> (4 * (h + 2 * (i >> 3) + 4 * (i & 1)))) & 15u) - z), s);
+            for (int i = 0; i < 16; i++) v[i] = __fmul_rn((float)((int)((w[i >> 2] >> (8 * (i & 3) + 4 * h)) & 15u) - z), s);
             OT *o = out + (size_t)r * ldo + k;
-            if (vec && k + 16 <= K) {
+            if (vec && k + 16 <= q.K) {
                 if constexpr (sizeof(OT) == 4) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
@@ -174,87 +188,76 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint32_t *codes, 
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; i++)
-                    if (k + i < K) o[i] = from_f<OT>(v[i]);
+                    if (k + i < q.K) o[i] = from_f<OT>(v[i]);
             }
         }
     }
 }
 
-// places codes given one per byte, row-major, and [R][G] scales / zero points into the stored order
-__global__ void __launch_bounds__(256) pack_kernel(const uint8_t *src, int R, int K, const void *sc, const uint8_t *zs, int scale_dtype, int group,
-                                                   uint32_t *codes, void *scales, uint8_t *zeros, int KT, int R16, int G) {
+// places codes given one per byte, row-major, and [R][G] scales / zero points into blocks (one warp: one block)
+__global__ void __launch_bounds__(256) pack_kernel(const uint8_t *src, const void *sc, const uint8_t *zs, unsigned char *packed, const Geom q, size_t jobs) {
     pdl_wait();
     pdl_trigger();
-    const size_t words = (size_t)(R16 / 16) * KT * 128, n = (size_t)gridDim.x * blockDim.x;
-    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < words; i += n) {
-        const int j = (int)(i & 3), lane = (int)((i >> 2) & 31);
-        const size_t tile = i >> 7;
-        const int rb = (int)(tile / KT), kt = (int)(tile % KT);
+    const int lane = threadIdx.x & 31;
+    const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (job >= jobs) return;
+    const int rb = (int)(job / q.KB), k0 = (int)(job % q.KB) * 128, G = (q.K + q.group - 1) / q.group;
+    unsigned char *blk = packed + job * q.block_bytes;
+#pragma unroll 1
+    for (int i = 0; i < 8; i++) {
+        const int tile = i >> 2, j = i & 3;
         uint32_t w = 0;
 #pragma unroll
         for (int b = 0; b < 8; b++) {
-            const int h = b & 1, q = (b >> 1) & 1, e = b >> 2;
-            const int r = rb * 16 + (lane >> 2) + 8 * h, k = kt * 64 + j * 16 + (lane & 3) * 2 + 8 * q + e;
-            uint32_t c = 8;
-            if (r < R && k < K) c = src[(size_t)r * K + k] & 15u;
-            else if (zs) c = r < R ? zs[(size_t)r * G + min(k, K - 1) / group] & 15u : 0u;   // padding stands for 0
+            const int r = rb * 16 + (lane >> 2) + 8 * (b & 1), k = k0 + tile * 64 + j * 16 + (lane & 3) * 4 + (b >> 1);
+            uint32_t c = 8;   // padding stands for 0
+            if (r < q.R && k < q.K) c = src[(size_t)r * q.K + k] & 15u;
+            else if (zs) c = r < q.R ? zs[(size_t)r * G + min(k / q.group, G - 1)] & 15u : 0u;
             w |= c << (4 * b);
         }
-        codes[i] = w;
+        *reinterpret_cast<uint32_t *>(blk + tile * 512 + lane * 16 + j * 4) = w;
     }
-    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)G * R16; i += n) {
-        const int r = (int)(i % R16), g = (int)(i / R16);
+    const int n = 128 / q.group;
+    for (int i = lane; i < n * 16; i += 32) {
+        const int r = rb * 16 + (i & 15), g = k0 / q.group + (i >> 4), slot = scale_slot(i & 15, i >> 4, n);
+        const bool in = r < q.R && g < G;
         const size_t at = (size_t)r * G + g;
-        if (scale_dtype == EESD_F32) ((float *)scales)[i] = r < R ? ((const float *)sc)[at] : 0.f;
-        else ((__nv_bfloat16 *)scales)[i] = r < R ? ((const __nv_bfloat16 *)sc)[at] : __float2bfloat16_rn(0.f);
-        if (zs) zeros[i] = r < R ? zs[at] & 15u : 0;
+        store_scale(blk, q, slot, !in ? 0.f : q.scale_dtype == EESD_F32 ? ((const float *)sc)[at] : to_f(((const __nv_bfloat16 *)sc)[at]));
+        // (a padded group's codes are those of the last real one: so is its zero point)
+        if (zs) blk[q.off_zeros + slot] = r < q.R ? zs[(size_t)r * G + min(g, G - 1)] & 15u : 0;
     }
 }
 
 // ------------------------------------------------------------------------------------ projection
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
-    __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
-    return *reinterpret_cast<uint32_t *>(&r);
-}
-__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
-    __half2 r = __hfma2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b), *reinterpret_cast<__half2 *>(&c));
-    return *reinterpret_cast<uint32_t *>(&r);
-}
-__device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
+// A block of threads (one per multiprocessor, kWarps warps) owns a run of row blocks and a slice of K; the slices of a
+// run are one cluster.  Its (row block, 128 columns) units, in storage order, are cut evenly among its warps, so the load is even
+// to one unit whatever the shape; a warp's first and last row block may be shared with its neighbours and are added up at the end.
+// Weights go straight into registers, kAhead units ahead.
+//
+// The products are integer: a code enters as the signed byte 16 (c - 8), its four bits with the top one flipped in the byte's upper half
+// (one three-input logic operation, for half the registers after one shift), an activation as
+// signed 8-bit digits of a fixed-point number, one power-of-two scale for each token row and 128 columns; a digit is a
+// column of the matrix instruction.  The sums of a group are exact, a zero point is taken off them exactly (16 (z - 8) times the group's
+// sum of digits), and fp32 begins where a group's sum meets its scale.  Up to 4 rows take 4 digits (31 bits of the largest
+// magnitude in the 128 columns), more rows 3 (22.99 bits).  Against fp16 terms (two per fp32 row, 1024 + c minus 1024 + z) this
+// takes 3 instead of 9 operations for 8 codes, half to three quarters of the matrix instructions (both kinds: one per 8
+// cycles and sub-processor, measured), and keeps the sums exact.
+constexpr int kWarps = 16;
+template <int NT> constexpr int kAhead = NT == 6 ? 2 : 4;   // units a warp's loads run ahead
+template <int NT> constexpr int kDigits = NT <= 2 ? 4 : 3;
+template <int NT> constexpr int kTok = NT == 1 ? 2 : NT == 2 ? 4 : NT == 3 ? 8 : 16;   // token rows; column d * kTok + m is digit d of row m
+constexpr int kMaxRun = 32;     // row blocks of a run
+constexpr int kSmem = 227 * 1024;
+// staged activations of 128 columns: fragments [step pair][n-tile][lane][4 words], then {sum of the group's digits, unscale} [group][column]
+__host__ __device__ constexpr int act_bytes(int NT, int G) { return 1024 * NT + 128 / G * NT * 64; }
 
 struct ProjArgs {
-    const uint4 *codes;
-    const void *scales;
-    const uint8_t *zeros;
+    const unsigned char *packed;
     const void *A;
+    const unsigned char *frag;   // staged form of A (stage_kernel); null: every block of threads stages for itself
     float *out;
     size_t lda, ldo;
-    int R, R16, K, KT, M, a_dtype, scale_dtype, vec;
-};
-
-constexpr int kWarps = 8;
-
-// NT n-tiles of 8 columns; an fp32 row takes two columns (two fp16 terms), a bf16 row one.  RB row blocks of 16 per warp.
-// KC: tiles (64 columns of the matrix) whose activations are staged at a time.
-template <int NT, int RB> struct Shape {
-    static constexpr int rows = kWarps * RB * 16;
-    static constexpr int U = RB == 1 ? 4 : 2;         // tiles a warp loads ahead
-    static constexpr int KC = NT == 1 ? 16 : 8;
-    static constexpr int act_words = KC * 4 * NT * 64;
-    static constexpr int red_ld = rows + 4;
-    __host__ __device__ static constexpr size_t act_bytes() {
-        const size_t act = (size_t)act_words * 4, red = (size_t)(NT == 1 ? 8 : EESD_MAX_ROWS) * red_ld * 4;
-        return act > red ? act : red;
-    }
+    int R, K, KB, RB, M, a_dtype, vec, chunk;   // KB, RB: blocks along K, row blocks; chunk: blocks along K staged at a time
 };
 
 __device__ __forceinline__ float4 load_a4(const ProjArgs &p, int m, int k) {
@@ -276,280 +279,373 @@ __device__ __forceinline__ float4 load_a4(const ProjArgs &p, int m, int k) {
     return make_float4(v[0], v[1], v[2], v[3]);
 }
 
-// The activations enter as fp16 after a power-of-two scale per token row that puts the largest staged magnitude into
-// [2^14, 2^15): an fp32 row as two terms (22 bits; what is below 2^-39 of the row's largest is lost), a bf16 row as one (exact
-// down to 2^-29 of it).  Fields are the biased exponents of that scale; they only ever fall, so sums already taken are brought
-// along by an exact multiplication.
-__device__ __forceinline__ int scale_field(uint32_t max_bits) {
-    if (max_bits >= 0x7f800000u) return 127;            // an infinity or NaN: the row's results are not finite anyway
-    const int f = 268 - (int)(max_bits >> 23);          // 2^(14 - exponent)
-    return f < 253 ? f : 253;
+// A warp turns 128 columns of token row m (lane: columns 4 * lane .. + 3) into digits at dst.  The scale 2^f puts the largest
+// magnitude just below 127.5 * 256^(digits - 1), as far up as signed digits reach; f stops at 126 (so that 2^-f stays normal).
+template <int NT, int G>
+__device__ __forceinline__ void stage_piece(unsigned char *dst, float4 v, int m) {
+    constexpr int D = kDigits<NT>, TOK = kTok<NT>;
+    const int lane = threadIdx.x & 31;
+    const uint32_t mx = __reduce_max_sync(0xffffffffu, max(max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu),
+                                                           max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu)));
+    const bool bad = mx >= 0x7f800000u;   // a NaN or infinity: the row's results are NaN
+    int f = (D == 4 ? 30 : 22) + 127 - (int)(mx >> 23);
+    if (f > 126) f = 126;
+    if (__uint_as_float(mx) * __int_as_float((127 + f) << 23) > (D == 4 ? 2139062016.f : 8355711.f)) f--;   // 0x7f7f7f00, 0x7f7f7f
+    const float sc = bad ? 0.f : __int_as_float((127 + f) << 23);
+    const float un = (bad ? __uint_as_float(0x7fc00000u) : __int_as_float((127 - f) << 23)) * 0.0625f;   // (codes enter 16-fold)
+    constexpr uint32_t bias = D == 4 ? 0x80808080u : 0x00808080u;   // q + bias has the digits + 128 as its bytes
+    uint32_t q[4];
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) q[i] = ((uint32_t)(bad ? 0 : __float2int_rn(x[i] * sc)) + bias) ^ bias;
+    // word d: digit d of the four columns
+    const uint32_t lo01 = __byte_perm(q[0], q[1], 0x5140), lo23 = __byte_perm(q[2], q[3], 0x5140), hi01 = __byte_perm(q[0], q[1], 0x7362), hi23 = __byte_perm(q[2], q[3], 0x7362);
+    const uint32_t w[4] = {__byte_perm(lo01, lo23, 0x5410), __byte_perm(lo01, lo23, 0x7632), __byte_perm(hi01, hi23, 0x5410), __byte_perm(hi01, hi23, 0x7632)};
+    uint32_t *act = reinterpret_cast<uint32_t *>(dst);
+    const int step = lane >> 3, half = (lane >> 2) & 1, t = lane & 3;
+#pragma unroll
+    for (int d = 0; d < D; d++) {
+        const int col = d * TOK + m;
+        act[(((step >> 1) * NT + (col >> 3)) * 32 + (col & 7) * 4 + t) * 4 + (step & 1) * 2 + half] = w[d];
+    }
+    // sums of a group's digits, two at a time as 16-bit fields of the bytes + 128
+#pragma unroll
+    for (int d = 0; d < D; d += 2) {
+        uint32_t sum = __dp4a(w[d] ^ 0x80808080u, 0x01010101u, 0u) | __dp4a(w[d + 1] ^ 0x80808080u, 0x01010101u, 0u) << 16;
+        if (G == 128) sum = __reduce_add_sync(0xffffffffu, sum);
+        else
+#pragma unroll
+            for (int o = 1; o < G / 4; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane % (G / 4) == 0) {
+            float2 *c = reinterpret_cast<float2 *>(dst + 1024 * NT) + lane / (G / 4) * NT * 8 + m;
+            c[d * TOK] = make_float2(__int_as_float((int)(sum & 0xffffu) - 128 * G), un * (float)(1u << (8 * d)));
+            if (d + 1 < D) c[(d + 1) * TOK] = make_float2(__int_as_float((int)(sum >> 16) - 128 * G), un * (float)(1ull << (8 * d + 8)));
+        }
+    }
 }
 
-template <int NT, int RB, int G, bool ZP>
-__global__ void __launch_bounds__(kWarps * 32) project_kernel(const ProjArgs p) {
-    using S = Shape<NT, RB>;
-    constexpr int U = S::U, KC = S::KC, ROWS = S::rows;
-    extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t *act = reinterpret_cast<uint32_t *>(smem);   // activations as B fragments [tile][step pair][n-tile][lane][4]; afterwards the partial results
-    float *sS = reinterpret_cast<float *>(smem + S::act_bytes());   // scales of the staged groups, [group][row]
-    constexpr int kGrp = KC * 64 / G + 1;
-    uint8_t *sZ = reinterpret_cast<uint8_t *>(sS + kGrp * ROWS);
-    __shared__ uint32_t s_max[2][EESD_MAX_ROWS];
-    __shared__ int s_field[2][EESD_MAX_ROWS];
+// the same for a whole matrix, into global memory (many token rows: staging once costs less than once per block of threads)
+template <int NT, int G>
+__global__ void __launch_bounds__(256) stage_kernel(const ProjArgs p, unsigned char *frag) {
+    pdl_wait();      // everything before this launch is complete once the trigger fires: the projection may read the matrix before its own wait
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, job = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (job >= p.KB * p.M) return;
+    const int m = job / p.KB, kb = job % p.KB;
+    stage_piece<NT, G>(frag + (size_t)kb * act_bytes(NT, G), load_a4(p, m, kb * 128 + lane * 4), m);
+}
 
+// (x ^ 0x80..) & 0xf0..: in every byte 16 times the code of its upper half less 8 (with both constants known the compiler would
+// take two operations)
+__device__ __forceinline__ uint32_t signed16(uint32_t x, uint32_t flip) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(x), "r"(flip), "n"(0xf0f0f0f0));   // (a ^ b) & c
+    return r;
+}
+// s8 x s8 products onto c (an exact integer sum)
+__device__ __forceinline__ void mma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const int (&c)[4]) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const unsigned char *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// N bytes (2 to 32) of a matrix that is read once
+template <int N> struct Bytes { uint32_t v[(N + 3) / 4]; };
+template <int N> __device__ __forceinline__ void load_once(Bytes<N> &d, const unsigned char *p) {
+    if constexpr (N == 2) asm volatile("{.reg .b16 t; ld.global.L1::no_allocate.b16 t, [%1]; cvt.u32.u16 %0, t;}" : "=r"(d.v[0]) : "l"(p));
+    if constexpr (N == 4) asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(d.v[0]) : "l"(p));
+    if constexpr (N == 8) asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(d.v[0]), "=r"(d.v[1]) : "l"(p));
+    if constexpr (N >= 16)
+#pragma unroll
+        for (int i = 0; i < N / 16; i++)
+            asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(d.v[4 * i]), "=r"(d.v[4 * i + 1]), "=r"(d.v[4 * i + 2]), "=r"(d.v[4 * i + 3]) : "l"(p + 16 * i));
+}
+
+// shared memory: activations | partial results of shared row blocks | results
+struct Smem { int slots, outs, total; };
+__host__ __device__ inline Smem carve(int NT, int G, int M, int chunk, int run) {
+    Smem s;
+    s.slots = chunk * act_bytes(NT, G);
+    s.outs = s.slots + kWarps * 2 * M * 64;
+    s.total = s.outs + run * M * 64;
+    return s;
+}
+
+// first unit of warp w
+__device__ __forceinline__ int unit_of(int units, int w) { return (int)(((long long)units * w) / kWarps); }
+
+template <int NT, int G, bool ZP, bool F32S>
+__global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs p) {
+    constexpr int NG = 128 / G, kScaleBytes = 2 * NG * (F32S ? 4 : 2), kZeros = 1024 + 8 * kScaleBytes, kRecord = kZeros + (ZP ? NG * 16 : 0), U = kAhead<NT>;
+    constexpr int kAct = act_bytes(NT, G), NA = NT == 6 ? 2 : 1;   // NA: n-tiles that hold different token rows
+    extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t = lane & 3;
-    const int splits = (int)gridDim.y, split = (int)blockIdx.y;
-    const int kt0 = (int)((long long)p.KT * split / splits), n = (int)((long long)p.KT * (split + 1) / splits) - kt0;
-    const int row0 = blockIdx.x * ROWS;
-    const bool two = p.a_dtype == EESD_F32;
-    const int n_tok = two ? NT * 4 : NT * 8;             // token rows the n-tiles can hold
+    const int splits = (int)gridDim.y, split = (int)blockIdx.y, runs = (int)gridDim.x;
+    const int rb0 = (int)((long long)p.RB * blockIdx.x / runs), run = (int)((long long)p.RB * (blockIdx.x + 1) / runs) - rb0;
+    const int kb0 = (int)((long long)p.KB * split / splits), kbn = (int)((long long)p.KB * (split + 1) / splits) - kb0;
+    const Smem sm = carve(NT, G, p.M, p.chunk, 0);
+    unsigned char *act = smem;
+    float *slots = reinterpret_cast<float *>(smem + sm.slots), *outs = reinterpret_cast<float *>(smem + sm.outs);
 
-    if (tid < EESD_MAX_ROWS) { s_max[0][tid] = 0; s_field[1][tid] = 253; }
-    pdl_wait();
+    if (!p.frag) pdl_wait();   // (with staged activations the launch before this one is their kernel, and the matrix is complete already)
     pdl_trigger();
 
-    const uint4 *src[RB];
-    bool live[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; rb++) {
-        const int blk = row0 / 16 + warp * RB + rb;
-        live[rb] = blk * 16 < p.R16;
-        src[rb] = p.codes + ((size_t)(live[rb] ? blk : 0) * p.KT + kt0) * 32 + lane;
-    }
-    uint4 cur[U][RB], nxt[U][RB];
-    auto fetch = [&](uint4 (&w)[U][RB], int base) {
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int rb = 0; rb < RB; rb++)
-                w[u][rb] = base + u < n && live[rb] ? ld_stream(src[rb] + (size_t)(base + u) * 32) : make_uint4(0, 0, 0, 0);
-    };
-    fetch(cur, 0);
-
-    float acc[RB][NT][4], gacc[RB][NT][4];
-#pragma unroll
-    for (int rb = 0; rb < RB; rb++)
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) acc[rb][nt][i] = gacc[rb][nt][i] = 0.f;
-
-    int g0 = 0;   // first staged group
-    auto stage = [&](int c0) {
-        const int ph = (c0 / KC) & 1;
-        const int k0 = (kt0 + c0) * 64, nk = min(KC, n - c0) * 64, pieces = (nk + 127) / 128;
-        __syncthreads();   // the previous stage is used up; s_max[ph] is zero
-        for (int it = warp; it < p.M * pieces; it += kWarps) {
-            const int m = it % p.M, k = it / p.M * 128 + lane * 4;
-            uint32_t mx = 0;
-            if (k < nk) {
-                const float4 v = load_a4(p, m, k0 + k);
-                mx = max(max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu),
-                         max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu));
+    for (int c0 = 0; c0 < kbn; c0 += p.chunk) {
+        const int cn = min(p.chunk, kbn - c0);
+        const int units = run * cn;
+        const int u0 = unit_of(units, warp), u1 = unit_of(units, warp + 1);
+        const int rb_first = u0 / cn;
+        int rbi = rb_first, kp = u0 - rbi * cn;
+        // loads ahead: unit fu at src, fleft units to the end of its row block
+        struct Unit {
+            Bytes<16> w[2];
+            Bytes<kScaleBytes> s;
+            Bytes<2 * NG> z;
+        } ring[U];
+        const unsigned char *src = p.packed + ((size_t)(rb0 + rbi) * p.KB + kb0 + c0 + kp) * kRecord;
+        const size_t jump = (size_t)(p.KB - cn) * kRecord;
+        int fleft = cn - kp, fu = u0;
+        auto fetch = [&](Unit &r) {
+            if (fu < u1) {
+                load_once(r.w[0], src + lane * 16);
+                load_once(r.w[1], src + 512 + lane * 16);
+                load_once(r.s, src + 1024 + g8 * kScaleBytes);
+                if (ZP) load_once(r.z, src + kZeros + g8 * 2 * NG);
             }
-            mx = __reduce_max_sync(0xffffffffu, mx);
-            if (lane == 0) atomicMax(&s_max[ph][m], mx);
-        }
-        g0 = k0 / G;
-        const int ng = (k0 + nk - 1) / G - g0 + 1, groups = (p.K + G - 1) / G;   // (a group past the end only meets zero activations: scale 0)
-        for (int i = tid; i < ng * ROWS; i += kWarps * 32) {
-            const int gr = i / ROWS, r = row0 + i % ROWS;
-            const size_t at = (size_t)(g0 + gr) * p.R16 + r;
-            const bool in = r < p.R16 && g0 + gr < groups;
-            sS[i] = in ? (p.scale_dtype == EESD_F32 ? __ldg((const float *)p.scales + at) : to_f(__ldg((const __nv_bfloat16 *)p.scales + at))) : 0.f;
-            if (ZP) sZ[i] = in ? __ldg(p.zeros + at) : 0;
-        }
-        __syncthreads();
-        for (int it = warp; it < p.M * pieces; it += kWarps) {
-            const int m = it % p.M, k = it / p.M * 128 + lane * 4;
-            const int field = min(s_field[ph ^ 1][m], scale_field(s_max[ph][m]));
-            if (k < nk) {
-                const float4 v = load_a4(p, m, k0 + k);
-                const float sc = __int_as_float(field << 23);
-                const float x[4] = {v.x * sc, v.y * sc, v.z * sc, v.w * sc};
-                __half hi[4], lo[4];
+            fu++;
+            src += kRecord;
+            if (--fleft == 0) { fleft = cn; src += jump; }
+        };
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    hi[i] = __float2half_rn(x[i]);
-                    lo[i] = __float2half_rn(x[i] - __half2float(hi[i]));
-                }
-                const int j = (k & 63) >> 4, q = (k >> 3) & 1, tt = (k & 7) >> 1;
-                auto put = [&](int col, const __half *h) {
-                    uint32_t *d = act + ((((k >> 6) * 2 + (j >> 1)) * NT + (col >> 3)) * 32 + (col & 7) * 4 + tt) * 4 + (j & 1) * 2 + q;
-                    __half2 a = __halves2half2(h[0], h[1]), b = __halves2half2(h[2], h[3]);
-                    d[0] = *reinterpret_cast<uint32_t *>(&a);
-                    d[4] = *reinterpret_cast<uint32_t *>(&b);
-                };
-                put(m, hi);
-                if (two) put(m + n_tok, lo);
-            }
-        }
-        if (c0) {   // bring the sums along to the new scale
-            float f[NT][2];
+        for (int s = 0; s < U; s++) fetch(ring[s]);
+
+        if (c0) __syncthreads();   // the previous chunk's activations are used up
+        if (p.frag) {
+            if (!c0) pdl_wait();
+            const unsigned char *f = p.frag + (size_t)(kb0 + c0) * kAct;
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(act);
+            for (int i = tid * 16; i < cn * kAct; i += kWarps * 512) copy16(at + i, f + i);
+            asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+        } else {
+            constexpr int kBatch = 4;
+            for (int it0 = warp; it0 < p.M * cn; it0 += kWarps * kBatch) {
+                float4 v[kBatch];
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const int m = (nt * 8 + 2 * t + e) % n_tok;
-                    const int old = s_field[ph ^ 1][m], d = min(old, scale_field(s_max[ph][m])) - old;
-                    f[nt][e] = m >= p.M || d == 0 ? 1.f : d < -126 ? 0.f : __int_as_float((127 + d) << 23);
+                for (int i = 0; i < kBatch; i++) {
+                    const int it = it0 + i * kWarps, m = it / cn, k = (kb0 + c0 + it - m * cn) * 128 + lane * 4;
+                    v[i] = it < p.M * cn ? load_a4(p, m, k) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
 #pragma unroll
-            for (int rb = 0; rb < RB; rb++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) acc[rb][nt][i] *= f[nt][i & 1];
-        }
-        if (tid < EESD_MAX_ROWS) {
-            s_field[ph][tid] = min(s_field[ph ^ 1][tid], scale_field(s_max[ph][tid]));
-            s_max[ph ^ 1][tid] = 0;
-        }
-        __syncthreads();
-    };
-
-    auto fold = [&](int gr) {   // group sums times the group's scales into the totals
-#pragma unroll
-        for (int rb = 0; rb < RB; rb++) {
-            const float *s = sS + gr * ROWS + (warp * RB + rb) * 16 + g8;
-            const float s0 = s[0], s1 = s[8];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                acc[rb][nt][0] = fmaf(gacc[rb][nt][0], s0, acc[rb][nt][0]);
-                acc[rb][nt][1] = fmaf(gacc[rb][nt][1], s0, acc[rb][nt][1]);
-                acc[rb][nt][2] = fmaf(gacc[rb][nt][2], s1, acc[rb][nt][2]);
-                acc[rb][nt][3] = fmaf(gacc[rb][nt][3], s1, acc[rb][nt][3]);
-                gacc[rb][nt][0] = gacc[rb][nt][1] = gacc[rb][nt][2] = gacc[rb][nt][3] = 0.f;
+                for (int i = 0; i < kBatch; i++) {
+                    const int it = it0 + i * kWarps, m = it / cn;
+                    if (it < p.M * cn) stage_piece<NT, G>(act + (it - m * cn) * kAct, v[i], m);
+                }
             }
         }
-    };
+        __syncthreads();
 
-    for (int base = 0; base < n; base += U) {
-        fetch(nxt, base + U);
-        if (base % KC == 0) stage(base);
+        float acc[NA][4];
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int c = base + u;
-            if (c < n) {
-                const int k0 = (kt0 + c) * 64;
-                const uint4 *bp = reinterpret_cast<const uint4 *>(act) + (size_t)(c % KC) * 2 * NT * 32 + lane;
-                uint32_t z0[RB], z1[RB];
+        for (int n = 0; n < NA; n++)
 #pragma unroll
-                for (int jp = 0; jp < 2; jp++) {
-                    const int gr = (k0 + jp * 32) / G - g0;
-                    if (jp == 0 || G == 32) {
+            for (int i = 0; i < 4; i++) acc[n][i] = 0.f;
+        // A sum starts at the bits of 1.5 * 2^23, so that it reads as 12582912 + sum in fp32 (|sum| <= 2^21, with the zero point's part below 2^22)
+        const int start[4] = {0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000};
+        uint32_t flip;
+        asm volatile("mov.b32 %0, 0x80808080;" : "=r"(flip));
+        const unsigned char *bp = act + kp * kAct;
+        for (int u = u0; u < u1;) {
 #pragma unroll
-                        for (int rb = 0; rb < RB; rb++) {
-                            // 1024 + z and -(64 + z) as fp16 pairs, by their bit patterns
-                            if (ZP) {
-                                const uint8_t *z = sZ + gr * ROWS + (warp * RB + rb) * 16 + g8;
-                                z0[rb] = 0x64006400u + (uint32_t)z[0] * 0x00010001u;
-                                z1[rb] = 0xD400D400u + (uint32_t)z[8] * 0x00100010u;
-                            } else {
-                                z0[rb] = 0x64086408u;
-                                z1[rb] = 0xD480D480u;
-                            }
-                        }
-                    }
+            for (int slot = 0; slot < U; slot++) {
+                if (u == u1) break;
+                Unit &r = ring[slot];
+                int g[NT][4];
+#pragma unroll
+                for (int jp = 0; jp < 2; jp++) {   // 64 columns: a tile, two steps
                     uint4 b[NT];
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) b[nt] = bp[(jp * NT + nt) * 32];
+                    for (int nt = 0; nt < NT; nt++) b[nt] = *reinterpret_cast<const uint4 *>(bp + (jp * NT + nt) * 512 + lane * 16);
 #pragma unroll
                     for (int jj = 0; jj < 2; jj++) {
+                        const uint32_t x = r.w[jp].v[jj * 2], y = r.w[jp].v[jj * 2 + 1];
+                        const uint32_t a[4] = {signed16(x << 4, flip), signed16(x, flip), signed16(y << 4, flip), signed16(y, flip)};
+                        const bool first = (jp * 2 + jj) % (G / 32) == 0;
 #pragma unroll
-                        for (int rb = 0; rb < RB; rb++) {
-                            const uint4 v = cur[u][rb];
-                            const uint32_t w = jp == 0 ? (jj == 0 ? v.x : v.y) : (jj == 0 ? v.z : v.w), w8 = w >> 8;
-                            uint32_t a[4];
-                            a[0] = h2_sub((w & 0x000f000fu) | 0x64006400u, z0[rb]);               // 1024 + c - (1024 + z)
-                            a[1] = h2_fma((w & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, z1[rb]);   // (1024 + 16 c) / 16 - (64 + z)
-                            a[2] = h2_sub((w8 & 0x000f000fu) | 0x64006400u, z0[rb]);
-                            a[3] = h2_fma((w8 & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, z1[rb]);
-#pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma_16816(gacc[rb][nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w);
+                        for (int nt = 0; nt < NT; nt++) {
+                            if (first) mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, start);
+                            else mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, g[nt]);
                         }
+                        if ((jp * 64 + jj * 32 + 32) % G != 0) continue;
+                        // the group is complete: digits' sums less z times the activations' to fp32, the digits joined, times the scale
+                        const int gr = (jp * 64 + jj * 32) / G;
+                        float s0, s1;
+                        if (F32S) {
+                            s0 = __uint_as_float(r.s.v[gr]);
+                            s1 = __uint_as_float(r.s.v[NG + gr]);
+                        } else {   // halfwords gr and NG + gr
+                            const uint32_t sa = r.s.v[gr / 2], sb = r.s.v[(NG + gr) / 2];
+                            s0 = __uint_as_float(gr & 1 ? sa & 0xffff0000u : sa << 16);
+                            s1 = __uint_as_float((NG + gr) & 1 ? sb & 0xffff0000u : sb << 16);
+                        }
+                        int z0 = 0, z1 = 0;   // 16 (8 - z)
+                        if (ZP) {   // bytes gr and NG + gr
+                            z0 = 128 - 16 * (int)(r.z.v[gr / 4] >> (8 * (gr % 4)) & 0xffu);
+                            z1 = 128 - 16 * (int)(r.z.v[(NG + gr) / 4] >> (8 * ((NG + gr) % 4)) & 0xffu);
+                        }
+                        float h[NA][4];
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++) {
+                            const float4 c = *reinterpret_cast<const float4 *>(bp + 1024 * NT + (gr * NT + nt) * 64 + t * 16);   // columns 2t, 2t + 1: {sum, unscale}
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                const float q = __int_as_float(ZP ? g[nt][i] + (i < 2 ? z0 : z1) * __float_as_int(i & 1 ? c.z : c.x) : g[nt][i]) - 12582912.f, un = i & 1 ? c.w : c.y;
+                                h[nt % NA][i] = nt < NA ? q * un : fmaf(q, un, h[nt % NA][i]);
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < NA; n++)
+#pragma unroll
+                            for (int i = 0; i < 4; i++) acc[n][i] = fmaf(h[n][i], i < 2 ? s0 : s1, acc[n][i]);
                     }
-                    if (G == 32) fold(gr);
-                    else if (jp == 1 && (G == 64 || ((kt0 + c) & 1) || c == n - 1 || c % KC == KC - 1)) fold(gr);
+                }
+                fetch(r);
+                u++;
+                bp += kAct;
+                if (++kp == cn || u == u1) {
+                    // the row block's sums: to the results where the warp had all of it, else to the warp's slot for its first or last row block
+                    const bool first = rbi == rb_first, last = u == u1;
+                    float *d = first ? slots + warp * 2 * p.M * 16 : last ? slots + (warp * 2 + 1) * p.M * 16 : outs + rbi * p.M * 16;
+                    const bool add = !first && !last && c0;
+#pragma unroll
+                    for (int n = 0; n < NA; n++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            float v = acc[n][i];
+                            if (kTok<NT> <= 4) v += __shfl_xor_sync(0xffffffffu, v, 2);   // digits in other lanes of the quad
+                            if (kTok<NT> == 2) v += __shfl_xor_sync(0xffffffffu, v, 1);
+                            const int m = n * 8 + 2 * t + (i & 1);
+                            if (m < kTok<NT> && m < p.M) {
+                                float *o = d + m * 16 + g8 + (i >> 1) * 8;
+                                *o = add ? *o + v : v;
+                            }
+                            acc[n][i] = 0.f;
+                        }
+                    kp = 0;
+                    bp = act;
+                    rbi++;
                 }
             }
         }
+        __syncthreads();
+        // shared row blocks: the warps' parts in order
+        for (int i = warp; i < run; i += kWarps) {
+            const int a0 = i * cn, a1 = a0 + cn;
+            int w = (int)(((long long)a0 * kWarps) / units);   // next to the warp that holds unit a0
+            while (unit_of(units, w) > a0) w--;
+            while (unit_of(units, w + 1) <= a0) w++;
+            const int b0 = unit_of(units, w), b1 = unit_of(units, w + 1);
+            if (b0 < a0 && b1 > a1) continue;                  // inside one warp's range: already in the results
+            float v[EESD_MAX_ROWS / 2];
 #pragma unroll
-        for (int u = 0; u < U; u++)
+            for (int j = 0; j < EESD_MAX_ROWS / 2; j++) v[j] = c0 && j * 32 + lane < p.M * 16 ? outs[i * p.M * 16 + j * 32 + lane] : 0.f;
+            for (int x0 = b0; x0 < a1; w++, x0 = unit_of(units, w)) {
+                if (unit_of(units, w + 1) == x0) continue;     // a warp without units
+                const float *part = slots + (w * 2 + (x0 < a0)) * p.M * 16 + lane;   // its first row block, or (begun before this one) its last
 #pragma unroll
-            for (int rb = 0; rb < RB; rb++) cur[u][rb] = nxt[u][rb];
+                for (int j = 0; j < EESD_MAX_ROWS / 2; j++)
+                    if (j * 32 + lane < p.M * 16) v[j] += part[j * 32];
+            }
+#pragma unroll
+            for (int j = 0; j < EESD_MAX_ROWS / 2; j++)
+                if (j * 32 + lane < p.M * 16) outs[i * p.M * 16 + j * 32 + lane] = v[j];
+        }
     }
 
-    // partial results [token][row] into shared memory: the two terms joined, the power of two taken out
-    const int last = n > 0 ? ((n - 1) / KC) & 1 : 1;
-    __syncthreads();
-    float *red = reinterpret_cast<float *>(act);
-#pragma unroll
-    for (int rb = 0; rb < RB; rb++) {
-        const int r = (warp * RB + rb) * 16 + g8;
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                float v = acc[rb][nt][i];
-                const int col = nt * 8 + 2 * t + (i & 1);
-                if (two) {
-                    if constexpr (NT == 1) v += __shfl_xor_sync(0xffffffffu, v, 2);   // columns c and c + 4
-                    else if (nt < NT / 2) v += acc[rb][nt + NT / 2][i];
-                }
-                if (col < n_tok && col < p.M) red[col * S::red_ld + r + (i >> 1) * 8] = v * __int_as_float((254 - s_field[last][col]) << 23);
+    // the slices of K are one cluster: every block adds up its share of the row blocks over all of them, in slice order
+    if (splits > 1) cg::this_cluster().sync();
+    else __syncthreads();
+    for (int i = split + warp * splits; i < run; i += kWarps * splits)
+        for (int e = lane; e < p.M * 16; e += 32) {
+            const int m = e >> 4, r = (rb0 + i) * 16 + (e & 15);
+            float v = 0.f;
+            if (splits > 1) {
+                for (int s = 0; s < splits; s++) v += cg::this_cluster().map_shared_rank(outs, s)[i * p.M * 16 + e];
+            } else {
+                v = outs[i * p.M * 16 + e];
             }
-    }
-    const int total = p.M * ROWS;
-    if (splits == 1) {
-        __syncthreads();
-        for (int i = tid; i < total; i += kWarps * 32) {
-            const int m = i / ROWS, r = i % ROWS;
-            if (row0 + r < p.R) p.out[(size_t)m * p.ldo + row0 + r] = red[m * S::red_ld + r];
+            if (r < p.R) p.out[(size_t)m * p.ldo + r] = v;
         }
-        return;
-    }
-    // the slices of K are one cluster: every block adds its share of the rows over all of them, in slice order
-    cg::cluster_group cl = cg::this_cluster();
-    cl.sync();
-    for (int i = split * kWarps * 32 + tid; i < total; i += splits * kWarps * 32) {
-        const int m = i / ROWS, r = i % ROWS;
-        float v = 0.f;
-        for (int s = 0; s < splits; s++) v += cl.map_shared_rank(red, s)[m * S::red_ld + r];
-        if (row0 + r < p.R) p.out[(size_t)m * p.ldo + row0 + r] = v;
-    }
-    cl.sync();   // nobody leaves while its partial results are still being read
+    if (splits > 1) cg::this_cluster().sync();   // nobody leaves while its results are still being read
 }
 
-template <int NT, int RB, int G, bool ZP>
-cudaError_t launch_project(cudaStream_t s, const ProjArgs &p, int splits) {
-    using S = Shape<NT, RB>;
-    const size_t n_grp = (size_t)S::KC * 64 / G + 1;
-    const size_t smem = S::act_bytes() + n_grp * S::rows * 4 + (ZP ? n_grp * S::rows : 0);
-    auto kernel = project_kernel<NT, RB, G, ZP>;
-    if (smem > 40 * 1024) {   // more than a kernel gets unasked: once per device
+// How a projection is cut: `splits` slices of K (a cluster of 1, 2, 4 or 8 blocks), `runs` runs of row blocks, `chunk` blocks of
+// 128 columns staged at a time.
+struct Cut { int splits, runs, chunk, smem; };
+
+inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
+    Cut best = {};
+    double cost = 1e300;
+    for (int s = 1; s <= 8; s *= 2) {
+        if (s > KB) break;
+        const int clusters = s <= 2 ? 148 / s : s == 4 ? 33 : 15;   // that are resident together (what the occupancy query answers on a B200)
+        const int waves = (RB + clusters * kMaxRun - 1) / (clusters * kMaxRun);
+        const int runs = RB < clusters * waves ? RB : clusters * waves;
+        const int run = (RB + runs - 1) / runs, slice = (KB + s - 1) / s;
+        const Smem fixed = carve(NT, G, M, 0, run);
+        int chunk = (kSmem - fixed.total) / act_bytes(NT, G);
+        if (chunk < 1) continue;
+        const int n_chunks = (slice + chunk - 1) / chunk;
+        chunk = (slice + n_chunks - 1) / n_chunks;
+        // units a warp streams, plus what staging a chunk and joining a cluster take in units of time
+        const double c = (double)waves * (run * (double)slice / kWarps + n_chunks * (4.0 + 0.02 * M * chunk) + (s > 1 ? 2.0 + 0.5 * s : 0.0));
+        if (c < cost) {
+            cost = c;
+            best = {s, runs, chunk, carve(NT, G, M, chunk, run).total};
+        }
+    }
+    return best;
+}
+
+// staged activations: bytes of scratch (0: each block of threads stages for itself)
+inline int n_tiles(int M) { return M <= 2 ? 1 : M <= 4 ? 2 : M <= 8 ? 3 : 6; }
+inline bool stage_first(int M, int KB) { return M * KB > 32; }
+inline size_t frag_bytes(int M, int KB, int group) { return !stage_first(M, KB) ? 0 : (size_t)KB * act_bytes(n_tiles(M), group); }
+
+template <int NT, int G, bool ZP, bool F32S>
+cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
+    auto kernel = project_kernel<NT, G, ZP, F32S>;
+    {   // more shared memory than a kernel gets unasked: once per device
         static std::atomic<uint64_t> done{0};
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
         if (dev > 63 || !(done.load(std::memory_order_acquire) >> dev & 1)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
             if (e != cudaSuccess) return e;
             if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
         }
     }
+    const Cut cut = pick_cut(NT, G, p.M, p.RB, p.KB);
+    if (!cut.runs) return cudaErrorInvalidConfiguration;
+    p.chunk = cut.chunk;
+    p.frag = nullptr;
+    if (stage_first(p.M, p.KB)) {
+        launch_k(stage_kernel<NT, G>, dim3((p.KB * p.M + 7) / 8), dim3(256), 0, s, pdl_enabled(), p, scratch);
+        p.frag = scratch;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((p.R16 + S::rows - 1) / S::rows, splits);
+    cfg.gridDim = dim3(cut.runs, cut.splits);
     cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = cut.smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int na = 0;
-    if (splits > 1) {
+    if (cut.splits > 1) {
         attr[na].id = cudaLaunchAttributeClusterDimension;
         attr[na].val.clusterDim.x = 1;
-        attr[na].val.clusterDim.y = splits;
+        attr[na].val.clusterDim.y = cut.splits;
         attr[na].val.clusterDim.z = 1;
         na++;
     }
@@ -563,28 +659,21 @@ cudaError_t launch_project(cudaStream_t s, const ProjArgs &p, int splits) {
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int NT, int RB>
-cudaError_t launch_group(cudaStream_t s, const ProjArgs &p, int group, int splits) {
-    const bool zp = p.zeros != nullptr;
-    switch (group) {
-        case 32: return zp ? launch_project<NT, RB, 32, true>(s, p, splits) : launch_project<NT, RB, 32, false>(s, p, splits);
-        case 64: return zp ? launch_project<NT, RB, 64, true>(s, p, splits) : launch_project<NT, RB, 64, false>(s, p, splits);
-        default: return zp ? launch_project<NT, RB, 128, true>(s, p, splits) : launch_project<NT, RB, 128, false>(s, p, splits);
-    }
+template <int NT, int G>
+cudaError_t launch_kind(cudaStream_t s, const ProjArgs &p, bool zp, bool f32s, unsigned char *scratch) {
+    if (zp) return f32s ? launch_project<NT, G, true, true>(s, p, scratch) : launch_project<NT, G, true, false>(s, p, scratch);
+    return f32s ? launch_project<NT, G, false, true>(s, p, scratch) : launch_project<NT, G, false, false>(s, p, scratch);
 }
-
-// slices of K: as many as keep about four blocks per multiprocessor, at most 8 (a cluster) and at least two tiles each
-inline int pick_splits(int row_tiles, int KT) {
-    int s = 1;
-    while (s < 8 && row_tiles * s * 2 <= 4 * 148 && KT >= 4 * s) s *= 2;
-    return s;
+template <int NT>
+cudaError_t launch_group(cudaStream_t s, const ProjArgs &p, int group, bool zp, bool f32s, unsigned char *scratch) {
+    return group == 32 ? launch_kind<NT, 32>(s, p, zp, f32s, scratch)
+           : group == 64 ? launch_kind<NT, 64>(s, p, zp, f32s, scratch)
+                         : launch_kind<NT, 128>(s, p, zp, f32s, scratch);
 }
 
 }  // namespace w4
 
 namespace {
-inline size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
 int w4_check(const eesd_w4 *m) {
     if (!m || m->R < 1 || m->K < 1 || m->R > (1 << 28) || m->K > (1 << 28)) return EESD_ERR_BADARG;
     if (m->group != 32 && m->group != 64 && m->group != 128) return EESD_ERR_UNSUPPORTED;
@@ -599,9 +688,22 @@ int w4_open(const eesd_w4 *m, const void *packed, size_t bytes, eesd_w4_layout *
     if (bytes < l->total_bytes) return EESD_ERR_NOMEM;
     return EESD_OK;
 }
-// warps' jobs of the quantisation kernels, eight to a block
-bool w4_grid(const eesd_w4_layout &l, unsigned int *blocks) {
-    const size_t jobs = (size_t)l.row_blocks * ((l.k_tiles + 1) / 2), b = (jobs + 7) / 8;
+w4::Geom w4_geom(const eesd_w4 *m, const eesd_w4_layout &l) {
+    w4::Geom q;
+    q.group = m->group;
+    q.scale_dtype = m->scale_dtype;
+    q.zp = m->zero_point;
+    q.R = m->R;
+    q.K = m->K;
+    q.KB = l.k_blocks;
+    q.block_bytes = (int)l.block_bytes;
+    q.off_zeros = (int)l.zeros;
+    return q;
+}
+// blocks of storage, one warp each, eight to a thread block
+bool w4_grid(const eesd_w4_layout &l, size_t *jobs, unsigned int *blocks) {
+    *jobs = (size_t)l.row_blocks * l.k_blocks;
+    const size_t b = (*jobs + 7) / 8;
     if (b > 0x7fffffffu) return false;
     *blocks = (unsigned int)b;
     return true;
@@ -618,13 +720,13 @@ int eesd_w4_layout_of(const eesd_w4 *m, eesd_w4_layout *out) {
     if (st) return st;
     if (!out) return EESD_ERR_BADARG;
     out->row_blocks = (m->R + 15) / 16;
-    out->k_tiles = (m->K + 63) / 64;
+    out->k_blocks = (m->K + 127) / 128;
     out->groups = (m->K + m->group - 1) / m->group;
-    const size_t r16 = (size_t)out->row_blocks * 16;
-    out->codes = 0;
-    out->scales = up((size_t)out->row_blocks * out->k_tiles * 512, 256);
-    out->zeros = up(out->scales + r16 * out->groups * (m->scale_dtype == EESD_F32 ? 4 : 2), 256);
-    out->total_bytes = up(out->zeros + (m->zero_point ? r16 * out->groups : 0), 256);
+    const size_t n = 128 / m->group * 16;
+    out->scales = 1024;
+    out->zeros = out->scales + n * (m->scale_dtype == EESD_F32 ? 4 : 2);
+    out->block_bytes = out->zeros + (m->zero_point ? n : 0);
+    out->total_bytes = (size_t)out->row_blocks * out->k_blocks * out->block_bytes;
     return EESD_OK;
 }
 
@@ -633,20 +735,18 @@ int eesd_w4_quantize(void *cuda_stream, const eesd_w4 *m, int w_dtype, const voi
     const int st = w4_open(m, packed, packed_bytes, &l);
     if (st) return st;
     if (!W || (w_dtype != EESD_F32 && w_dtype != EESD_BF16) || ldw < m->K) return EESD_ERR_BADARG;
+    size_t jobs;
     unsigned int blocks;
-    if (!w4_grid(l, &blocks)) return EESD_ERR_UNSUPPORTED;
+    if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
     const size_t es = w_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)W % es) return EESD_ERR_BADARG;
     const bool vec = ((uintptr_t)W & 15) == 0 && (size_t)ldw * es % 16 == 0;
-    char *p = (char *)packed;
-    uint8_t *z = m->zero_point ? (uint8_t *)(p + l.zeros) : nullptr;
+    unsigned char *p = (unsigned char *)packed;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     if (w_dtype == EESD_F32)
-        launch_k(w4::quantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const float *)W, (size_t)ldw, m->R, m->K, m->group, m->scale_dtype,
-                 m->zero_point != 0, (uint32_t *)p, (void *)(p + l.scales), z, l.k_tiles, l.row_blocks * 16, vec);
+        launch_k(w4::quantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const float *)W, (size_t)ldw, p, w4_geom(m, l), jobs, vec);
     else
-        launch_k(w4::quantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const __nv_bfloat16 *)W, (size_t)ldw, m->R, m->K, m->group,
-                 m->scale_dtype, m->zero_point != 0, (uint32_t *)p, (void *)(p + l.scales), z, l.k_tiles, l.row_blocks * 16, vec);
+        launch_k(w4::quantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const __nv_bfloat16 *)W, (size_t)ldw, p, w4_geom(m, l), jobs, vec);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
@@ -655,20 +755,18 @@ int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, 
     const int st = w4_open(m, packed, packed_bytes, &l);
     if (st) return st;
     if (!out || (out_dtype != EESD_F32 && out_dtype != EESD_BF16) || ldo < m->K) return EESD_ERR_BADARG;
+    size_t jobs;
     unsigned int blocks;
-    if (!w4_grid(l, &blocks)) return EESD_ERR_UNSUPPORTED;
+    if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
     const size_t es = out_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)out % es) return EESD_ERR_BADARG;
     const bool vec = ((uintptr_t)out & 15) == 0 && (size_t)ldo * es % 16 == 0;
-    const char *p = (const char *)packed;
-    const uint8_t *z = m->zero_point ? (const uint8_t *)(p + l.zeros) : nullptr;
+    const unsigned char *p = (const unsigned char *)packed;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     if (out_dtype == EESD_F32)
-        launch_k(w4::dequantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const uint32_t *)p, (const void *)(p + l.scales), z, m->R, m->K,
-                 m->group, m->scale_dtype, (float *)out, (size_t)ldo, l.k_tiles, l.row_blocks * 16, vec);
+        launch_k(w4::dequantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), p, (float *)out, (size_t)ldo, w4_geom(m, l), jobs, vec);
     else
-        launch_k(w4::dequantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const uint32_t *)p, (const void *)(p + l.scales), z, m->R,
-                 m->K, m->group, m->scale_dtype, (__nv_bfloat16 *)out, (size_t)ldo, l.k_tiles, l.row_blocks * 16, vec);
+        launch_k(w4::dequantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), p, (__nv_bfloat16 *)out, (size_t)ldo, w4_geom(m, l), jobs, vec);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
@@ -678,16 +776,20 @@ int eesd_w4_pack(void *cuda_stream, const eesd_w4 *m, const uint8_t *codes, cons
     if (st) return st;
     if (!codes || !scales || (zeros != nullptr) != (m->zero_point != 0)) return EESD_ERR_BADARG;
     if ((uintptr_t)scales % (m->scale_dtype == EESD_F32 ? 4 : 2)) return EESD_ERR_BADARG;
-    char *p = (char *)packed;
-    const size_t words = (size_t)l.row_blocks * l.k_tiles * 128, want = (words + 255) / 256;
-    const unsigned int blocks = (unsigned int)(want < 148 * 64 ? want : 148 * 64);
-    launch_k(w4::pack_kernel, dim3(blocks), dim3(256), 0, (cudaStream_t)cuda_stream, pdl_enabled(), codes, m->R, m->K, scales, zeros, m->scale_dtype, m->group,
-             (uint32_t *)p, (void *)(p + l.scales), m->zero_point ? (uint8_t *)(p + l.zeros) : (uint8_t *)nullptr, l.k_tiles, l.row_blocks * 16, l.groups);
+    size_t jobs;
+    unsigned int blocks;
+    if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
+    launch_k(w4::pack_kernel, dim3(blocks), dim3(256), 0, (cudaStream_t)cuda_stream, pdl_enabled(), codes, scales, zeros, (unsigned char *)packed, w4_geom(m, l), jobs);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
+size_t eesd_w4_project_scratch_bytes(const eesd_w4 *m, int M) {
+    if (w4_check(m) || M < 1 || M > EESD_MAX_ROWS) return 0;
+    return w4::frag_bytes(M, (m->K + 127) / 128, m->group);
+}
+
 int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,
-                         float *out, int64_t ldo, int M) {
+                         float *out, int64_t ldo, int M, void *scratch, size_t scratch_bytes) {
     eesd_w4_layout l;
     const int st = w4_open(m, packed, packed_bytes, &l);
     if (st) return st;
@@ -695,29 +797,31 @@ int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed
     if (a_dtype != EESD_F32 && a_dtype != EESD_BF16) return EESD_ERR_BADARG;
     const size_t es = a_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)A % es || ((uintptr_t)out & 3)) return EESD_ERR_BADARG;
-    const char *b = (const char *)packed;
-    w4::ProjArgs p;
-    p.codes = (const uint4 *)(b + l.codes);
-    p.scales = b + l.scales;
-    p.zeros = m->zero_point ? (const uint8_t *)(b + l.zeros) : nullptr;
+    if (const size_t need = w4::frag_bytes(M, l.k_blocks, m->group)) {
+        if (!scratch || ((uintptr_t)scratch & 15)) return EESD_ERR_BADARG;
+        if (scratch_bytes < need) return EESD_ERR_NOMEM;
+    }
+    w4::ProjArgs p = {};
+    p.packed = (const unsigned char *)packed;
     p.A = A;
     p.out = out;
     p.lda = (size_t)lda;
     p.ldo = (size_t)ldo;
     p.R = m->R;
-    p.R16 = l.row_blocks * 16;
     p.K = m->K;
-    p.KT = l.k_tiles;
+    p.KB = l.k_blocks;
+    p.RB = l.row_blocks;
     p.M = M;
     p.a_dtype = a_dtype;
-    p.scale_dtype = m->scale_dtype;
     p.vec = ((uintptr_t)A % (4 * es)) == 0 && lda % 4 == 0;
-    const int cols = a_dtype == EESD_F32 ? 2 * M : M;
+    const int nt = w4::n_tiles(M);
+    const bool zp = m->zero_point != 0, f32s = m->scale_dtype == EESD_F32;
+    unsigned char *sc = (unsigned char *)scratch;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    cudaError_t e;
-    if (cols <= 8) e = w4::launch_group<1, 1>(s, p, m->group, w4::pick_splits((p.R16 + 127) / 128, p.KT));
-    else if (cols <= 16) e = w4::launch_group<2, 1>(s, p, m->group, w4::pick_splits((p.R16 + 127) / 128, p.KT));
-    else e = w4::launch_group<4, 2>(s, p, m->group, w4::pick_splits((p.R16 + 255) / 256, p.KT));
+    const cudaError_t e = nt == 1   ? w4::launch_group<1>(s, p, m->group, zp, f32s, sc)
+                          : nt == 2 ? w4::launch_group<2>(s, p, m->group, zp, f32s, sc)
+                          : nt == 3 ? w4::launch_group<3>(s, p, m->group, zp, f32s, sc)
+                                    : w4::launch_group<6>(s, p, m->group, zp, f32s, sc);
     if (e != cudaSuccess) return EESD_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }

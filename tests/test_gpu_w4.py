@@ -2,11 +2,10 @@
 implementations.
 
 Quantisation is integer work on exactly rounded quotients, so codes, scales, zero points and values are compared for
-equality.  The projection's bound, per output, with S = sum |A| |value| over the row and SG its part in one group (g columns):
-an fp32 activation enters as two fp16 terms (2^-22 of itself, or 2^-39 of its row's largest), a bf16 one as one (exact, or
-2^-40); one m16n8k16 step adds 16 products to the running sum, each of the 17 addends cut at 2^-24 of the largest: 17 * 2^-24 SG, g / 16
-steps a group and one cut tile more; a group's sum times its scale and the addition to the total: 2 * 2^-24 of at most S for each group,
-8 slices and the scale at the end."""
+equality.  The projection's bound, per output, with S = sum |A| |value| over the row: an activation is rounded to a multiple of a
+power of two 2^-f, the smallest (f <= 126) with the largest of its row's 128 columns at most 8355711 (up to 4 rows 2139062016) of them, so
+it is off by at most half a multiple: 1 / 8355711 (1 / 2139062016) of that largest, or 2^-127; sums of products within a group are exact integers; joining up to four digits, the scale and the addition to the total round
+once each, 6 * 2^-24 of at most S for each of the row's groups; 8 slices of K, 16 warps' parts and their joins: 26 * 2^-24 S."""
 import ctypes as C
 
 import numpy as np
@@ -127,10 +126,10 @@ def check_project(m, value, A, group):
     out = eesd.project_rows(A, m)
     a = A.double()
     ref, S = a @ value.t(), a.abs() @ value.abs().t()
-    K = value.shape[1]
-    largest = a.abs().amax(1, keepdim=True) * value.abs().sum(1)[None]
-    terms = 2.0 ** -22 * S + 2.0 ** -38 * largest
-    bound = terms + ((group // 16 + 4) * 17 + 2 * (-(-K // group)) + 10) * 2.0 ** -24 * S + 1e-37
+    M, K = A.shape
+    pad = torch.nn.functional.pad(a.abs(), (0, -K % 128)).view(M, -1, 128)
+    step = (pad.amax(-1) * (1 / 2139062016 if M <= 4 else 1 / 8355711) + 2.0 ** -127).repeat_interleave(128, 1)[:, :K]
+    bound = step @ value.abs().t() + (6 * -(-K // group) + 26) * 2.0 ** -24 * S + 1e-44
     assert out.dtype == torch.float32 and out.shape == ref.shape
     assert bool(((out.double() - ref).abs() <= bound).all()), float(((out.double() - ref).abs() / bound).max())
     return out
@@ -182,7 +181,7 @@ def test_project_not_finite_rows_keep_to_themselves():
     out = eesd.project_rows(A, m)
     for i in range(7):
         if i in (1, 3, 6):
-            assert not out[i].isfinite().any()
+            assert out[i].isnan().all()
         else:
             assert torch.equal(out[i], clean[i])
 
@@ -198,7 +197,7 @@ def test_project_strided_rows_and_untouched_neighbours():
         A = wide[:4, :K]
         out = torch.full((4, R + 5), 7.0, device="cuda")
         st = eesd.lib().eesd_w4_project_rows(torch.cuda.current_stream().cuda_stream, C.addressof(m.desc), m.buffer.data_ptr(), m.buffer.numel(),
-                                             b._DTYPES[A.dtype], A.data_ptr(), A.stride(0), out.data_ptr(), R + 5, 4)
+                                             b._DTYPES[A.dtype], A.data_ptr(), A.stride(0), out.data_ptr(), R + 5, 4, None, 0)
         assert st == 0
         assert torch.equal(out[:, :R], eesd.project_rows(A, m)) and (out[:, R:] == 7.0).all()
 
@@ -239,16 +238,27 @@ def test_refusals():
     out = torch.zeros(2, 64, device="cuda")
     p, n, d = m.buffer.data_ptr(), m.buffer.numel(), C.addressof(m.desc)
     s = torch.cuda.current_stream().cuda_stream
-    good = dict(m=d, p=p, n=n, dt=0, A=A.data_ptr(), lda=128, out=out.data_ptr(), ldo=64, M=2)
+    good = dict(m=d, p=p, n=n, dt=0, A=A.data_ptr(), lda=128, out=out.data_ptr(), ldo=64, M=2, s=None, sn=0)
 
     def call(**kw):
         a = {**good, **kw}
-        return L.eesd_w4_project_rows(s, a["m"], a["p"], a["n"], a["dt"], a["A"], a["lda"], a["out"], a["ldo"], a["M"])
+        return L.eesd_w4_project_rows(s, a["m"], a["p"], a["n"], a["dt"], a["A"], a["lda"], a["out"], a["ldo"], a["M"], a["s"], a["sn"])
 
     assert call() == 0
     for kw in (dict(m=None), dict(p=None), dict(p=p + 4), dict(A=None), dict(A=A.data_ptr() + 2), dict(out=None), dict(M=0), dict(M=17), dict(lda=127), dict(ldo=63), dict(dt=2)):
         assert call(**kw) == -1, kw
     assert call(n=n - 1) == -2
+    big, *_ = random_matrix(64, 1024, 64, "f32", False, 9)   # (5 rows x 8 blocks of 128 columns: staged in scratch)
+    A5, out5, db = torch.zeros(5, 1024, device="cuda"), torch.zeros(5, 64, device="cuda"), C.addressof(big.desc)
+    need = L.eesd_w4_project_scratch_bytes(db, 5)
+    sc = torch.zeros(need + 16, dtype=torch.uint8, device="cuda")
+    assert need > 0 and L.eesd_w4_project_scratch_bytes(db, 17) == 0 and L.eesd_w4_project_scratch_bytes(d, 5) == 0
+    five = dict(m=db, p=big.buffer.data_ptr(), n=big.buffer.numel(), A=A5.data_ptr(), lda=1024, out=out5.data_ptr(), M=5)
+    assert call(**five, s=sc.data_ptr(), sn=need) == 0
+    assert call(**five) == -1 and call(**five, s=sc.data_ptr() + 8, sn=need) == -1 and call(**five, s=sc.data_ptr(), sn=need - 1) == -2
+    assert torch.equal(eesd.project_rows(A5, big, scratch=sc), out5)
+    with pytest.raises(ValueError):
+        eesd.project_rows(A5, big, scratch=sc.float())
     w = torch.zeros(64, 128, device="cuda")
     assert L.eesd_w4_quantize(s, d, 0, w.data_ptr(), 127, p, n) == -1
     assert L.eesd_w4_quantize(s, d, 5, w.data_ptr(), 128, p, n) == -1

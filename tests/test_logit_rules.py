@@ -235,16 +235,16 @@ def test_w4_layout_and_its_refusals_without_a_device():
     L, l = eesd.lib(), b.W4Layout()
     for R, K, g, sd, zp in ((1, 1, 32, 0, 0), (17, 65, 64, 1, 1), (27648, 5120, 128, 1, 0), (8192, 28672, 32, 0, 1)):
         assert L.eesd_w4_layout_of(C.byref(b.W4Desc(R, K, g, sd, zp)), C.byref(l)) == 0
-        rb, kt, G = -(-R // 16), -(-K // 64), -(-K // g)
-        assert (l.row_blocks, l.k_tiles, l.groups, l.codes) == (rb, kt, G, 0)
-        assert l.scales >= rb * kt * 512 and l.zeros >= l.scales + rb * 16 * G * (4, 2)[sd] and l.total_bytes >= l.zeros + rb * 16 * G * zp
-        assert l.scales % 256 == 0 and l.zeros % 256 == 0
+        n = 128 // g * 16
+        assert (l.row_blocks, l.k_blocks, l.groups) == (-(-R // 16), -(-K // 128), -(-K // g))
+        assert (l.scales, l.zeros, l.block_bytes) == (1024, 1024 + n * (4, 2)[sd], 1024 + n * (4, 2)[sd] + n * zp)
+        assert l.block_bytes % 16 == 0 and l.total_bytes == l.row_blocks * l.k_blocks * l.block_bytes
     for bad, st in (((0, 8, 32, 0, 0), -1), ((8, 0, 32, 0, 0), -1), ((8, 8, 16, 0, 0), -8), ((8, 8, 32, 2, 0), -1), ((8, 8, 32, 0, 2), -1), ((2 ** 29, 8, 32, 0, 0), -1)):
         assert L.eesd_w4_layout_of(C.byref(b.W4Desc(*bad)), C.byref(l)) == st
     assert L.eesd_w4_layout_of(None, C.byref(l)) == -1
     d = b.W4Desc(8, 8, 32, 0, 0)
     assert L.eesd_w4_layout_of(C.byref(d), None) == -1
     p = C.addressof(d)
-    assert L.eesd_w4_project_rows(None, p, None, 1 << 20, 0, 1 << 20, 8, 1 << 20, 8, 1) == -1
-    assert L.eesd_w4_project_rows(None, p, 1 << 20, 10, 0, 1 << 20, 8, 1 << 20, 8, 1) == -2
+    assert L.eesd_w4_project_rows(None, p, None, 1 << 20, 0, 1 << 20, 8, 1 << 20, 8, 1, None, 0) == -1
+    assert L.eesd_w4_project_rows(None, p, 1 << 20, 10, 0, 1 << 20, 8, 1 << 20, 8, 1, None, 0) == -2
     assert L.eesd_w4_quantize(None, p, 0, None, 8, 1 << 20, 1 << 20) == -1
