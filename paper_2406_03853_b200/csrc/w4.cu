@@ -37,8 +37,16 @@ __device__ __forceinline__ void store_scale(unsigned char *blk, const Geom &q, i
 }
 
 // ------------------------------------------------------------------------------------ quantisation
-// float64 -> nearest bf16 (ties to even) without double rounding: towards zero in fp32, the lost part kept in the last bit
-__device__ __forceinline__ float round_scale(double x, int scale_dtype) {
+// The quotient's nearest value of the scale's type (ties to even).  For bf16 it is rounded once: towards zero in fp32 with what is lost
+// kept in the last bit, then to nearest.
+__device__ __forceinline__ float round_scale(float x, float by, int scale_dtype) {
+    if (scale_dtype == EESD_F32) return __fdiv_rn(x, by);
+    float f = __fdiv_rz(x, by);
+    if (__fmaf_rn(-f, by, x) != 0.f) f = __uint_as_float(__float_as_uint(f) | 1u);
+    return __bfloat162float(__float2bfloat16_rn(f));
+}
+__device__ __forceinline__ float round_scale(double x, double by, int scale_dtype) {   // (x: a difference that fp32 does not hold)
+    x /= by;
     if (scale_dtype == EESD_F32) return __double2float_rn(x);
     float f = __double2float_rz(x);
     if ((double)f != x) f = __uint_as_float(__float_as_uint(f) | 1u);
@@ -56,142 +64,216 @@ __device__ __forceinline__ float nearest_quotient(float x, float s) {
     return q;
 }
 
-template <typename WT> __device__ __forceinline__ void load16(const WT *row, int k, int K, bool vec, float *v) {
-    constexpr int N = Vec16<WT>::N;
-    if (vec && k + 16 <= K) {
+// Both kernels give a warp one block, a lane the same four neighbouring columns of all its 16 rows (lane l: columns 4 l .. 4 l + 3), so
+// that a row is one contiguous access; the lane's codes of rows g and g + 8 are one word of the block: word (l / 4) % 4 of
+// fragment lane 4 g + l % 4 in tile l / 16.
+__device__ __forceinline__ int word_at(int lane, int g) { return (lane >> 4) * 512 + (g * 4 + (lane & 3)) * 16 + ((lane >> 2) & 3) * 4; }
+
+// four neighbouring weights as they come from memory
+template <typename WT> struct Four;
+template <> struct Four<float> {
+    float4 v;
+    __device__ __forceinline__ void load(const float *p) { v = __ldcs(reinterpret_cast<const float4 *>(p)); }
+    __device__ __forceinline__ void set(float4 x) { v = x; }
+    __device__ __forceinline__ float4 get() const { return v; }
+};
+template <> struct Four<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = __ldcs(reinterpret_cast<const uint2 *>(p)); }
+    __device__ __forceinline__ void set(float4 x) {   // (exact: the values are bf16)
+        v.x = __float_as_uint(x.x) >> 16 | (__float_as_uint(x.y) & 0xffff0000u);
+        v.y = __float_as_uint(x.z) >> 16 | (__float_as_uint(x.w) & 0xffff0000u);
+    }
+    __device__ __forceinline__ float4 get() const {
+        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+    }
+};
+template <typename WT> __device__ __forceinline__ float4 load4(const WT *p, int left) {   // the first `left` of four, the others 0
+    return make_float4(left > 0 ? to_f(p[0]) : 0.f, left > 1 ? to_f(p[1]) : 0.f, left > 2 ? to_f(p[2]) : 0.f, left > 3 ? to_f(p[3]) : 0.f);
+}
+__device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+
+// 16 rows' values reduced over the 8, 16 or 32 lanes of a group, the rows halved among the lanes at each exchange (15 exchanges, not
+// 80): afterwards a lane holds row rows_of(lane) (and, for 8 lanes, the next one) in m[0] (and m[1])
+template <int G, bool MIN> __device__ __forceinline__ void reduce_rows(float (&m)[16], int lane) {
 #pragma unroll
-        for (int i = 0; i < 16; i += N) Vec16<WT>::load_stream(row + k + i, v + i);
-    } else {
+    for (int b = 0; b < (G == 32 ? 3 : 4); b++) {
+        const bool up = lane >> b & 1;
 #pragma unroll
-        for (int i = 0; i < 16; i++) v[i] = k + i < K ? to_f(row[k + i]) : 0.f;
+        for (int i = 0; i < 8 >> b; i++) {
+            const float send = up ? m[i] : m[i + (8 >> b)], keep = up ? m[i + (8 >> b)] : m[i];
+            const float got = __shfl_xor_sync(0xffffffffu, send, 1 << b);
+            m[i] = MIN ? min_nan(keep, got) : max_nan(keep, got);
+        }
+    }
+    if (G == 128) {
+        const float got = __shfl_xor_sync(0xffffffffu, m[0], 16);
+        m[0] = MIN ? min_nan(m[0], got) : max_nan(m[0], got);
     }
 }
-
-// w[t] of four neighbouring lanes (steps 0..3 of a tile) <-> their 16 bytes in storage (lane t's words of steps 0..3)
-__device__ __forceinline__ uint4 transpose4(const uint32_t (&w)[4], int i) {
-    uint32_t o[4];
-#pragma unroll
-    for (int r = 0; r < 4; r++) {
-        const int t = i ^ r;
-        const uint32_t send = t == 0 ? w[0] : t == 1 ? w[1] : t == 2 ? w[2] : w[3];
-        o[r] = r ? __shfl_xor_sync(0xffffffffu, send, r) : send;   // lane i ^ r's word i
-    }
-    uint4 v;
-    v.x = i == 0 ? o[0] : i == 1 ? o[1] : i == 2 ? o[2] : o[3];   // o[r] belongs at place i ^ r
-    v.y = i == 0 ? o[1] : i == 1 ? o[0] : i == 2 ? o[3] : o[2];
-    v.z = i == 0 ? o[2] : i == 1 ? o[3] : i == 2 ? o[0] : o[1];
-    v.w = i == 0 ? o[3] : i == 1 ? o[2] : i == 2 ? o[1] : o[0];
-    return v;
+template <int G> __device__ __forceinline__ int rows_of(int lane) { return (lane & 1) * 8 + (lane & 2) * 2 + (lane & 4) / 2 + (G == 32 ? 0 : (lane >> 3 & 1)); }
+template <int G> __device__ __forceinline__ int holder_of(int lane, int r) {   // the lane of one's own group that holds row r
+    const int back = (r >> 3 & 1) + (r >> 1 & 2) + (r << 1 & 4);
+    return G == 32 ? (lane & 24) + back : (lane & 16) + back + (r & 1) * 8;
 }
 
-// One warp: one block.  A unit is rows (g, g + 8) x 16 columns (a step): its 32 codes are exactly four words.  Lane l takes step l % 8 of
-// rows l / 8 (+ 8), and of rows l / 8 + 4 (+ 8): eight neighbouring lanes read 128 contiguous columns of a row, and a group's
-// statistics are a butterfly over 2, 4 or 8 of them.
-template <typename WT>
-__global__ void __launch_bounds__(256) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
+// Reads a weight once, writes half a byte: bound by memory, if the arithmetic stays small.  The product with 1 / s, rounded to an
+// integer, is the quotient's nearest or its neighbour across a half: the exact remainder (one fused multiply-add) tells, and a row
+// where some remainder reaches half a scale is put right (common only as ties: bf16 weights over bf16 scales).  Scales below 2^-100,
+// whose reciprocal would not do, are left to nearest_quotient at the end.
+template <typename WT, int G, bool ZP>
+__global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 3 : 2) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, step = lane & 7;
+    const int lane = threadIdx.x & 31;
     const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (job >= jobs) return;
-    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + step * 16;
+    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + lane * 4;
     unsigned char *blk = packed + job * q.block_bytes;
-    const int lanes = q.group / 16;   // lanes that share a group
+    const WT *src = W + (size_t)rb * 16 * ldw + k;
+    const bool whole = vec && k + 4 <= q.K;
+    const int last = q.R - 1 - rb * 16;   // (rows that do not exist: the last one's address, zeros)
+    Four<WT> v[16];
+    if (whole) {   // (decided once, so that all 16 loads are in flight together)
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-        const int g8 = (lane >> 3) + 4 * half;
-        float v[2][16];
+        for (int r = 0; r < 16; r++) v[r].load(src + (size_t)min(r, last) * ldw);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; r++) v[r].set(load4(src + (size_t)min(r, last) * ldw, q.K - k));
+    }
+    if (last < 15)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+            if (r > last) v[r].set(make_float4(0.f, 0.f, 0.f, 0.f));
+    float hi[16], lo[16];
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const float4 x = v[r].get();
+        if (ZP) {
+            lo[r] = min_nan(min_nan(min_nan(x.x, x.y), min_nan(x.z, x.w)), 0.f);
+            hi[r] = max_nan(max_nan(max_nan(x.x, x.y), max_nan(x.z, x.w)), 0.f);
+        } else {
+            hi[r] = max_nan(max_nan(fabsf(x.x), fabsf(x.y)), max_nan(fabsf(x.z), fabsf(x.w)));
+        }
+    }
+    reduce_rows<G, false>(hi, lane);
+    if (ZP) reduce_rows<G, true>(lo, lane);
+    constexpr int N = G == 32 ? 2 : 1;   // (row, group) pairs a lane works out
+    float s[N], inv[N];
+    int z[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        s[i] = ZP ? round_scale((double)hi[i] - (double)lo[i], 15.0, q.scale_dtype) : round_scale(hi[i], 7.f, q.scale_dtype);
+        // a NaN or infinity among the weights: the whole group reads back as NaN
+        if (!(hi[i] <= 3.402823466e38f) || (ZP && !(lo[i] >= -3.402823466e38f))) s[i] = __uint_as_float(0x7fc00000u);
+        inv[i] = s[i] >= 0x1p-100f && s[i] <= 3.402823466e38f ? __frcp_rn(s[i]) : 0.f;
+        z[i] = ZP ? (s[i] > 0.f ? (int)fminf(nearest_quotient(-lo[i], s[i]), 15.f) : 0) : 8;
+        if (G != 128 || lane < 16) {
+            const int slot = scale_slot(rows_of<G>(lane) + i, lane / (G / 4), 128 / G);
+            store_scale(blk, q, slot, s[i]);
+            if (ZP) blk[q.off_zeros + slot] = (unsigned char)z[i];
+        }
+    }
+    uint32_t again = 0;   // rows left to the end
+#pragma unroll
+    for (int g = 0; g < 8; g++) {
+        uint32_t w = 0;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const int r = rb * 16 + g8 + 8 * h;
-            if (r < q.R) {
-                load16(W + (size_t)r * ldw, k, q.K, vec, v[h]);
-            } else {
+            const int r = g + 8 * h, from = holder_of<G>(lane, r), i = N == 2 ? r & 1 : 0;
+            const float sr = __shfl_sync(0xffffffffu, s[i], from), ir = __shfl_sync(0xffffffffu, inv[i], from);
+            const int zr = ZP ? __shfl_sync(0xffffffffu, z[i], from) : 8;
+            const float4 x4 = v[r].get();
+            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+            float y[4], rem[4];
 #pragma unroll
-                for (int i = 0; i < 16; i++) v[h][i] = 0.f;
+            for (int j = 0; j < 4; j++) {
+                y[j] = __fmaf_rn(x[j], ir, 12582912.f);                  // 1.5 * 2^23 + the integer
+                rem[j] = __fmaf_rn(12582912.f - y[j], sr, x[j]);
             }
+            const float most = fmaxf(fmaxf(fabsf(rem[0]), fabsf(rem[1])), fmaxf(fabsf(rem[2]), fabsf(rem[3])));
+            if (most + most >= sr && sr > 0.f) {
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float twice = fabsf(rem[j] + rem[j]);
+                    if (twice > sr || (twice == sr && (__float_as_int(y[j]) & 1))) y[j] += copysignf(1.f, rem[j]);
+                }
+            }
+            // low bytes: the integers; plus z; 16 becomes 15
+            uint32_t c = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040), __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040), 0x5410);
+            c = __vadd4(c, (uint32_t)zr * 0x01010101u);
+            if (ZP) c -= c >> 4 & 0x01010101u;
+            if (ir == 0.f && sr > 0.f) again |= 1u << r;
+            w |= (c & 0x0f0f0f0fu) << (4 * h);
         }
-        uint32_t w[4] = {0, 0, 0, 0};
+        *reinterpret_cast<uint32_t *>(blk + word_at(lane, g)) = w;
+    }
+    __syncwarp();   // scales and zero points of the warp's other lanes are in memory
+    while (again) {
+        const int r = __ffs(again) - 1, slot = scale_slot(r, lane / (G / 4), 128 / G);
+        again &= again - 1;
+        const float4 x4 = load4(src + (size_t)r * ldw, q.K - k);   // (a row that does not exist is never here: its scale is 0)
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w}, sr = load_scale(blk, q, slot);
+        const int zr = ZP ? blk[q.off_zeros + slot] : 8;
+        const float least = ZP ? -(float)zr : -8.f, most = ZP ? 15.f - (float)zr : 7.f;
+        uint32_t c = 0;
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            float lo = 0.f, hi = 0.f;
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 16; i++) { lo = fminf(lo, v[h][i]); hi = fmaxf(hi, v[h][i]); bad |= v[h][i] != v[h][i]; }
-            bad |= hi > 3.402823466e38f || lo < -3.402823466e38f;
-            for (int o = 1; o < lanes; o <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                bad |= (bool)__shfl_xor_sync(0xffffffffu, (int)bad, o);
-            }
-            float s = q.zp ? round_scale(((double)hi - (double)lo) / 15.0, q.scale_dtype) : round_scale((double)fmaxf(hi, -lo) / 7.0, q.scale_dtype);
-            if (bad) s = __uint_as_float(0x7fc00000u);   // a NaN or infinity among the weights: the whole group reads back as NaN
-            const bool some = s > 0.f;
-            const int z = q.zp ? (some ? (int)fminf(nearest_quotient(-lo, s), 15.f) : 0) : 8;
-            const float least = q.zp ? -(float)z : -8.f, most = q.zp ? 15.f - (float)z : 7.f;
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                // padding columns (and an all-zero group) hold the zero point's code: they stand for 0
-                const int c = (some && k + i < q.K ? (int)fminf(fmaxf(nearest_quotient(v[h][i], s), least), most) : 0) + z;
-                w[i >> 2] |= (uint32_t)c << (8 * (i & 3) + 4 * h);
-            }
-            if (step % lanes == 0) {
-                const int slot = scale_slot(g8 + 8 * h, step / lanes, 8 / lanes);
-                store_scale(blk, q, slot, s);
-                if (q.zp) blk[q.off_zeros + slot] = (unsigned char)z;
-            }
-        }
-        const uint4 o = transpose4(w, step & 3);
-        *reinterpret_cast<uint4 *>(blk + (step >> 2) * 512 + (g8 * 4 + (step & 3)) * 16) = o;
+        for (int j = 0; j < 4; j++) c |= (uint32_t)((int)fminf(fmaxf(nearest_quotient(x[j], sr), least), most) + zr) << (8 * j);
+        uint32_t *w = reinterpret_cast<uint32_t *>(blk + word_at(lane, r & 7));
+        const int sh = r & 8 ? 4 : 0;
+        *w = (*w & ~(0x0f0f0f0fu << sh)) | c << sh;
     }
 }
 
-template <typename OT>
+template <typename OT, int G>
 __global__ void __launch_bounds__(256) dequantize_kernel(const unsigned char *packed, OT *out, size_t ldo, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, step = lane & 7;
+    const int lane = threadIdx.x & 31;
     const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (job >= jobs) return;
-    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + step * 16;
+    const int rb = (int)(job / q.KB), k = (int)(job % q.KB) * 128 + lane * 4;
     const unsigned char *blk = packed + job * q.block_bytes;
+    if (k >= q.K) return;
+    uint32_t w[8];
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-        const int g8 = (lane >> 3) + 4 * half;
-        const uint4 raw = __ldcs(reinterpret_cast<const uint4 *>(blk + (step >> 2) * 512 + (g8 * 4 + (step & 3)) * 16));
-        const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
-        const uint4 tr = transpose4(in, step & 3);   // the transposition is its own inverse
-        const uint32_t w[4] = {tr.x, tr.y, tr.z, tr.w};
+    for (int g = 0; g < 8; g++) w[g] = __ldcs(reinterpret_cast<const uint32_t *>(blk + word_at(lane, g)));
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int r = rb * 16 + g8 + 8 * h;
-            if (r >= q.R || k >= q.K) continue;
-            const int slot = scale_slot(r, step * 16 / q.group, 128 / q.group);
-            const float s = load_scale(blk, q, slot);
-            const int z = q.zp ? blk[q.off_zeros + slot] : 8;
-            float v[16];
+    for (int r = 0; r < 16; r++) {
+        if (rb * 16 + r >= q.R) continue;
+        const int slot = scale_slot(r, lane / (G / 4), 128 / G);
+        const float s = load_scale(blk, q, slot), z = 8388608.f + (q.zp ? (float)blk[q.off_zeros + slot] : 8.f);
+        const uint32_t c = w[r & 7] >> (r & 8 ? 4 : 0) & 0x0f0f0f0fu;
+        float v[4];
 #pragma unroll
-            for (int i = 0; i < 16; i++) v[i] = __fmul_rn((float)((int)((w[i >> 2] >> (8 * (i & 3) + 4 * h)) & 15u) - z), s);
-            OT *o = out + (size_t)r * ldo + k;
-            if (vec && k + 16 <= q.K) {
-                if constexpr (sizeof(OT) == 4) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                } else {
-                    uint32_t p[8];
-#pragma unroll
-                    for (int i = 0; i < 8; i++)
-                        p[i] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[2 * i])) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[2 * i + 1])) << 16);
-                    *reinterpret_cast<uint4 *>(o) = make_uint4(p[0], p[1], p[2], p[3]);
-                    *reinterpret_cast<uint4 *>(o + 8) = make_uint4(p[4], p[5], p[6], p[7]);
-                }
+        for (int j = 0; j < 4; j++) v[j] = __fmul_rn(__uint_as_float(__byte_perm(c, 0x4b000000u, 0x7650 + j)) - z, s);   // 2^23 + c - (2^23 + z)
+        OT *o = out + (size_t)(rb * 16 + r) * ldo + k;
+        if (vec && k + 4 <= q.K) {
+            if constexpr (sizeof(OT) == 4) {
+                *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
             } else {
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (k + i < q.K) o[i] = from_f<OT>(v[i]);
+                const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+                *reinterpret_cast<uint2 *>(o) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
             }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (k + j < q.K) o[j] = from_f<OT>(v[j]);
         }
     }
+}
+
+template <typename WT>
+void launch_quantize(cudaStream_t s, unsigned int blocks, const WT *W, size_t ldw, unsigned char *packed, const Geom &q, size_t jobs, bool vec) {
+    auto k = q.zp ? (q.group == 32 ? quantize_kernel<WT, 32, true> : q.group == 64 ? quantize_kernel<WT, 64, true> : quantize_kernel<WT, 128, true>)
+                  : (q.group == 32 ? quantize_kernel<WT, 32, false> : q.group == 64 ? quantize_kernel<WT, 64, false> : quantize_kernel<WT, 128, false>);
+    launch_k(k, dim3(blocks), dim3(256), 0, s, pdl_enabled(), W, ldw, packed, q, jobs, vec);
+}
+template <typename OT>
+void launch_dequantize(cudaStream_t s, unsigned int blocks, const unsigned char *packed, OT *out, size_t ldo, const Geom &q, size_t jobs, bool vec) {
+    auto k = q.group == 32 ? dequantize_kernel<OT, 32> : q.group == 64 ? dequantize_kernel<OT, 64> : dequantize_kernel<OT, 128>;
+    launch_k(k, dim3(blocks), dim3(256), 0, s, pdl_enabled(), packed, out, ldo, q, jobs, vec);
 }
 
 // places codes given one per byte, row-major, and [R][G] scales / zero points into blocks (one warp: one block)
@@ -740,13 +822,11 @@ int eesd_w4_quantize(void *cuda_stream, const eesd_w4 *m, int w_dtype, const voi
     if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
     const size_t es = w_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)W % es) return EESD_ERR_BADARG;
-    const bool vec = ((uintptr_t)W & 15) == 0 && (size_t)ldw * es % 16 == 0;
-    unsigned char *p = (unsigned char *)packed;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (w_dtype == EESD_F32)
-        launch_k(w4::quantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const float *)W, (size_t)ldw, p, w4_geom(m, l), jobs, vec);
-    else
-        launch_k(w4::quantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), (const __nv_bfloat16 *)W, (size_t)ldw, p, w4_geom(m, l), jobs, vec);
+    const bool vec = ((uintptr_t)W % (4 * es)) == 0 && ldw % 4 == 0;
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const w4::Geom q = w4_geom(m, l);
+    if (w_dtype == EESD_F32) w4::launch_quantize(s, blocks, (const float *)W, (size_t)ldw, (unsigned char *)packed, q, jobs, vec);
+    else w4::launch_quantize(s, blocks, (const __nv_bfloat16 *)W, (size_t)ldw, (unsigned char *)packed, q, jobs, vec);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
@@ -760,13 +840,11 @@ int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, 
     if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
     const size_t es = out_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)out % es) return EESD_ERR_BADARG;
-    const bool vec = ((uintptr_t)out & 15) == 0 && (size_t)ldo * es % 16 == 0;
-    const unsigned char *p = (const unsigned char *)packed;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (out_dtype == EESD_F32)
-        launch_k(w4::dequantize_kernel<float>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), p, (float *)out, (size_t)ldo, w4_geom(m, l), jobs, vec);
-    else
-        launch_k(w4::dequantize_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, pdl_enabled(), p, (__nv_bfloat16 *)out, (size_t)ldo, w4_geom(m, l), jobs, vec);
+    const bool vec = ((uintptr_t)out % (4 * es)) == 0 && ldo % 4 == 0;
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const w4::Geom q = w4_geom(m, l);
+    if (out_dtype == EESD_F32) w4::launch_dequantize(s, blocks, (const unsigned char *)packed, (float *)out, (size_t)ldo, q, jobs, vec);
+    else w4::launch_dequantize(s, blocks, (const unsigned char *)packed, (__nv_bfloat16 *)out, (size_t)ldo, q, jobs, vec);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
