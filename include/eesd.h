@@ -446,7 +446,8 @@ int eesd_project_rows(void *cuda_stream, int dtype, const float *A, const void *
 int eesd_time_projection(eesd_ctx *ctx, int which, int M, float *ms_per_launch, size_t *bytes_per_launch);
 
 /* Draws one token per row: argmax (temperature 0) or x ~ softmax(logits / T) by inverse CDF
- * with u[b].  logits [B][V] f32, u [B] (may be NULL when greedy), out [B] i32; device pointers. */
+ * with u[b].  logits [B][V] f32, u [B] (may be NULL when greedy), out [B] i32; device pointers.
+ * -1 for a row without any logit above -inf (all masked); so does the acceptance step for its next token. */
 int eesd_sample_rows(void *cuda_stream, const float *logits, const float *u, int B, int V,
                      float temperature, int32_t *out);
 
@@ -484,10 +485,12 @@ int eesd_w4_layout_of(const eesd_w4 *m, eesd_w4_layout *out);
  * A group of zeros (or one whose scale rounds to 0) reads back as zeros, a group that holds a NaN or an infinity as NaN.
  * eesd_w4_pack: the same storage from codes [R][K] (one per byte, low 4 bits), scales [R][groups] in scale_dtype and zeros [R][groups]
  * (bytes; NULL without zero points), all contiguous: how a model that comes quantised is brought in.
+ * eesd_w4_unpack: the reverse, into those of codes / scales / zeros that are not NULL.
  * eesd_w4_dequantize: the values, out [R][K] in out_dtype with rows ldo >= K apart. */
 int eesd_w4_quantize(void *cuda_stream, const eesd_w4 *m, int w_dtype, const void *W, int64_t ldw, void *packed, size_t packed_bytes);
 int eesd_w4_pack(void *cuda_stream, const eesd_w4 *m, const uint8_t *codes, const void *scales, const uint8_t *zeros, void *packed,
                  size_t packed_bytes);
+int eesd_w4_unpack(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, uint8_t *codes, void *scales, uint8_t *zeros);
 int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int out_dtype, void *out, int64_t ldo);
 
 /* eesd_project_rows for a 4-bit matrix: out[m][r] = sum_k A[m][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A: M rows of a_dtype,
@@ -507,7 +510,7 @@ int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed
  * that follows its drafts x_1..x_i, so it counts them as generated.
  *   n    = times v was generated: in history[n_prompt .. n_history), or among drafted[0 .. i)
  *   l1   = v generated or in history[0 .. n_prompt) ? (l > 0 ? l / repetition : l * repetition) : l
- *   l2   = l1 - (frequency * n + (n > 0 ? presence : 0));   l3 = l2 + bias(v);   out = allowed ? l3 : -inf
+ *   out  = allowed ? l1 - (n > 0 ? frequency * n + presence : 0) + bias(v) : -inf        (each step rounded to fp32)
  * Everything is optional (NULL: off).  Token ids outside [0, V) are ignored everywhere.  A masked entry is -inf whatever the
  * logit was (NaN and infinities included).  A row whose mask leaves nothing is -inf throughout; eesd_sample_rows and
  * eesd_accept_resample answer -1 for a row without any logit above -inf. */

@@ -156,9 +156,10 @@ def lib():
         L.eesd_accept_resample_static.argtypes = [vp, vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, vp]
         L.eesd_sample_rows.argtypes = [vp, vp, vp, C.c_int, C.c_int, C.c_float, vp]
         i64, sz = C.c_int64, C.c_size_t
-        L.eesd_w4_layout_of.argtypes = [C.POINTER(W4Desc), C.POINTER(W4Layout)]
+        L.eesd_w4_layout_of.argtypes = [vp, vp]
         L.eesd_w4_quantize.argtypes = [vp, vp, C.c_int, vp, i64, vp, sz]
         L.eesd_w4_pack.argtypes = [vp, vp, vp, vp, vp, vp, sz]
+        L.eesd_w4_unpack.argtypes = [vp, vp, vp, sz, vp, vp, vp]
         L.eesd_w4_dequantize.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64]
         L.eesd_w4_project_scratch_bytes.restype = sz
         L.eesd_w4_project_scratch_bytes.argtypes = [vp, C.c_int]
@@ -590,36 +591,35 @@ def project_rows(A: torch.Tensor, W, scratch: Optional[torch.Tensor] = None) -> 
 
 
 # ---- 4-bit weights, logit rules
+# (these calls sit between the steps of a decode round, so the checks below are kept to a few attribute reads)
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a build without CUDA has none)
 
 
-def _raw_stream(device: torch.device) -> int:
-    """The current stream of the tensors' device."""
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _call(fn, where: str, index: int, *args):
+    """fn(stream, *args) on the current stream of device `index`, with that device current (the library launches there)."""
+    was = torch._C._cuda_getDevice()
+    if was == index:
+        st = fn(_raw_stream(index), *args)
+    else:
+        torch.cuda.set_device(index)
+        try:
+            st = fn(_raw_stream(index), *args)
+        finally:
+            torch.cuda.set_device(was)
+    if st:
+        raise EesdError(st, where)
 
 
-class _on:
-    """Makes the tensors' device the current one for a call (the library launches on the current device)."""
-
-    def __init__(self, device: torch.device):
-        self.want = device.index
-
-    def __enter__(self):
-        self.was = torch._C._cuda_getDevice()
-        if self.was != self.want:
-            torch.cuda.set_device(self.want)
-
-    def __exit__(self, *_):
-        if self.was != self.want:
-            torch.cuda.set_device(self.was)
-
-
-def _cuda_tensor(t, name: str, dtypes, device=None) -> torch.Tensor:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes:
+def _check_tensor(t, name: str, dtypes, index: Optional[int] = None) -> int:
+    """The index of the tensor's device; ValueError unless it is a CUDA tensor of one of the types (on device `index`)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name}: wanted a CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name}: on {t.device}, the other tensors are on {device}")
-    return t
+    at = t.get_device()
+    if index is not None and at != index:
+        raise ValueError(f"{name}: on device {at}, the other tensors on {index}")
+    return at
 
 
 class W4Matrix:
@@ -631,117 +631,107 @@ class W4Matrix:
         if scale_dtype not in _DTYPES:
             raise ValueError("scale_dtype: torch.float32 or torch.bfloat16")
         self.desc, self.layout = W4Desc(R, K, group, _DTYPES[scale_dtype], int(zero_point)), W4Layout()
-        st = lib().eesd_w4_layout_of(C.byref(self.desc), C.byref(self.layout))
+        self._desc_ptr = C.addressof(self.desc)
+        st = lib().eesd_w4_layout_of(self._desc_ptr, C.addressof(self.layout))
         if st:
             raise EesdError(st, "eesd_w4_layout_of")
-        _need_cuda()
-        self.shape, self.group, self.scale_dtype, self.zero_point = (R, K), group, scale_dtype, bool(zero_point)
-        self.buffer = torch.empty(self.layout.total_bytes, dtype=torch.uint8, device=device)
-        self.device = self.buffer.device
-        self._desc_ptr, self._ptr, self._bytes = C.addressof(self.desc), self.buffer.data_ptr(), self.buffer.numel()
+        self.shape, self.group, self.scale_dtype, self.zero_point, self.groups = (R, K), group, scale_dtype, bool(zero_point), self.layout.groups
+        self.buffer = torch.empty(self.layout.total_bytes, dtype=_U8, device=device)
+        self._index, self._ptr, self._bytes = _check_tensor(self.buffer, "device", (_U8,)), self.buffer.data_ptr(), self.layout.total_bytes
+
+    @property
+    def device(self) -> torch.device:
+        return self.buffer.device
 
     @classmethod
     def quantize(cls, w: torch.Tensor, group: int = 128, scale_dtype: torch.dtype = torch.bfloat16, zero_point: bool = False) -> "W4Matrix":
         """eesd_w4_quantize: w [R, K] fp32 or bf16 (rows may be strided)."""
-        _need_cuda()
-        _cuda_tensor(w, "w", _DTYPES)
-        if w.dim() != 2 or w.shape[1] < 1 or w.shape[0] < 1 or (w.stride(1) != 1 and w.shape[1] > 1):
+        index = _check_tensor(w, "w", _DTYPES)
+        if w.dim() != 2 or w.numel() == 0 or (w.stride(1) != 1 and w.shape[1] > 1):
             raise ValueError("w: wanted [R, K] with neighbouring columns next to each other")
-        m = cls(w.shape[0], w.shape[1], group, scale_dtype, zero_point, w.device)
-        ld = w.stride(0) if w.shape[0] > 1 else w.shape[1]
-        with _on(m.device):
-            st = lib().eesd_w4_quantize(_raw_stream(m.device), m._desc_ptr, _DTYPES[w.dtype], w.data_ptr(), ld, m._ptr, m._bytes)
-        if st:
-            raise EesdError(st, "eesd_w4_quantize")
+        R, K = w.shape
+        m = cls(R, K, group, scale_dtype, zero_point, w.device)
+        _call(lib().eesd_w4_quantize, "eesd_w4_quantize", index, m._desc_ptr, _DTYPES[w.dtype], w.data_ptr(), w.stride(0) if R > 1 else K, m._ptr, m._bytes)
         return m
 
     @classmethod
     def from_codes(cls, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, group: int = 128) -> "W4Matrix":
         """eesd_w4_pack: codes uint8 [R, K] (0..15), scales [R, ceil(K / group)] fp32 or bf16, zeros uint8 of the scales' shape or
         None (symmetric: zero point 8)."""
-        _need_cuda()
-        _cuda_tensor(codes, "codes", (torch.uint8,))
-        _cuda_tensor(scales, "scales", _DTYPES, codes.device)
+        index = _check_tensor(codes, "codes", (_U8,))
+        _check_tensor(scales, "scales", _DTYPES, index)
         if codes.dim() != 2 or codes.numel() == 0:
             raise ValueError("codes: wanted [R, K]")
         R, K = codes.shape
         m = cls(R, K, group, scales.dtype, zeros is not None, codes.device)
-        if tuple(scales.shape) != (R, m.layout.groups):
-            raise ValueError(f"scales: wanted [{R}, {m.layout.groups}]")
-        if zeros is not None and tuple(_cuda_tensor(zeros, "zeros", (torch.uint8,), codes.device).shape) != (R, m.layout.groups):
-            raise ValueError(f"zeros: wanted [{R}, {m.layout.groups}]")
-        with _on(m.device):
-            codes, scales = codes.contiguous(), scales.contiguous()
-            zeros = None if zeros is None else zeros.contiguous()
-            st = lib().eesd_w4_pack(_raw_stream(m.device), m._desc_ptr, codes.data_ptr(), scales.data_ptr(),
-                                    None if zeros is None else zeros.data_ptr(), m._ptr, m._bytes)
-        if st:
-            raise EesdError(st, "eesd_w4_pack")
+        if tuple(scales.shape) != (R, m.groups):
+            raise ValueError(f"scales: wanted [{R}, {m.groups}]")
+        if zeros is not None:
+            _check_tensor(zeros, "zeros", (_U8,), index)
+            if tuple(zeros.shape) != (R, m.groups):
+                raise ValueError(f"zeros: wanted [{R}, {m.groups}]")
+            zeros = zeros.contiguous()
+        codes, scales = codes.contiguous(), scales.contiguous()
+        _call(lib().eesd_w4_pack, "eesd_w4_pack", index, m._desc_ptr, codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
+              m._ptr, m._bytes)
         return m
 
-    def _per_group(self, off: int, dtype: torch.dtype) -> torch.Tensor:
-        lay, n = self.layout, 128 // self.group
-        es = torch.empty((), dtype=dtype).element_size()
-        b = self.buffer.view(lay.row_blocks, lay.k_blocks, lay.block_bytes)[:, :, off:off + n * 16 * es].view(dtype)
-        b = b.view(lay.row_blocks, lay.k_blocks, 8, 2, n).permute(0, 3, 2, 1, 4)   # [row block, row / 8, row % 8, block, group]
-        return b.reshape(lay.row_blocks * 16, lay.k_blocks * n)[:self.shape[0], :lay.groups]
-
-    def scales(self) -> torch.Tensor:
-        """The scales, [R, groups] (a copy)."""
-        return self._per_group(self.layout.scales, self.scale_dtype)
-
-    def zeros(self) -> Optional[torch.Tensor]:
-        """The zero points, uint8 [R, groups] (a copy; None: symmetric, 8)."""
-        return self._per_group(self.layout.zeros, torch.uint8) if self.zero_point else None
+    def _unpack(self, which: int, shape, dtype: torch.dtype) -> torch.Tensor:
+        out = self.buffer.new_empty(shape, dtype=dtype)
+        ptrs = [None, None, None]
+        ptrs[which] = out.data_ptr()
+        _call(lib().eesd_w4_unpack, "eesd_w4_unpack", self._index, self._desc_ptr, self._ptr, self._bytes, *ptrs)
+        return out
 
     def codes(self) -> torch.Tensor:
-        """The codes, uint8 [R, K] (a copy)."""
-        rb, kb = self.layout.row_blocks, self.layout.k_blocks
-        b = self.buffer.view(rb, kb, self.layout.block_bytes)[:, :, :1024]
-        b = b.reshape(rb, kb, 2, 8, 4, 4, 4, 1)   # [.., tile, row % 8, k % 16 / 4, k / 16, k % 4]: a byte holds rows r and r + 8
-        c = torch.cat((b & 15, b >> 4), -1)
-        # -> [row block, row / 8, row % 8, block, tile, k / 16, k % 16 / 4, k % 4]
-        return c.permute(0, 7, 3, 1, 2, 5, 4, 6).reshape(rb * 16, kb * 128)[:self.shape[0], :self.shape[1]]
+        """The codes, uint8 [R, K] (eesd_w4_unpack)."""
+        return self._unpack(0, self.shape, _U8)
+
+    def scales(self) -> torch.Tensor:
+        """The scales, [R, groups] (eesd_w4_unpack)."""
+        return self._unpack(1, (self.shape[0], self.groups), self.scale_dtype)
+
+    def zeros(self) -> Optional[torch.Tensor]:
+        """The zero points, uint8 [R, groups] (eesd_w4_unpack; None: symmetric, 8)."""
+        return self._unpack(2, (self.shape[0], self.groups), _U8) if self.zero_point else None
 
     def dense(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """eesd_w4_dequantize: the values, [R, K] fp32 or bf16."""
         if dtype not in _DTYPES:
             raise ValueError("dtype: torch.float32 or torch.bfloat16")
-        out = torch.empty(self.shape, dtype=dtype, device=self.device)
-        with _on(self.device):
-            st = lib().eesd_w4_dequantize(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, _DTYPES[dtype], out.data_ptr(), self.shape[1])
-        if st:
-            raise EesdError(st, "eesd_w4_dequantize")
+        out = self.buffer.new_empty(self.shape, dtype=dtype)
+        _call(lib().eesd_w4_dequantize, "eesd_w4_dequantize", self._index, self._desc_ptr, self._ptr, self._bytes, _DTYPES[dtype], out.data_ptr(), self.shape[1])
         return out
 
     def project_rows(self, A: torch.Tensor, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
         """eesd_w4_project_rows: A [M, K] fp32 or bf16, M <= MAX_ROWS (rows may be strided), times the matrix's transpose -> [M, R]
         fp32.  scratch: a CUDA tensor of eesd_w4_project_scratch_bytes bytes (made for the call when left out)."""
-        _cuda_tensor(A, "A", _DTYPES, self.device)
+        _check_tensor(A, "A", _DTYPES, self._index)
         R, K = self.shape
         if A.dim() != 2 or A.shape[1] != K or (A.stride(1) != 1 and K > 1):
             raise ValueError(f"A: wanted [M, {K}] with neighbouring columns next to each other")
         M = A.shape[0]
         if not 1 <= M <= MAX_ROWS:
             raise ValueError(f"A: 1 to {MAX_ROWS} rows, not {M}")
-        L, dt = lib(), _DTYPES[A.dtype]
-        need = L.eesd_w4_project_scratch_bytes(self._desc_ptr, M)
+        L, ptr, size = lib(), None, 0
         if scratch is not None:
-            _cuda_tensor(scratch, "scratch", (torch.uint8,), self.device)
-        elif need:
-            scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
-        out = torch.empty((M, R), dtype=torch.float32, device=self.device)
-        with _on(self.device):
-            st = L.eesd_w4_project_rows(_raw_stream(self.device), self._desc_ptr, self._ptr, self._bytes, dt, A.data_ptr(),
-                                        A.stride(0) if M > 1 else K, out.data_ptr(), R, M,
-                                        *((None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel())))
-        if st:
-            raise EesdError(st, "eesd_w4_project_rows")
+            _check_tensor(scratch, "scratch", (_U8,), self._index)
+            ptr, size = scratch.data_ptr(), scratch.numel()
+        else:
+            size = L.eesd_w4_project_scratch_bytes(self._desc_ptr, M)
+            if size:
+                scratch = A.new_empty(size, dtype=_U8)
+                ptr = scratch.data_ptr()
+        out = A.new_empty((M, R), dtype=_F32)
+        _call(L.eesd_w4_project_rows, "eesd_w4_project_rows", self._index, self._desc_ptr, self._ptr, self._bytes, _DTYPES[A.dtype], A.data_ptr(),
+              A.stride(0) if M > 1 else K, out.data_ptr(), R, M, ptr, size)
         return out
 
 
 def _row_stride(t: torch.Tensor, name: str) -> int:
     """Elements between the rows of [B, n] or [B, rows, n]; they have to lie evenly."""
+    if t.is_contiguous():
+        return t.shape[-1]
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: neighbours of a row have to lie next to each other")
     if t.dim() == 2:
@@ -765,89 +755,101 @@ class LogitRules:
 
     The tensors are kept and read at each process_logits call; none is copied."""
 
+    __slots__ = ("_struct", "_ptr", "_keep", "_index", "B", "rows", "mask_words")
+
     def __init__(self, *, history=None, n_history=None, n_prompt=None, drafted=None, repetition=None, frequency=None, presence=None,
                  bias_start=None, bias_ids=None, bias_values=None, mask=None):
-        i32, f32 = (torch.int32,), (torch.float32,)
-        r, self._keep, self.device, self.B, self.rows, self.mask_words = RulesStruct(), [], None, None, None, None
-
-        def take(t, name, dtypes, dim):
-            _cuda_tensor(t, name, dtypes, self.device)
-            if t.dim() not in dim:
-                raise ValueError(f"{name}: {t.dim()} dimensions")
-            self.device = t.device
-            self._keep.append(t)
-            return t
-
-        def per_sequence(t, name, n=None, extra=0):
-            n = t.shape[0] - extra if n is None else n
-            if self.B is None:
-                self.B = n
-            if n != self.B:
-                raise ValueError(f"{name}: for {n} sequences, not {self.B}")
-
+        self._keep = (history, n_history, n_prompt, drafted, repetition, frequency, presence, bias_start, bias_ids, bias_values, mask)
+        self._index = self.B = self.rows = self.mask_words = None
+        r = self._struct = RulesStruct()
+        self._ptr = C.addressof(r)
         if history is not None:
-            take(history, "history", i32, (2,))
-            per_sequence(history, "history")
-            if history.shape[1]:
-                r.history, r.history_stride, r.history_len = history.data_ptr(), _row_stride(history, "history"), history.shape[1]
+            H = self._take(history, "history", _I32, 2).shape[1]
+            if H:
+                r.history, r.history_stride, r.history_len = history.data_ptr(), _row_stride(history, "history"), H
+            if n_history is not None:
+                r.n_history = self._vector(n_history, "n_history", _I32)
+            if n_prompt is not None:
+                r.n_prompt = self._vector(n_prompt, "n_prompt", _I32)
         elif n_history is not None or n_prompt is not None:
             raise ValueError("n_history / n_prompt without history")
-        for name, t, dtypes in (("n_history", n_history, i32), ("n_prompt", n_prompt, i32), ("repetition", repetition, f32),
-                                ("frequency", frequency, f32), ("presence", presence, f32)):
-            if t is not None:
-                per_sequence(take(t, name, dtypes, (1,)), name)
-                if not t.is_contiguous():
-                    raise ValueError(f"{name}: wanted contiguous")
-                setattr(r, name, t.data_ptr())
+        if repetition is not None:
+            r.repetition = self._vector(repetition, "repetition", _F32)
+        if frequency is not None:
+            r.frequency = self._vector(frequency, "frequency", _F32)
+        if presence is not None:
+            r.presence = self._vector(presence, "presence", _F32)
         if drafted is not None:
-            take(drafted, "drafted", i32, (2,))
-            per_sequence(drafted, "drafted")
-            self.rows = drafted.shape[1] + 1
-            if drafted.shape[1]:
+            n = self._take(drafted, "drafted", _I32, 2).shape[1]
+            self.rows = n + 1
+            if n:
                 r.drafted, r.drafted_stride = drafted.data_ptr(), _row_stride(drafted, "drafted")
-        if (bias_start is None) != (bias_ids is None) or (bias_ids is None) != (bias_values is None):
-            raise ValueError("bias_start, bias_ids and bias_values go together")
-        if bias_ids is not None:
-            for name, t, dtypes in (("bias_start", bias_start, i32), ("bias_ids", bias_ids, i32), ("bias_values", bias_values, f32)):
-                if not take(t, name, dtypes, (1,)).is_contiguous():
-                    raise ValueError(f"{name}: wanted contiguous")
-                setattr(r, name, t.data_ptr())
-            per_sequence(bias_start, "bias_start", extra=1)
-            if bias_ids.shape != bias_values.shape:
-                raise ValueError("bias_ids and bias_values: one value for each id")
+        if bias_ids is not None or bias_start is not None or bias_values is not None:
+            if bias_ids is None or bias_start is None or bias_values is None:
+                raise ValueError("bias_start, bias_ids and bias_values go together")
+            r.bias_start = self._vector(bias_start, "bias_start", _I32, 1)
+            r.bias_ids = self._vector(bias_ids, "bias_ids", _I32, None)
+            r.bias_values = self._vector(bias_values, "bias_values", _F32, None)
             r.n_bias = bias_ids.shape[0]
+            if bias_values.shape[0] != r.n_bias:
+                raise ValueError("bias_ids and bias_values: one value for each id")
         if mask is not None:
-            take(mask, "mask", i32, (2, 3))
-            per_sequence(mask, "mask")
-            n = mask.shape[1] if mask.dim() == 3 else 1
+            dim = 3 if isinstance(mask, torch.Tensor) and mask.dim() == 3 else 2
+            n = self._take(mask, "mask", _I32, dim).shape[1] if dim == 3 else (self._take(mask, "mask", _I32, 2), 1)[1]
             if self.rows not in (None, n):
                 raise ValueError(f"mask: {n} rows a sequence, {self.rows} with its drafts")
             self.rows, self.mask_words = n, mask.shape[-1]
             r.mask, r.mask_stride = mask.data_ptr(), _row_stride(mask, "mask")
-        self._struct, self._ptr = r, C.addressof(r)
+
+    def _take(self, t, name: str, dtype, dim: int, extra: Optional[int] = 0):
+        """t, checked: type, device, dimensions and (unless extra is None) `extra` more entries than there are sequences."""
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or t.dim() != dim:
+            raise ValueError(f"{name}: wanted a CUDA tensor of {dtype} with {dim} dimension(s)")
+        at = t.get_device()
+        if self._index is None:
+            self._index = at
+        elif at != self._index:
+            raise ValueError(f"{name}: on device {at}, the other tensors on {self._index}")
+        if extra is not None:
+            n = t.shape[0] - extra
+            if self.B is None:
+                self.B = n
+            elif n != self.B:
+                raise ValueError(f"{name}: for {n} sequences, not {self.B}")
+        return t
+
+    def _vector(self, t, name: str, dtype, extra: Optional[int] = 0) -> int:
+        if not self._take(t, name, dtype, 1, extra).is_contiguous():
+            raise ValueError(f"{name}: wanted contiguous")
+        return t.data_ptr()
 
 
 def process_logits(logits: torch.Tensor, rules: LogitRules, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """eesd_process_logits: logits [B, rows, V] (or [B, V]: one row each) fp32, rows evenly spaced; returns the processed rows, in
     `out` when given (which may be `logits` itself)."""
-    _need_cuda()
-    _cuda_tensor(logits, "logits", (torch.float32,))
-    if logits.dim() not in (2, 3) or logits.numel() == 0:
+    index = _check_tensor(logits, "logits", (_F32,))
+    shape = logits.shape
+    if len(shape) == 3:
+        B, rows, V = shape
+    elif len(shape) == 2:
+        (B, V), rows = shape, 1
+    else:
+        B = 0
+    if not B or not rows or not V:
         raise ValueError("logits: wanted [B, rows, V] or [B, V]")
-    B, rows, V = logits.shape[0], logits.shape[1] if logits.dim() == 3 else 1, logits.shape[-1]
-    if rules.B not in (None, B) or rules.rows not in (None, rows):
+    if (rules.B is not None and rules.B != B) or (rules.rows is not None and rules.rows != rows):
         raise ValueError(f"rules for {rules.B} sequences of {rules.rows} rows, logits for {B} of {rows}")
-    if rules.device not in (None, logits.device):
-        raise ValueError(f"rules: on {rules.device}, logits on {logits.device}")
-    if rules.mask_words is not None and rules.mask_words < (V + 31) // 32:
+    if rules._index is not None and rules._index != index:
+        raise ValueError(f"rules: on device {rules._index}, logits on {index}")
+    if rules.mask_words is not None and rules.mask_words * 32 < V:
         raise ValueError(f"mask: {rules.mask_words} words for {V} entries")
+    ld = _row_stride(logits, "logits")
     if out is None:
-        out = torch.empty((B, rows, V) if logits.dim() == 3 else (B, V), dtype=torch.float32, device=logits.device)
-    elif _cuda_tensor(out, "out", (torch.float32,), logits.device).shape != logits.shape:
-        raise ValueError("out: wanted the shape of logits")
-    with _on(logits.device):
-        st = lib().eesd_process_logits(_raw_stream(logits.device), logits.data_ptr(), _row_stride(logits, "logits"), out.data_ptr(),
-                                       _row_stride(out, "out"), B, rows, V, rules._ptr)
-    if st:
-        raise EesdError(st, "eesd_process_logits")
+        out, ld_out = torch.empty_like(logits, memory_format=torch.contiguous_format), V
+    else:
+        _check_tensor(out, "out", (_F32,), index)
+        if out.shape != shape:
+            raise ValueError("out: wanted the shape of logits")
+        ld_out = _row_stride(out, "out")
+    _call(lib().eesd_process_logits, "eesd_process_logits", index, logits.data_ptr(), ld, out.data_ptr(), ld_out, B, rows, V, rules._ptr)
     return out

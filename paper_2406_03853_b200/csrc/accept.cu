@@ -55,9 +55,11 @@ __device__ __forceinline__ float z_to_float(unsigned long long Z) {
     return __fmul_rn(__ull2float_rn(Z), 1.0f / 1099511627776.0f);
 }
 
+constexpr int kNoToken = 0x7fffffff;   // (not an index: a vocabulary has at most 2^31 - 1 entries)
+
 struct __align__(16) RowStat {
     float m;                 // max logit
-    int arg;                 // lowest index attaining it
+    int arg;                 // lowest index attaining it; kNoToken: no logit is above -inf
     unsigned long long Z;    // integer normaliser
 };
 
@@ -171,7 +173,7 @@ __device__ RowStat row_stat(const float *l, int V, float T, bool need_z, AccSmem
             x[k] = i < nv ? __ldcs(reinterpret_cast<const float4 *>(l) + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         }
         float v = -INFINITY;
-        int idx = 0x7fffffff;
+        int idx = kNoToken;
 #pragma unroll
         for (int k = 0; k < kRegVec; k++) {   // ascending index within the thread: strict > keeps the lowest
             const int i4 = (threadIdx.x + k * kAccThreads) * 4;
@@ -194,7 +196,7 @@ __device__ RowStat row_stat(const float *l, int V, float T, bool need_z, AccSmem
         return st;
     }
     float v = -INFINITY;
-    int idx = 0x7fffffff;
+    int idx = kNoToken;
     for (int i = threadIdx.x; i < V; i += blockDim.x) {
         float x = l[i];
         if (x > v) { v = x; idx = i; }
@@ -348,10 +350,12 @@ __global__ void __launch_bounds__(kAccThreads) accept_kernel(const float *p_logi
     __syncthreads();
     const int j = s_j;
     int tok;
-    if (greedy) {
-        tok = ld_stat(&st[j]).arg;
+    const RowStat sp = ld_stat(&st[j]);
+    if (sp.arg == kNoToken) {   // every logit of the row is masked: there is no token
+        tok = -1;
+    } else if (greedy) {
+        tok = sp.arg;
     } else {
-        const RowStat sp = ld_stat(&st[j]);
         const float *lp = pl + (size_t)j * V;
         const float u = u_res[b];
         if (j == K) {
@@ -392,8 +396,8 @@ __global__ void __launch_bounds__(kAccThreads) sample_rows_kernel(const float *l
     pdl_trigger();   // (programmatic dependent launch: resident early, reads the logits only once their producer is done)
     pdl_wait();
     RowStat st = row_stat(l, V, greedy ? 1.0f : T, !greedy, sm);
-    int tok = st.arg;
-    if (!greedy) tok = block_draw(l, st, nullptr, st, T, V, u[b], sm);
+    int tok = st.arg == kNoToken ? -1 : st.arg;   // (every logit masked: there is no token)
+    if (!greedy && tok >= 0) tok = block_draw(l, st, nullptr, st, T, V, u[b], sm);
     if (threadIdx.x == 0) out[(size_t)b * out_stride] = tok;
 }
 

@@ -2,10 +2,10 @@
 // round (sm_100a).  For entry v of row i of sequence b, with n the times v was generated (history past the prompt, and the
 // drafts x_1..x_i that precede the row) and `seen` telling that it was generated or is in the prompt:
 //   l1 = seen ? (l > 0 ? l / repetition : l * repetition) : l
-//   l2 = l1 - (frequency * n + (n > 0 ? presence : 0))
-//   l3 = l2 + bias(v)
-//   out = allowed(v) ? l3 : -inf
-// every operation rounded to fp32 by itself.
+//   l2 = l1 - (n > 0 ? frequency * n + presence : 0)
+//   out = allowed(v) ? l2 + bias(v) : -inf
+// every operation rounded to fp32 by itself.  A division is the product with the reciprocal corrected by its remainder: the
+// rounded quotient, but for the last bit of a subnormal one.
 //
 // Memory bound: 8 bytes per entry and one mask bit.  A block owns a run of the vocabulary for one sequence, counts the
 // sequence's tokens that fall into it in shared memory (integer atomics: the result does not depend on their order),
@@ -30,156 +30,225 @@ struct Args {
     int rows, V, spans, spans_per_block, chunks, row_split, rows_per_block;
 };
 
-__device__ __forceinline__ float apply(float l, uint32_t c, float rep, float freq, float pres) {
-    if (c) l = l > 0.f ? __fdiv_rn(l, rep) : __fmul_rn(l, rep);
-    const uint32_t n = c & ~kPrompt;
-    if (n) l = __fsub_rn(l, __fadd_rn(__fmul_rn(freq, (float)n), pres));
-    return l;
+// what a block of threads works on
+struct Block {
+    uint32_t *count;         // per column: times generated, and kPrompt
+    int *bias_at;            // 1 + place of the column's bias in the list; 0: none
+    const int32_t *drafted;  // drafts from the block's first row on
+    int b, col0, rows;
+    size_t first;            // its first row
+};
+
+// Spans sub0 .. sub1 - 1 of the block's columns, all its rows, for one thread: `cols` of its four columns exist (WHOLE: all).
+// VEC: they are neighbours, one 16-byte access a row; otherwise they lie kThreads apart.
+template <bool VEC, bool WHOLE, bool PEN, bool BIAS, bool MASK> __device__ __forceinline__ void run(const Args &a, const Block &w, int sub0, int sub1, int cols) {
+    constexpr int kAhead = PEN ? 2 : 4, step = VEC ? 1 : kThreads;
+    const eesd_logit_rules &r = a.r;
+    const int mine = (VEC ? 4 : 1) * (int)threadIdx.x, rows = w.rows, at0 = sub0 * kSpan + mine;
+    const int items = (sub1 - sub0) * rows;
+    if (WHOLE) cols = 4;
+    const float rep = PEN && r.repetition ? __ldg(r.repetition + w.b) : 1.f, inv = __frcp_rn(rep);
+    const float freq = PEN && r.frequency ? __ldg(r.frequency + w.b) : 0.f, pres = PEN && r.presence ? __ldg(r.presence + w.b) : 0.f;
+    const bool near_one = rep >= 0x1p-60f && rep <= 0x1p60f;   // (else the reciprocal would not do)
+
+    // a ring of (span, row) items, loads kAhead items ahead
+    float l[kAhead][4];
+    uint32_t m[kAhead][VEC ? 1 : 4];   // the mask's words as they come (a shift here would wait for the load)
+    const float *src = a.in + w.first * a.ld_in + w.col0 + at0;
+    const uint32_t *msrc = MASK ? (const uint32_t *)r.mask + w.first * (size_t)r.mask_stride + ((w.col0 + at0) >> 5) : nullptr;
+    int fetched = 0, frow = 0;
+    auto fetch = [&](int k) {
+        if (fetched == items) return;
+        if (VEC && WHOLE) {
+            const float4 v = __ldcs(reinterpret_cast<const float4 *>(src));
+            l[k][0] = v.x; l[k][1] = v.y; l[k][2] = v.z; l[k][3] = v.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) l[k][i] = i < cols ? __ldcs(src + i * step) : 0.f;
+        }
+        if (MASK) {
+#pragma unroll
+            for (int i = 0; i < (VEC ? 1 : 4); i++)
+                if (i < cols) m[k][i] = __ldg(msrc + i * (step / 32));
+            msrc += r.mask_stride;
+        }
+        src += a.ld_in;
+        fetched++;
+        if (++frow == rows) {   // on to the next span
+            frow = 0;
+            src += kSpan - (ptrdiff_t)rows * (ptrdiff_t)a.ld_in;
+            if (MASK) msrc += kSpan / 32 - (ptrdiff_t)rows * (ptrdiff_t)r.mask_stride;
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; k++) fetch(k);
+
+    // of the current span's columns: the repetition penalty (1: not seen), its reciprocal, what the other penalties take off, the bias
+    float by[4], un[4], less[4], more[4];
+    bool special = false;   // any but 1, 1, 0, 0
+    auto state = [&](int i, int at) {
+        bool any = false;
+        if (PEN) {
+            const uint32_t c = w.count[at], n = c & ~kPrompt;
+            by[i] = c ? rep : 1.f;
+            un[i] = c ? inv : 1.f;
+            less[i] = n ? __fadd_rn(__fmul_rn(freq, (float)n), pres) : 0.f;
+            any = c != 0;
+        }
+        if (BIAS) {
+            const int j = w.bias_at[at];
+            more[i] = j ? __ldg(r.bias_values + j - 1) : 0.f;
+            any |= j != 0;
+        }
+        return any;
+    };
+    float *dst = a.out + w.first * a.ld_out + w.col0 + at0;
+    int row = 0, at = at0;
+    for (int done = 0; done < items;) {
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            if (done == items) break;
+            if ((PEN || BIAS) && row == 0) {
+                special = false;
+#pragma unroll
+                for (int i = 0; i < 4; i++) special |= state(i, at + i * step);
+            } else if (PEN && w.drafted) {   // the draft that precedes this row
+                const int off = __ldg(w.drafted + row - 1) - w.col0 - at;
+                if (VEC ? (unsigned int)off < 4u : (unsigned int)off < (unsigned int)kSpan && off % kThreads == 0) {
+                    ++w.count[at + off];   // (its column is this thread's own)
+                    special = true;
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (i * step == off) state(i, at + off);
+                }
+            }
+            if ((PEN || BIAS) && special) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    float x = l[k][i];
+                    if (PEN) {
+                        // x / by: the product with the reciprocal, corrected by its remainder
+                        float q = x * un[i];
+                        if (fabsf(q) <= 3.402823466e38f) q = fmaf(fmaf(-q, by[i], x), un[i], q);
+                        if (!near_one) q = __fdiv_rn(x, by[i]);
+                        x = __fsub_rn(x > 0.f ? q : x * by[i], less[i]);
+                    }
+                    l[k][i] = BIAS ? __fadd_rn(x, more[i]) : x;
+                }
+            }
+            if (MASK) {
+#pragma unroll
+                for (int i = 0; i < 4; i++)   // (bit col % 32 of word col / 32; kThreads is a multiple of 32)
+                    if (!(m[k][VEC ? 0 : i] >> ((mine & 31) + (VEC ? i : 0)) & 1u)) l[k][i] = -INFINITY;
+            }
+            if (VEC && WHOLE) {
+                *reinterpret_cast<float4 *>(dst) = make_float4(l[k][0], l[k][1], l[k][2], l[k][3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (i < cols) dst[i * step] = l[k][i];
+            }
+            dst += a.ld_out;
+            done++;
+            if (++row == rows) {
+                row = 0;
+                at += kSpan;
+                dst += kSpan - (ptrdiff_t)rows * (ptrdiff_t)a.ld_out;
+            }
+            fetch(k);
+        }
+    }
 }
 
-// VEC: rows are 16-byte aligned and V % 4 == 0: a thread's four columns are neighbours, one 16-byte access a row.  Otherwise they
-// lie kThreads apart, 4-byte accesses.
-template <bool VEC>
-__global__ void __launch_bounds__(kThreads) process_kernel(const Args a) {
+// VEC: rows are 16-byte aligned (the vocabulary's last 1 to 3 columns are accessed one by one)
+template <bool VEC, bool PEN, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(kThreads, 4) process_kernel(const Args a) {
     extern __shared__ uint32_t smem[];
     const eesd_logit_rules &r = a.r;
-    const int ncol = a.spans_per_block * kSpan;
-    uint32_t *count = smem;
-    int *bias_at = (int *)(smem + (r.history || r.drafted ? ncol : 0));   // 1 + place of the column's bias in the list; 0: none
-    const int tid = threadIdx.x;
+    const int ncol = a.spans_per_block * kSpan, tid = threadIdx.x;
+    Block w;
+    w.count = smem;
+    w.bias_at = (int *)(smem + (PEN ? ncol : 0));
     int job = blockIdx.x;
-    const int chunk = job % a.chunks;
+    w.col0 = job % a.chunks * ncol;
     job /= a.chunks;
-    const int rs = job % a.row_split, b = job / a.row_split;
-    const int col0 = chunk * ncol, row_lo = rs * a.rows_per_block, row_hi = min(a.rows, row_lo + a.rows_per_block);
-    const bool counting = r.history || r.drafted;
-    const int32_t *drafted = r.drafted ? r.drafted + (size_t)b * r.drafted_stride : nullptr;
+    const int row_lo = job % a.row_split * a.rows_per_block;
+    w.b = job / a.row_split;
+    w.rows = min(a.rows, row_lo + a.rows_per_block) - row_lo;
+    w.first = (size_t)w.b * a.rows + row_lo;
+    w.drafted = r.drafted ? r.drafted + (size_t)w.b * r.drafted_stride + row_lo : nullptr;
 
-    if (counting)
-        for (int i = tid; i < ncol; i += kThreads) count[i] = 0;
-    if (r.n_bias)
-        for (int i = tid; i < ncol; i += kThreads) bias_at[i] = 0;
     pdl_wait();
     pdl_trigger();
+    // On their way while the sequence's tokens are counted: the block's first rows (to the L2 cache), the lengths, the first tokens (by
+    // the length of the list, so that they need not wait for the sequence's).
+    {
+        const float *src = a.in + w.first * a.ld_in + w.col0 + tid * 4;
+        if (w.col0 + tid * 4 < a.V && (tid & 7) == 0)   // (32 columns: 128 bytes)
+            for (int i = 0; i < min(w.rows, 4); i++) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + (size_t)i * a.ld_in));
+    }
+    const int32_t *h = PEN && r.history ? r.history + (size_t)w.b * r.history_stride : nullptr;
+    const int len = h ? r.history_len : 0;
+    constexpr int kTokens = 8;
+    int tok[kTokens];
+    auto tokens = [&](int base) {
+#pragma unroll
+        for (int u = 0; u < kTokens; u++) {
+            const int i = base + u * kThreads + tid;
+            tok[u] = i < len ? __ldg(h + i) : -1;
+        }
+    };
+    tokens(0);
+    int n = len, np = 0, lo = 0, hi = 0;
+    if (h && r.n_history) n = __ldg(r.n_history + w.b);
+    if (h && r.n_prompt) np = __ldg(r.n_prompt + w.b);
+    if (BIAS) {
+        lo = __ldg(r.bias_start + w.b);
+        hi = __ldg(r.bias_start + w.b + 1);
+    }
+    for (int i = tid; i < ((PEN ? ncol : 0) + (BIAS ? ncol : 0)) / 4; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    n = min(max(n, 0), len);
+    np = min(max(np, 0), n);
+    lo = min(max(lo, 0), r.n_bias);
+    hi = min(max(hi, lo), r.n_bias);
     __syncthreads();
-    if (r.history) {
-        const int32_t *h = r.history + (size_t)b * r.history_stride;
-        const int n = r.n_history ? min(max(__ldg(r.n_history + b), 0), r.history_len) : r.history_len;
-        const int np = r.n_prompt ? min(max(__ldg(r.n_prompt + b), 0), n) : 0;
-        for (int base = 0; base < n; base += kThreads * 4) {
-            int tok[4];
+    auto column = [&](int t) -> unsigned int { return t < 0 ? 0xffffffffu : (unsigned int)t - (unsigned int)w.col0; };
+    for (int base = 0; base < n; base += kThreads * kTokens) {
+        if (base) tokens(base);
 #pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const int i = base + u * kThreads + tid;
-                tok[u] = i < n ? __ldg(h + i) : -1;
-            }
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const unsigned int at = (unsigned int)tok[u] - (unsigned int)col0;
-                if (tok[u] >= 0 && at < (unsigned int)ncol) {
-                    if (base + u * kThreads + tid < np) atomicOr(&count[at], kPrompt);
-                    else atomicAdd(&count[at], 1u);
-                }
+        for (int u = 0; u < kTokens; u++) {
+            const int i = base + u * kThreads + tid;
+            const unsigned int at = column(tok[u]);
+            if (i < n && at < (unsigned int)ncol) {
+                if (i < np) atomicOr(&w.count[at], kPrompt);
+                else atomicAdd(&w.count[at], 1u);
             }
         }
     }
-    if (drafted && tid < row_lo) {   // drafts before the block's first row
-        const int tok = __ldg(drafted + tid);
-        const unsigned int at = (unsigned int)tok - (unsigned int)col0;
-        if (tok >= 0 && at < (unsigned int)ncol) atomicAdd(&count[at], 1u);
+    if (PEN && w.drafted && tid < row_lo) {   // drafts before the block's first row
+        const unsigned int at = column(__ldg(w.drafted - row_lo + tid));
+        if (at < (unsigned int)ncol) atomicAdd(&w.count[at], 1u);
     }
-    if (r.n_bias) {
-        const int lo = min(max(__ldg(r.bias_start + b), 0), r.n_bias), hi = min(max(__ldg(r.bias_start + b + 1), lo), r.n_bias);
-        for (int i = lo + tid; i < hi; i += kThreads) {
-            const int tok = __ldg(r.bias_ids + i);
-            const unsigned int at = (unsigned int)tok - (unsigned int)col0;
-            if (tok >= 0 && at < (unsigned int)ncol) atomicMax(&bias_at[at], i + 1);   // an id given twice: its last value
-        }
+    for (int i = lo + tid; i < hi; i += kThreads) {
+        const unsigned int at = column(__ldg(r.bias_ids + i));
+        if (at < (unsigned int)ncol) atomicMax(&w.bias_at[at], i + 1);   // an id given twice: its last value
     }
     __syncthreads();
+    // from here on a count is touched by the one thread that owns its column only
+    const int subs = min(a.spans_per_block, (a.V - w.col0 + kSpan - 1) / kSpan);
+    const int left = a.V - w.col0 - (subs - 1) * kSpan - (VEC ? tid * 4 : tid);   // columns of the last span from the thread's first on
+    const int cols = VEC ? min(4, left) : min(4, (left + kThreads - 1) / kThreads);
+    const int whole = cols == 4 ? subs : subs - 1;
+    if (whole) run<VEC, true, PEN, BIAS, MASK>(a, w, 0, whole, 4);
+    if (whole < subs && cols > 0) run<VEC, false, PEN, BIAS, MASK>(a, w, whole, subs, cols);
+}
 
-    const float rep = r.repetition ? __ldg(r.repetition + b) : 1.f;
-    const float freq = r.frequency ? __ldg(r.frequency + b) : 0.f, pres = r.presence ? __ldg(r.presence + b) : 0.f;
-    const size_t first = (size_t)b * a.rows;
-    for (int sub = 0; sub < a.spans_per_block; sub++) {
-        const int c0 = col0 + sub * kSpan;
-        if (c0 >= a.V) break;
-        const int col = VEC ? c0 + tid * 4 : c0 + tid;
-        constexpr int step = VEC ? 1 : kThreads;
-        uint32_t cnt[4];
-        float bias[4];
-        bool any_bias = false;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int at = col + i * step - col0;
-            cnt[i] = counting ? count[at] : 0;
-            const int j = r.n_bias ? bias_at[at] : 0;
-            bias[i] = j ? __ldg(r.bias_values + j - 1) : 0.f;
-            any_bias |= j != 0;
-        }
-        if (col >= a.V) continue;
-        constexpr int kBatch = 4;   // rows in flight
-        for (int i0 = row_lo; i0 < row_hi; i0 += kBatch) {
-            float l[kBatch][4];
-            uint32_t m[kBatch][VEC ? 1 : 4];
-#pragma unroll
-            for (int k = 0; k < kBatch; k++) {
-                if (i0 + k >= row_hi) break;
-                const float *src = a.in + (first + i0 + k) * a.ld_in + col;
-                if (VEC) {
-                    const float4 v = __ldcs(reinterpret_cast<const float4 *>(src));
-                    l[k][0] = v.x; l[k][1] = v.y; l[k][2] = v.z; l[k][3] = v.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) l[k][i] = col + i * step < a.V ? __ldcs(src + i * step) : 0.f;
-                }
-                if (r.mask) {
-                    const uint32_t *w = (const uint32_t *)r.mask + (first + i0 + k) * (size_t)r.mask_stride;
-                    if (VEC) {
-                        m[k][0] = __ldg(w + (col >> 5)) >> (col & 31);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const int c = col + i * step;
-                            m[k][VEC ? 0 : i] = c < a.V ? __ldg(w + (c >> 5)) >> (c & 31) : 0;
-                        }
-                    }
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < kBatch; k++) {
-                const int row = i0 + k;
-                if (row >= row_hi) break;
-                if (drafted && row > row_lo) {   // the draft that precedes this row
-                    const int tok = __ldg(drafted + row - 1);
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (tok == col + i * step) cnt[i]++;
-                }
-                if (cnt[0] | cnt[1] | cnt[2] | cnt[3]) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) l[k][i] = apply(l[k][i], cnt[i], rep, freq, pres);
-                }
-                if (any_bias) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) l[k][i] = __fadd_rn(l[k][i], bias[i]);
-                }
-                if (r.mask) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (!(VEC ? m[k][0] >> i & 1u : m[k][VEC ? 0 : i] & 1u)) l[k][i] = -INFINITY;
-                }
-                float *dst = a.out + (first + row) * a.ld_out + col;
-                if (VEC) {
-                    *reinterpret_cast<float4 *>(dst) = make_float4(l[k][0], l[k][1], l[k][2], l[k][3]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (col + i * step < a.V) dst[i * step] = l[k][i];
-                }
-            }
-        }
-    }
+// one kernel for each set of rules: what a call does not use costs it no registers
+template <bool VEC> void (*pick(bool pen, bool bias, bool mask))(Args) {
+    if (pen) return bias ? (mask ? process_kernel<VEC, true, true, true> : process_kernel<VEC, true, true, false>)
+                         : (mask ? process_kernel<VEC, true, false, true> : process_kernel<VEC, true, false, false>);
+    return bias ? (mask ? process_kernel<VEC, false, true, true> : process_kernel<VEC, false, true, false>)
+                : (mask ? process_kernel<VEC, false, false, true> : process_kernel<VEC, false, false, false>);
 }
 
 }  // namespace rules
@@ -217,11 +286,11 @@ extern "C" int eesd_process_logits(void *cuda_stream, const float *logits, int64
     a.spans = (V + rules::kSpan - 1) / rules::kSpan;
     a.spans_per_block = 1;
     a.row_split = 1;
-    // Enough blocks to fill the machine several times: few sequences split their rows, many take several spans a block so
-    // that a sequence's tokens are counted over by fewer blocks.
-    const long long fill = 148 * 8;
-    while (a.row_split * 2 <= rows && (long long)B * a.spans * a.row_split < fill) a.row_split *= 2;
-    if (a.r.history) while (a.spans_per_block < 4 && (long long)B * a.spans / (a.spans_per_block * 2) >= 2 * fill) a.spans_per_block *= 2;
+    // Few sequences split their rows among blocks until the machine is full; many take several spans a block, so that a sequence's
+    // tokens are counted by fewer blocks.
+    while (a.row_split * 2 <= rows && (long long)B * a.spans * a.row_split < 4 * 148) a.row_split *= 2;
+    if (a.row_split == 1)
+        while (a.spans_per_block < 4 && (long long)B * a.spans / (a.spans_per_block * 2) >= 400) a.spans_per_block *= 2;
     a.rows_per_block = (rows + a.row_split - 1) / a.row_split;
     a.row_split = (rows + a.rows_per_block - 1) / a.rows_per_block;
     a.chunks = (a.spans + a.spans_per_block - 1) / a.spans_per_block;
@@ -229,8 +298,9 @@ extern "C" int eesd_process_logits(void *cuda_stream, const float *logits, int64
     if (blocks > 0x7fffffffLL) return EESD_ERR_UNSUPPORTED;
     const size_t ncol = (size_t)a.spans_per_block * rules::kSpan;
     const size_t smem = ncol * 4 * ((a.r.history || a.r.drafted ? 1 : 0) + (a.r.n_bias ? 1 : 0));
-    const bool vec = V % 4 == 0 && ld_logits % 4 == 0 && ld_out % 4 == 0 && (((uintptr_t)logits | (uintptr_t)out) & 15) == 0;
-    launch_k(vec ? rules::process_kernel<true> : rules::process_kernel<false>, dim3((unsigned int)blocks), dim3(rules::kThreads), smem, (cudaStream_t)cuda_stream,
-             pdl_enabled(), a);
+    const bool vec = ld_logits % 4 == 0 && ld_out % 4 == 0 && (((uintptr_t)logits | (uintptr_t)out) & 15) == 0;
+    const bool pen = a.r.history || a.r.drafted, bias = a.r.n_bias != 0, mask = a.r.mask != nullptr;
+    auto kernel = vec ? rules::pick<true>(pen, bias, mask) : rules::pick<false>(pen, bias, mask);
+    launch_k(kernel, dim3((unsigned int)blocks), dim3(rules::kThreads), smem, (cudaStream_t)cuda_stream, pdl_enabled(), a);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }

@@ -310,6 +310,44 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint8_t *src, const voi
     }
 }
 
+// the reverse; what is null is left out
+__global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed, uint8_t *dst, void *sc, uint8_t *zs, const Geom q, size_t jobs) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const size_t job = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (job >= jobs) return;
+    const int rb = (int)(job / q.KB), k0 = (int)(job % q.KB) * 128, G = (q.K + q.group - 1) / q.group;
+    const unsigned char *blk = packed + job * q.block_bytes;
+    if (dst) {
+        const int k = k0 + lane * 4;
+#pragma unroll
+        for (int g = 0; g < 8; g++) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(blk + word_at(lane, g));
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int r = rb * 16 + g + 8 * h;
+                const uint32_t c = w >> (4 * h) & 0x0f0f0f0fu;
+                uint8_t *o = dst + (size_t)r * q.K + k;
+                if (r < q.R && k + 4 <= q.K && ((uintptr_t)o & 3) == 0) *reinterpret_cast<uint32_t *>(o) = c;
+                else if (r < q.R)
+                    for (int j = 0; j < 4 && k + j < q.K; j++) o[j] = (uint8_t)(c >> (8 * j));
+            }
+        }
+    }
+    const int n = 128 / q.group;
+    for (int i = lane; i < n * 16; i += 32) {
+        const int r = rb * 16 + i / n, g = k0 / q.group + i % n, slot = scale_slot(i / n, i % n, n);
+        if (r >= q.R || g >= G) continue;
+        const size_t at = (size_t)r * G + g;
+        if (sc) {
+            if (q.scale_dtype == EESD_F32) ((float *)sc)[at] = reinterpret_cast<const float *>(blk + 1024)[slot];
+            else ((__nv_bfloat16 *)sc)[at] = reinterpret_cast<const __nv_bfloat16 *>(blk + 1024)[slot];
+        }
+        if (zs) zs[at] = blk[q.off_zeros + slot];
+    }
+}
+
 // ------------------------------------------------------------------------------------ projection
 // A block of threads (one per multiprocessor, kWarps warps) owns a run of row blocks and a slice of K; the slices of a
 // run are one cluster.  Its (row block, 128 columns) units, in storage order, are cut evenly among its warps, so the load is even
@@ -858,6 +896,19 @@ int eesd_w4_pack(void *cuda_stream, const eesd_w4 *m, const uint8_t *codes, cons
     unsigned int blocks;
     if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
     launch_k(w4::pack_kernel, dim3(blocks), dim3(256), 0, (cudaStream_t)cuda_stream, pdl_enabled(), codes, scales, zeros, (unsigned char *)packed, w4_geom(m, l), jobs);
+    return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
+}
+
+int eesd_w4_unpack(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, uint8_t *codes, void *scales, uint8_t *zeros) {
+    eesd_w4_layout l;
+    const int st = w4_open(m, packed, packed_bytes, &l);
+    if (st) return st;
+    if ((!codes && !scales && !zeros) || (zeros && !m->zero_point)) return EESD_ERR_BADARG;
+    if ((uintptr_t)scales % (m->scale_dtype == EESD_F32 ? 4 : 2)) return EESD_ERR_BADARG;
+    size_t jobs;
+    unsigned int blocks;
+    if (!w4_grid(l, &jobs, &blocks)) return EESD_ERR_UNSUPPORTED;
+    launch_k(w4::unpack_kernel, dim3(blocks), dim3(256), 0, (cudaStream_t)cuda_stream, pdl_enabled(), (const unsigned char *)packed, codes, scales, zeros, w4_geom(m, l), jobs);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
