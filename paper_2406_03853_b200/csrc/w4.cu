@@ -94,34 +94,76 @@ template <typename WT> __device__ __forceinline__ float4 load4(const WT *p, int 
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// 16 rows' values reduced over the 8, 16 or 32 lanes of a group, the rows halved among the lanes at each exchange (15 exchanges, not
-// 80): afterwards a lane holds row rows_of(lane) (and, for 8 lanes, the next one) in m[0] (and m[1])
-template <int G, bool MIN> __device__ __forceinline__ void reduce_rows(float (&m)[16], int lane) {
+// The extreme of each of 16 rows over a group's 8, 16 or 32 lanes, the rows halved among the lanes at each exchange: afterwards a lane
+// holds row first_row(lane) and, for 8 lanes, the eighth after it (lane bit 3 tells the two apart otherwise). 
+// fp32: 15 exchanges, not 80; bf16: rows g and g + 8 share a register, 8 exchanges for 16 lanes.
+__device__ __forceinline__ int first_row(int lane) { return (lane & 1) * 4 + (lane & 2) + (lane >> 2 & 1); }
+enum Extreme { kMost, kLeast, kMagnitude };
+template <Extreme E> __device__ __forceinline__ uint32_t extreme2(uint32_t a, uint32_t b) {   // of bf16 pairs; NaN wins; the sign of a magnitude means nothing
+    uint32_t r;
+    if (E == kMost) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else if (E == kLeast) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <Extreme E> __device__ __forceinline__ float extreme(float a, float b) {
+    return E == kMost ? max_nan(a, b) : E == kLeast ? min_nan(a, b) : max_nan(fabsf(a), fabsf(b));
+}
+template <int G, Extreme E> __device__ __forceinline__ void row_extremes(const Four<__nv_bfloat16> (&v)[16], int lane, float (&out)[2]) {
+    uint32_t m[8];
 #pragma unroll
-    for (int b = 0; b < (G == 32 ? 3 : 4); b++) {
+    for (int g = 0; g < 8; g++) {
+        const uint32_t a = extreme2<E>(v[g].v.x, v[g].v.y), b = extreme2<E>(v[g + 8].v.x, v[g + 8].v.y);
+        m[g] = extreme2<E>(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+    }
+#pragma unroll
+    for (int b = 0; b < 3; b++) {
         const bool up = lane >> b & 1;
 #pragma unroll
-        for (int i = 0; i < 8 >> b; i++) {
-            const float send = up ? m[i] : m[i + (8 >> b)], keep = up ? m[i + (8 >> b)] : m[i];
-            const float got = __shfl_xor_sync(0xffffffffu, send, 1 << b);
-            m[i] = MIN ? min_nan(keep, got) : max_nan(keep, got);
+        for (int i = 0; i < 4 >> b; i++) {
+            const uint32_t send = up ? m[i] : m[i + (4 >> b)], keep = up ? m[i + (4 >> b)] : m[i];
+            m[i] = extreme2<E>(keep, __shfl_xor_sync(0xffffffffu, send, 1 << b));
         }
     }
-    if (G == 128) {
-        const float got = __shfl_xor_sync(0xffffffffu, m[0], 16);
-        m[0] = MIN ? min_nan(m[0], got) : max_nan(m[0], got);
-    }
+    if (G >= 64) m[0] = extreme2<E>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 8));
+    if (G == 128) m[0] = extreme2<E>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 16));
+    out[0] = __uint_as_float(m[0] << 16);
+    out[1] = __uint_as_float(m[0] & 0xffff0000u);
+    if (G >= 64 && (lane & 8)) out[0] = out[1];
+    if (E == kMagnitude) out[0] = fabsf(out[0]), out[1] = fabsf(out[1]);
 }
-template <int G> __device__ __forceinline__ int rows_of(int lane) { return (lane & 1) * 8 + (lane & 2) * 2 + (lane & 4) / 2 + (G == 32 ? 0 : (lane >> 3 & 1)); }
-template <int G> __device__ __forceinline__ int holder_of(int lane, int r) {   // the lane of one's own group that holds row r
-    const int back = (r >> 3 & 1) + (r >> 1 & 2) + (r << 1 & 4);
-    return G == 32 ? (lane & 24) + back : (lane & 16) + back + (r & 1) * 8;
+template <int G, Extreme E> __device__ __forceinline__ void row_extremes(const Four<float> (&v)[16], int lane, float (&out)[2]) {
+    float m[16];
+#pragma unroll
+    for (int r = 0; r < 16; r++) m[r] = extreme<E>(extreme<E>(v[r].v.x, v[r].v.y), extreme<E>(v[r].v.z, v[r].v.w));
+#pragma unroll
+    for (int b = 0; b < 3; b++) {
+        const bool up = lane >> b & 1;
+#pragma unroll
+        for (int h = 0; h < 16; h += 8)
+#pragma unroll
+            for (int i = 0; i < 4 >> b; i++) {
+                const float send = up ? m[h + i] : m[h + i + (4 >> b)], keep = up ? m[h + i + (4 >> b)] : m[h + i];
+                m[h + i] = extreme<E>(keep, __shfl_xor_sync(0xffffffffu, send, 1 << b));
+            }
+    }
+    out[0] = m[0];
+    out[1] = m[8];
+    if (G >= 64) {
+        const bool up = lane & 8;
+        const float send = up ? out[0] : out[1], keep = up ? out[1] : out[0];
+        out[0] = extreme<E>(keep, __shfl_xor_sync(0xffffffffu, send, 8));
+    }
+    if (G == 128) out[0] = extreme<E>(out[0], __shfl_xor_sync(0xffffffffu, out[0], 16));
 }
 
-// Reads a weight once, writes half a byte: bound by memory, if the arithmetic stays small.  The product with 1 / s, rounded to an
-// integer, is the quotient's nearest or its neighbour across a half: the exact remainder (one fused multiply-add) tells, and a row
-// where some remainder reaches half a scale is put right (common only as ties: bf16 weights over bf16 scales).  Scales below 2^-100,
-// whose reciprocal would not do, are left to nearest_quotient at the end.
+// Reads a weight once, writes half a byte.  The product with 1 / s, rounded to an integer, is the quotient's nearest or its neighbour
+// across a half: the exact remainder (one fused multiply-add) tells, and a row where some remainder reaches half a scale is put
+// right (common only as ties: bf16 weights over bf16 scales, 3.5 us of the 40).  Scales below 2^-100, whose reciprocal would not
+// do, are left to nearest_quotient at the end.
+// Measured, 5120 x 13824: fp32 weights 47 to 58 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 37 to 51 us
+// (floor 27: bound by issue, 14 instructions for a lane's weight, 2.8 of 4 a cycle).  Columns 16 to a lane (one lane a scale, no exchange) reads in
+// pieces of 32 bytes and took 167 to 184 us.
 template <typename WT, int G, bool ZP>
 __global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 3 : 2) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
@@ -135,91 +177,90 @@ __global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 3 : 2) quantize_kernel(
     const bool whole = vec && k + 4 <= q.K;
     const int last = q.R - 1 - rb * 16;   // (rows that do not exist: the last one's address, zeros)
     Four<WT> v[16];
-    if (whole) {   // (decided once, so that all 16 loads are in flight together)
+    if (whole && last >= 15) {   // (decided once, so that all 16 loads are in flight together)
+        const WT *at = src;
 #pragma unroll
-        for (int r = 0; r < 16; r++) v[r].load(src + (size_t)min(r, last) * ldw);
+        for (int r = 0; r < 16; r++, at += ldw) v[r].load(at);
     } else {
 #pragma unroll
-        for (int r = 0; r < 16; r++) v[r].set(load4(src + (size_t)min(r, last) * ldw, q.K - k));
+        for (int r = 0; r < 16; r++) v[r].set(load4(src + (size_t)min(r, last) * ldw, r <= last ? q.K - k : 0));
     }
-    if (last < 15)
-#pragma unroll
-        for (int r = 0; r < 16; r++)
-            if (r > last) v[r].set(make_float4(0.f, 0.f, 0.f, 0.f));
-    float hi[16], lo[16];
-#pragma unroll
-    for (int r = 0; r < 16; r++) {
-        const float4 x = v[r].get();
-        if (ZP) {
-            lo[r] = min_nan(min_nan(min_nan(x.x, x.y), min_nan(x.z, x.w)), 0.f);
-            hi[r] = max_nan(max_nan(max_nan(x.x, x.y), max_nan(x.z, x.w)), 0.f);
-        } else {
-            hi[r] = max_nan(max_nan(fabsf(x.x), fabsf(x.y)), max_nan(fabsf(x.z), fabsf(x.w)));
-        }
+    // what a row's codes take: {s, 1 / s, 1.5 * 2^23 + z, -}, worked out by one lane a row and group
+    constexpr int NG = 128 / G, N = G == 32 ? 2 : 1;
+    __shared__ float4 table[8][NG][17];
+    float4 (*rows)[17] = table[threadIdx.x >> 5];
+    float hi[2], lo[2] = {0.f, 0.f};
+    if (ZP) {
+        row_extremes<G, kMost>(v, lane, hi);
+        row_extremes<G, kLeast>(v, lane, lo);
+    } else {
+        row_extremes<G, kMagnitude>(v, lane, hi);
     }
-    reduce_rows<G, false>(hi, lane);
-    if (ZP) reduce_rows<G, true>(lo, lane);
-    constexpr int N = G == 32 ? 2 : 1;   // (row, group) pairs a lane works out
-    float s[N], inv[N];
-    int z[N];
+    bool left = false;   // rows left to the end
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        s[i] = ZP ? round_scale((double)hi[i] - (double)lo[i], 15.0, q.scale_dtype) : round_scale(hi[i], 7.f, q.scale_dtype);
+        if (ZP) {
+            hi[i] = max_nan(hi[i], 0.f);
+            lo[i] = min_nan(lo[i], 0.f);
+        }
+        float s = ZP ? round_scale((double)hi[i] - (double)lo[i], 15.0, q.scale_dtype) : round_scale(hi[i], 7.f, q.scale_dtype);
         // a NaN or infinity among the weights: the whole group reads back as NaN
-        if (!(hi[i] <= 3.402823466e38f) || (ZP && !(lo[i] >= -3.402823466e38f))) s[i] = __uint_as_float(0x7fc00000u);
-        inv[i] = s[i] >= 0x1p-100f && s[i] <= 3.402823466e38f ? __frcp_rn(s[i]) : 0.f;
-        z[i] = ZP ? (s[i] > 0.f ? (int)fminf(nearest_quotient(-lo[i], s[i]), 15.f) : 0) : 8;
+        if (!(hi[i] <= 3.402823466e38f) || (ZP && !(lo[i] >= -3.402823466e38f))) s = __uint_as_float(0x7fc00000u);
+        const bool fine = s >= 0x1p-100f;
+        const int z = ZP ? (s > 0.f ? (int)fminf(nearest_quotient(-lo[i], s), 15.f) : 0) : 8, r = first_row(lane) + (N == 2 ? 8 * i : lane & 8), g = lane / (G / 4);
+        left = left || (s > 0.f && !fine);
         if (G != 128 || lane < 16) {
-            const int slot = scale_slot(rows_of<G>(lane) + i, lane / (G / 4), 128 / G);
-            store_scale(blk, q, slot, s[i]);
-            if (ZP) blk[q.off_zeros + slot] = (unsigned char)z[i];
+            rows[g][r] = make_float4(s == 0.f ? 1.f : s, fine ? __frcp_rn(s) : 0.f, 12582912.f + (float)z, 0.f);
+            const int slot = scale_slot(r, g, NG);
+            store_scale(blk, q, slot, s);
+            if (ZP) blk[q.off_zeros + slot] = (unsigned char)z;
         }
     }
-    uint32_t again = 0;   // rows left to the end
+    __syncwarp();
+    const float4 *mine = rows[lane / (G / 4)];
 #pragma unroll
     for (int g = 0; g < 8; g++) {
-        uint32_t w = 0;
+        uint32_t c[2];
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const int r = g + 8 * h, from = holder_of<G>(lane, r), i = N == 2 ? r & 1 : 0;
-            const float sr = __shfl_sync(0xffffffffu, s[i], from), ir = __shfl_sync(0xffffffffu, inv[i], from);
-            const int zr = ZP ? __shfl_sync(0xffffffffu, z[i], from) : 8;
-            const float4 x4 = v[r].get();
+            float sr, ir, zf = 12582920.f;
+            if (ZP) {
+                const float4 e = mine[g + 8 * h];
+                sr = e.x, ir = e.y, zf = e.z;
+            } else {
+                const float2 e = *reinterpret_cast<const float2 *>(&mine[g + 8 * h]);
+                sr = e.x, ir = e.y;
+            }
+            const float4 x4 = v[g + 8 * h].get();
             const float x[4] = {x4.x, x4.y, x4.z, x4.w};
             float y[4], rem[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                y[j] = __fmaf_rn(x[j], ir, 12582912.f);                  // 1.5 * 2^23 + the integer
-                rem[j] = __fmaf_rn(12582912.f - y[j], sr, x[j]);
+                y[j] = __fmaf_rn(x[j], ir, zf);   // 1.5 * 2^23 + the code
+                rem[j] = __fmaf_rn(zf - y[j], sr, x[j]);
             }
             const float most = fmaxf(fmaxf(fabsf(rem[0]), fabsf(rem[1])), fmaxf(fabsf(rem[2]), fabsf(rem[3])));
-            if (most + most >= sr && sr > 0.f) {
+            if (most + most >= sr) {
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     const float twice = fabsf(rem[j] + rem[j]);
-                    if (twice > sr || (twice == sr && (__float_as_int(y[j]) & 1))) y[j] += copysignf(1.f, rem[j]);
+                    if (twice > sr || (twice == sr && ((__float_as_int(y[j]) ^ __float_as_int(zf)) & 1))) y[j] += copysignf(1.f, rem[j]);
                 }
             }
-            // low bytes: the integers; plus z; 16 becomes 15
-            uint32_t c = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040), __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040), 0x5410);
-            c = __vadd4(c, (uint32_t)zr * 0x01010101u);
-            if (ZP) c -= c >> 4 & 0x01010101u;
-            if (ir == 0.f && sr > 0.f) again |= 1u << r;
-            w |= (c & 0x0f0f0f0fu) << (4 * h);
+            c[h] = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040), __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040), 0x5410);
+            if (ZP) c[h] -= c[h] >> 4 & 0x01010101u;   // 16 becomes 15
         }
-        *reinterpret_cast<uint32_t *>(blk + word_at(lane, g)) = w;
+        *reinterpret_cast<uint32_t *>(blk + word_at(lane, g)) = (c[0] & 0x0f0f0f0fu) | (c[1] << 4 & 0xf0f0f0f0u);
     }
-    __syncwarp();   // scales and zero points of the warp's other lanes are in memory
-    while (again) {
-        const int r = __ffs(again) - 1, slot = scale_slot(r, lane / (G / 4), 128 / G);
-        again &= again - 1;
+    if (!__any_sync(0xffffffffu, left)) return;
+    for (int r = 0; r < 16; r++) {
+        const float sr = mine[r].x;
+        if (!(sr < 0x1p-100f)) continue;
         const float4 x4 = load4(src + (size_t)r * ldw, q.K - k);   // (a row that does not exist is never here: its scale is 0)
-        const float x[4] = {x4.x, x4.y, x4.z, x4.w}, sr = load_scale(blk, q, slot);
-        const int zr = ZP ? blk[q.off_zeros + slot] : 8;
-        const float least = ZP ? -(float)zr : -8.f, most = ZP ? 15.f - (float)zr : 7.f;
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w}, zr = mine[r].z - 12582912.f;
         uint32_t c = 0;
 #pragma unroll
-        for (int j = 0; j < 4; j++) c |= (uint32_t)((int)fminf(fmaxf(nearest_quotient(x[j], sr), least), most) + zr) << (8 * j);
+        for (int j = 0; j < 4; j++) c |= (uint32_t)(int)(fminf(fmaxf(nearest_quotient(x[j], sr), ZP ? -zr : -8.f), ZP ? 15.f - zr : 7.f) + zr) << (8 * j);
         uint32_t *w = reinterpret_cast<uint32_t *>(blk + word_at(lane, r & 7));
         const int sh = r & 8 ? 4 : 0;
         *w = (*w & ~(0x0f0f0f0fu << sh)) | c << sh;
