@@ -716,6 +716,8 @@ class W4Matrix:
         L, ptr, size = lib(), None, 0
         if scratch is not None:
             _check_tensor(scratch, "scratch", (_U8,), self._index)
+            if not scratch.is_contiguous():
+                raise ValueError("scratch: wanted contiguous")
             ptr, size = scratch.data_ptr(), scratch.numel()
         else:
             size = L.eesd_w4_project_scratch_bytes(self._desc_ptr, M)

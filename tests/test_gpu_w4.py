@@ -284,3 +284,57 @@ def test_refusals():
     with pytest.raises(ValueError):
         eesd.W4Matrix.from_codes(torch.zeros(64, 128, device="cuda", dtype=torch.uint8), torch.zeros(64, 2, device="cuda"),
                                  torch.zeros(64, 1, device="cuda", dtype=torch.uint8), group=64)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("scale", ["f32", "bf16"])
+@pytest.mark.parametrize("zp", [False, True])
+def test_quantize_bf16_borders(group, scale, zp):
+    """bf16 weights take their extremes in pairs: every row and column decides once, and ties, subnormals and the largest values"""
+    g = torch.Generator().manual_seed(7)
+    w = torch.randn(64, 256, generator=g) * 0.02
+    for i in range(256):                                  # each column is the largest of some row's group, with either sign
+        w[i % 64, i] = (1 if i % 3 else -1) * (1 + i / 256)
+    w[0] = (torch.arange(256) % 29 / 2 - 7).clamp(-7, 7)  # ties
+    w[1] = 0.0
+    w[2] = 1e-40
+    w[3, 7], w[3, 9] = 3e38, -3e38 if not zp else -1.0
+    w[4] = -w[4].abs()
+    w[5] = w[5].abs()
+    w[6] = torch.randn(256, generator=g) * 1e-38
+    w[7] = -0.0
+    check_quantize(w.to(torch.bfloat16).cuda(), group, scale, zp)
+    check_quantize(w.to(torch.bfloat16).cuda()[:61, :200], group, scale, zp)
+
+
+def test_two_projections_at_once_and_one_scratch_for_two_graphs():
+    m, value, *_ = random_matrix(4096, 4096, 128, "bf16", True, 21)
+    rows = [torch.randn(9, 4096, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda") for i in range(2)]
+    alone = [eesd.project_rows(a, m) for a in rows]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in rows]
+    for _ in range(20):
+        outs = []
+        for a, s in zip(rows, streams):
+            with torch.cuda.stream(s):
+                outs.append(eesd.project_rows(a, m))
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, x) for o, x in zip(outs, alone))
+    # the scratch's contents are irrelevant: graphs replayed one after the other can share it
+    sc = torch.empty(b.lib().eesd_w4_project_scratch_bytes(m._desc_ptr, 9), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for a in rows:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(eesd.project_rows(a, m, scratch=sc))
+        graphs.append(graph)
+    for i in (0, 1, 1, 0, 1):
+        outs[i].zero_()
+        graphs[i].replay()
+        assert torch.equal(outs[i], alone[i])
+    with pytest.raises(ValueError):   # one byte seen many times
+        eesd.project_rows(rows[0], m, scratch=sc[:1].expand(sc.numel()))
+    with pytest.raises(eesd.EesdError):   # rows that lie on one another
+        eesd.project_rows(rows[0][:1].expand(3, 4096), m)
+    with pytest.raises(eesd.EesdError):
+        eesd.W4Matrix.quantize(rows[0][:1].expand(3, 4096))
