@@ -7,6 +7,7 @@ creating an Engine or calling a kernel entry point without CUDA raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence
@@ -622,6 +623,17 @@ def _check_tensor(t, name: str, dtypes, index: Optional[int] = None) -> int:
     return at
 
 
+@functools.lru_cache(maxsize=1024)
+def _w4_describe(R: int, K: int, group: int, scale_dtype: int, zero_point: int):
+    """eesd_w4_layout_of: (description, layout, the description's address) of such a matrix; nobody writes to them"""
+    desc, layout = W4Desc(R, K, group, scale_dtype, zero_point), W4Layout()
+    at = C.addressof(desc)
+    st = lib().eesd_w4_layout_of(at, C.addressof(layout))
+    if st:
+        raise EesdError(st, "eesd_w4_layout_of")
+    return desc, layout, at
+
+
 class W4Matrix:
     """A weight matrix [R, K] in 4 bits per weight with a scale (and optionally a zero point) per group of `group`
     neighbours along K (eesd_w4): `W4Matrix.quantize(w)` or `W4Matrix.from_codes(codes, scales, zeros)`, then
@@ -630,11 +642,7 @@ class W4Matrix:
     def __init__(self, R: int, K: int, group: int = 128, scale_dtype: torch.dtype = torch.bfloat16, zero_point: bool = False, device="cuda"):
         if scale_dtype not in _DTYPES:
             raise ValueError("scale_dtype: torch.float32 or torch.bfloat16")
-        self.desc, self.layout = W4Desc(R, K, group, _DTYPES[scale_dtype], int(zero_point)), W4Layout()
-        self._desc_ptr = C.addressof(self.desc)
-        st = lib().eesd_w4_layout_of(self._desc_ptr, C.addressof(self.layout))
-        if st:
-            raise EesdError(st, "eesd_w4_layout_of")
+        self.desc, self.layout, self._desc_ptr = _w4_describe(R, K, group, _DTYPES[scale_dtype], int(zero_point))
         self.shape, self.group, self.scale_dtype, self.zero_point, self.groups = (R, K), group, scale_dtype, bool(zero_point), self.layout.groups
         self.buffer = torch.empty(self.layout.total_bytes, dtype=_U8, device=device)
         self._index, self._ptr, self._bytes = _check_tensor(self.buffer, "device", (_U8,)), self.buffer.data_ptr(), self.layout.total_bytes
