@@ -421,8 +421,10 @@ template <int NT> constexpr int kDigits = NT <= 2 ? 4 : 3;
 template <int NT> constexpr int kTok = NT == 1 ? 2 : NT == 2 ? 4 : NT == 3 ? 8 : 16;   // token rows; column d * kTok + m is digit d of row m
 constexpr int kMaxRun = 32;     // row blocks of a run
 constexpr int kSmem = 227 * 1024;
-// staged activations of 128 columns: fragments [step pair][n-tile][lane][4 words], then {sum of the group's digits, unscale} [group][column]
-__host__ __device__ constexpr int act_bytes(int NT, int G) { return 1024 * NT + 128 / G * NT * 64; }
+// Staged activations of 128 columns: fragments [step pair][n-tile][lane][4 words], then for each group what its sums become fp32 with.  Up
+// to 4 rows, whose digits lie in several lanes: {sum of the group's digits, unscale} [group][column].  More rows, whose three digits a
+// lane holds: {unscale, sums of digits 0 + 256 * 1, of digits 2, -} [group][row].
+__host__ __device__ constexpr int act_bytes(int NT, int G) { return 1024 * NT + 128 / G * (NT == 3 ? 128 : NT == 6 ? 256 : NT * 64); }
 
 struct ProjArgs {
     const unsigned char *packed;
@@ -482,17 +484,24 @@ __device__ __forceinline__ void stage_piece(unsigned char *dst, float4 v, int m)
         act[(((step >> 1) * NT + (col >> 3)) * 32 + (col & 7) * 4 + t) * 4 + (step & 1) * 2 + half] = w[d];
     }
     // sums of a group's digits, two at a time as 16-bit fields of the bytes + 128
+    int sum[D + 1];
 #pragma unroll
     for (int d = 0; d < D; d += 2) {
-        uint32_t sum = __dp4a(w[d] ^ 0x80808080u, 0x01010101u, 0u) | __dp4a(w[d + 1] ^ 0x80808080u, 0x01010101u, 0u) << 16;
-        if (G == 128) sum = __reduce_add_sync(0xffffffffu, sum);
+        uint32_t two = __dp4a(w[d] ^ 0x80808080u, 0x01010101u, 0u) | __dp4a(w[d + 1] ^ 0x80808080u, 0x01010101u, 0u) << 16;
+        if (G == 128) two = __reduce_add_sync(0xffffffffu, two);
         else
 #pragma unroll
-            for (int o = 1; o < G / 4; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane % (G / 4) == 0) {
+            for (int o = 1; o < G / 4; o <<= 1) two += __shfl_xor_sync(0xffffffffu, two, o);
+        sum[d] = (int)(two & 0xffffu) - 128 * G;
+        sum[d + 1] = (int)(two >> 16) - 128 * G;
+    }
+    if (lane % (G / 4) == 0) {
+        if (NT >= 3) {
+            reinterpret_cast<float4 *>(dst + 1024 * NT)[lane / (G / 4) * TOK + m] = make_float4(un, __int_as_float(sum[0] + 256 * sum[1]), __int_as_float(sum[2]), 0.f);
+        } else {
             float2 *c = reinterpret_cast<float2 *>(dst + 1024 * NT) + lane / (G / 4) * NT * 8 + m;
-            c[d * TOK] = make_float2(__int_as_float((int)(sum & 0xffffu) - 128 * G), un * (float)(1u << (8 * d)));
-            if (d + 1 < D) c[(d + 1) * TOK] = make_float2(__int_as_float((int)(sum >> 16) - 128 * G), un * (float)(1ull << (8 * d + 8)));
+#pragma unroll
+            for (int d = 0; d < D; d++) c[d * TOK] = make_float2(__int_as_float(sum[d]), un * (float)(1u << (8 * d)));
         }
     }
 }
@@ -624,8 +633,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
         for (int n = 0; n < NA; n++)
 #pragma unroll
             for (int i = 0; i < 4; i++) acc[n][i] = 0.f;
-        // A sum starts at the bits of 1.5 * 2^23, so that it reads as 12582912 + sum in fp32 (|sum| <= 2^21, with the zero point's part below 2^22)
-        const int start[4] = {0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000};
+        // A single digit's sum starts at the bits of 1.5 * 2^23, so that it reads as 12582912 + sum in fp32 (|sum| <= 2^21, with the zero
+        // point's part below 2^22); digits 0 and 1 of more than 4 rows are joined as integers first (below 2^31)
+        const int start[4] = {0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000}, zero[4] = {0, 0, 0, 0};
         uint32_t flip;
         asm volatile("mov.b32 %0, 0x80808080;" : "=r"(flip));
         const unsigned char *bp = act + kp * kAct;
@@ -647,7 +657,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
                         const bool first = (jp * 2 + jj) % (G / 32) == 0;
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) {
-                            if (first) mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, start);
+                            if (first) mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, NT >= 3 && nt < 2 * NA ? zero : start);
                             else mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, g[nt]);
                         }
                         if ((jp * 64 + jj * 32 + 32) % G != 0) continue;
@@ -667,20 +677,38 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
                             z0 = 128 - 16 * (int)(r.z.v[gr / 4] >> (8 * (gr % 4)) & 0xffu);
                             z1 = 128 - 16 * (int)(r.z.v[(NG + gr) / 4] >> (8 * ((NG + gr) % 4)) & 0xffu);
                         }
-                        float h[NA][4];
+                        if constexpr (NT >= 3) {
+                            const float4 *meta = reinterpret_cast<const float4 *>(bp + 1024 * NT) + gr * kTok<NT> + 2 * t;
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) {
-                            const float4 c = *reinterpret_cast<const float4 *>(bp + 1024 * NT + (gr * NT + nt) * 64 + t * 16);   // columns 2t, 2t + 1: {sum, unscale}
+                            for (int n = 0; n < NA; n++) {
+                                const float4 c0 = meta[n * 8], c1 = meta[n * 8 + 1];   // the lane's two columns: token rows n * 8 + 2 t, + 1
 #pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const float q = __int_as_float(ZP ? g[nt][i] + (i < 2 ? z0 : z1) * __float_as_int(i & 1 ? c.z : c.x) : g[nt][i]) - 12582912.f, un = i & 1 ? c.w : c.y;
-                                h[nt % NA][i] = nt < NA ? q * un : fmaf(q, un, h[nt % NA][i]);
+                                for (int i = 0; i < 4; i++) {
+                                    const float4 c = i & 1 ? c1 : c0;
+                                    int lo = g[n][i] + 256 * g[NA + n][i], hi = g[2 * NA + n][i];
+                                    if (ZP) {
+                                        lo += (i < 2 ? z0 : z1) * __float_as_int(c.y);
+                                        hi += (i < 2 ? z0 : z1) * __float_as_int(c.z);
+                                    }
+                                    acc[n][i] = fmaf(fmaf(__int_as_float(hi) - 12582912.f, 65536.f, (float)lo) * c.x, i < 2 ? s0 : s1, acc[n][i]);
+                                }
                             }
+                        } else {
+                            float h[NA][4];
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++) {
+                                const float4 c = *reinterpret_cast<const float4 *>(bp + 1024 * NT + (gr * NT + nt) * 64 + t * 16);   // columns 2t, 2t + 1: {sum, unscale}
+#pragma unroll
+                                for (int i = 0; i < 4; i++) {
+                                    const float q = __int_as_float(ZP ? g[nt][i] + (i < 2 ? z0 : z1) * __float_as_int(i & 1 ? c.z : c.x) : g[nt][i]) - 12582912.f, un = i & 1 ? c.w : c.y;
+                                    h[nt % NA][i] = nt < NA ? q * un : fmaf(q, un, h[nt % NA][i]);
+                                }
+                            }
+#pragma unroll
+                            for (int n = 0; n < NA; n++)
+#pragma unroll
+                                for (int i = 0; i < 4; i++) acc[n][i] = fmaf(h[n][i], i < 2 ? s0 : s1, acc[n][i]);
                         }
-#pragma unroll
-                        for (int n = 0; n < NA; n++)
-#pragma unroll
-                            for (int i = 0; i < 4; i++) acc[n][i] = fmaf(h[n][i], i < 2 ? s0 : s1, acc[n][i]);
                     }
                 }
                 fetch(r);
