@@ -406,17 +406,21 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed
 // cycles and sub-processor, measured), and keeps the sums exact.
 //
 // Measured (a graph of calls, matrices that pass the L2 cache in turn; floor: bytes at the measured copy rate):
-//   15360 x 5120, groups of 128:               M = 1 12.1 us, 4 13.2, 8 15.0, 16 21.9 (floor 6.2)
-//   27648 x 5120, groups of 64, zero points:   M = 1 18.4, 5 25.6, 16 42.6 (floor 11.7)
-//   8192 x 28672, groups of 128, zero points:  M = 1 26.2 (4.7 TB/s), 4 30.0, 8 37.5, 16 58.5 (floor 18.6)
+//   15360 x 5120, groups of 128:               M = 1 12.1 us, 4 13.1, 5 14.9, 16 20.5 (floor 6.2)
+//   27648 x 5120, groups of 64, zero points:   M = 1 18.4, 5 23.3, 16 38.2 (floor 11.7)
+//   8192 x 28672, groups of 128, zero points:  M = 1 26.2 (4.7 TB/s), 4 30.0, 8 37.0, 16 52.8 (floor 18.6)
 // Few rows: about 5 us of launch, staging and joining, then memory (in the long case 71 % of its rate).  16 rows: 24 matrix
-// instructions, 18 shared-memory reads and some 200 instructions in all for 16 x 128 codes; the matrix pipe is 44 % busy, shared memory
-// 61 %, the issue slots 46 %, none of them alone the bound, and clusters of 4 leave 16 multiprocessors out.  Two row blocks a warp with half the warps (every
-// activation read serves twice the codes) took 65.8 us, the 5th generation tensor core (codes expanded into shared memory, one warp
-// issuing, 8 folding the sums out of tensor memory) 71 to 79 at 16 rows and 51 to 72 at 1: a unit of 128 x 128 costs it some 1000 cycles of
-// hand-overs between the warps, whatever the rows.
+// instructions, 16 shared-memory reads and some 190 instructions in all for 16 x 128 codes; when it took 58 us, the matrix pipe was 44 % busy, shared
+// memory 61 %, the issue slots 46 %, none of them alone the bound, and clusters of 4 leave 16 multiprocessors out.  Joining digits 0
+// and 1 as integers brought 53, from 58.  Two row blocks a warp with half the warps (every activation read serves twice the codes)
+// took 65.8, the tiles of 8 token rows after one another (24 registers fewer) 53.8, the 5th generation tensor core (codes expanded into shared
+// memory, one warp issuing, 8 folding the sums out of tensor memory) 71 to 79 at 16 rows and 51 to 72 at 1: a unit of 128 x 128 costs it some
+// 1000 cycles of hand-overs between the warps, whatever the rows.
 constexpr int kWarps = 16;
-template <int NT> constexpr int kAhead = NT == 6 ? 2 : 4;   // units a warp's loads run ahead
+// Units a warp's loads run ahead.  Few rows need the bytes in flight (8192 x 28672, M = 1: 2, 3, 4 units 29.0, 27.0, 26.2 us); with more the
+// products leave time, and the registers and the shorter loop are worth more (27648 x 5120, M = 5: 2, 3, 4 units 23.3, 24.6, 24.6; 15360 x 5120,
+// M = 16: 1, 2, 3 units 20.5, 21.7, 21.3).  12, 20 or 24 warps are slower nearly everywhere (M = 16: 55, 60, 66 against 53).
+template <int NT> constexpr int kAhead = NT == 6 ? 1 : NT == 3 ? 2 : 4;
 template <int NT> constexpr int kDigits = NT <= 2 ? 4 : 3;
 template <int NT> constexpr int kTok = NT == 1 ? 2 : NT == 2 ? 4 : NT == 3 ? 8 : 16;   // token rows; column d * kTok + m is digit d of row m
 constexpr int kMaxRun = 32;     // row blocks of a run
@@ -785,7 +789,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
 // 128 columns staged at a time.
 // How the matrix is cut: slices of K (a cluster's blocks), runs of row blocks, columns staged at a time.  The cost is in units of 16 x
 // 128 codes a warp streams.  Forced to 1, 2, 4 or 8 slices, 5120 to 28672 columns and 5 to 16 rows never ran more than 1 % faster than the
-// choice made here, and up to 2.7 times slower (8 slices of 27648 x 5120: 71.1 against 42.6 us).
+// choice made here, and up to twice slower (5 rows, 8 slices of 27648 x 5120: 49.8 against 25.7 us).
 struct Cut { int splits, runs, chunk, smem; };
 
 inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
