@@ -410,9 +410,9 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed
 //   27648 x 5120, groups of 64, zero points:   M = 1 18.4, 5 23.3, 16 38.2 (floor 11.7)
 //   8192 x 28672, groups of 128, zero points:  M = 1 26.2 (4.7 TB/s), 4 30.0, 8 37.0, 16 52.8 (floor 18.6)
 // Few rows: about 5 us of launch, staging and joining, then memory (in the long case 71 % of its rate).  16 rows: 24 matrix
-// instructions, 16 shared-memory reads and some 190 instructions in all for 16 x 128 codes; when it took 58 us, the matrix pipe was 44 % busy, shared
-// memory 61 %, the issue slots 46 %, none of them alone the bound, and clusters of 4 leave 16 multiprocessors out.  Joining digits 0
-// and 1 as integers brought 53, from 58.  Two row blocks a warp with half the warps (every activation read serves twice the codes)
+// instructions, 16 shared-memory reads and 178 instructions in all for 16 x 128 codes; the matrix pipe is 56 % busy, shared memory 64 %,
+// the issue slots 51 %, none of them alone the bound, and clusters of 4 leave 16 multiprocessors out.  Joining digits 0 and 1 as integers
+// brought 53, from 58.  Two row blocks a warp with half the warps (every activation read serves twice the codes)
 // took 65.8, the tiles of 8 token rows after one another (24 registers fewer) 53.8, the 5th generation tensor core (codes expanded into shared
 // memory, one warp issuing, 8 folding the sums out of tensor memory) 71 to 79 at 16 rows and 51 to 72 at 1: a unit of 128 x 128 costs it some
 // 1000 cycles of hand-overs between the warps, whatever the rows.
