@@ -159,13 +159,14 @@ template <int G, Extreme E> __device__ __forceinline__ void row_extremes(const F
 
 // Reads a weight once, writes half a byte.  The product with 1 / s, rounded to an integer, is the quotient's nearest or its neighbour
 // across a half: the exact remainder (one fused multiply-add) tells, and a row where some remainder reaches half a scale is put
-// right (common only as ties: bf16 weights over bf16 scales, 3.5 us of the 40).  Scales below 2^-100, whose reciprocal would not
+// right (common only as ties: bf16 weights over bf16 scales, 3 us of the 37).  Scales below 2^-100, whose reciprocal would not
 // do, are left to nearest_quotient at the end.
-// Measured, 5120 x 13824: fp32 weights 47 to 58 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 37 to 51 us
-// (floor 27: bound by issue, 14 instructions for a lane's weight, 2.8 of 4 a cycle).  Columns 16 to a lane (one lane a scale, no exchange) reads in
+// Measured, 5120 x 13824: fp32 weights 46 to 55 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 34 to 49 us
+// (floor 27: bound by issue, 14 instructions for a lane's weight, 2.8 of 4 a cycle with 3 blocks a multiprocessor; 4 blocks took it from
+// 40 to 37 us with groups of 128 and bf16 scales).  Columns 16 to a lane (one lane a scale, no exchange) reads in
 // pieces of 32 bytes and took 167 to 184 us.
 template <typename WT, int G, bool ZP>
-__global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 3 : 2) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
+__global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 4 : 2) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
@@ -218,37 +219,51 @@ __global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 3 : 2) quantize_kernel(
     }
     __syncwarp();
     const float4 *mine = rows[lane / (G / 4)];
+    constexpr int kTogether = sizeof(WT) == 4 ? 2 : 1;   // rows that one branch decides for (bf16, whose ties are common, 2: 43 us instead of 40)
 #pragma unroll
     for (int g = 0; g < 8; g++) {
         uint32_t c[2];
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            float sr, ir, zf = 12582920.f;
-            if (ZP) {
-                const float4 e = mine[g + 8 * h];
-                sr = e.x, ir = e.y, zf = e.z;
-            } else {
-                const float2 e = *reinterpret_cast<const float2 *>(&mine[g + 8 * h]);
-                sr = e.x, ir = e.y;
-            }
-            const float4 x4 = v[g + 8 * h].get();
-            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
-            float y[4], rem[4];
+        for (int h0 = 0; h0 < 2; h0 += kTogether) {
+            float y[kTogether][4], rem[kTogether][4], sr[kTogether], zf[kTogether];
+            bool off = false;
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                y[j] = __fmaf_rn(x[j], ir, zf);   // 1.5 * 2^23 + the code
-                rem[j] = __fmaf_rn(zf - y[j], sr, x[j]);
-            }
-            const float most = fmaxf(fmaxf(fabsf(rem[0]), fabsf(rem[1])), fmaxf(fabsf(rem[2]), fabsf(rem[3])));
-            if (most + most >= sr) {
+            for (int h = 0; h < kTogether; h++) {
+                const int r = g + 8 * (h0 + h);
+                float ir;
+                zf[h] = 12582920.f;
+                if (ZP) {
+                    const float4 e = mine[r];
+                    sr[h] = e.x, ir = e.y, zf[h] = e.z;
+                } else {
+                    const float2 e = *reinterpret_cast<const float2 *>(&mine[r]);
+                    sr[h] = e.x, ir = e.y;
+                }
+                const float4 x4 = v[r].get();
+                const float x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    const float twice = fabsf(rem[j] + rem[j]);
-                    if (twice > sr || (twice == sr && ((__float_as_int(y[j]) ^ __float_as_int(zf)) & 1))) y[j] += copysignf(1.f, rem[j]);
+                    y[h][j] = __fmaf_rn(x[j], ir, zf[h]);   // 1.5 * 2^23 + the code
+                    rem[h][j] = __fmaf_rn(zf[h] - y[h][j], sr[h], x[j]);
                 }
+                const float most = fmaxf(fmaxf(fabsf(rem[h][0]), fabsf(rem[h][1])), fmaxf(fabsf(rem[h][2]), fabsf(rem[h][3])));
+                off |= most + most >= sr[h];
             }
-            c[h] = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040), __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040), 0x5410);
-            if (ZP) c[h] -= c[h] >> 4 & 0x01010101u;   // 16 becomes 15
+            if (off) {
+#pragma unroll
+                for (int h = 0; h < kTogether; h++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float twice = fabsf(rem[h][j] + rem[h][j]);
+                        if (twice > sr[h] || (twice == sr[h] && ((__float_as_int(y[h][j]) ^ __float_as_int(zf[h])) & 1))) y[h][j] += copysignf(1.f, rem[h][j]);
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < kTogether; h++) {
+                uint32_t &q4 = c[h0 + h];
+                q4 = __byte_perm(__byte_perm(__float_as_uint(y[h][0]), __float_as_uint(y[h][1]), 0x0040), __byte_perm(__float_as_uint(y[h][2]), __float_as_uint(y[h][3]), 0x0040), 0x5410);
+                if (ZP) q4 -= q4 >> 4 & 0x01010101u;   // 16 becomes 15
+            }
         }
         *reinterpret_cast<uint32_t *>(blk + word_at(lane, g)) = (c[0] & 0x0f0f0f0fu) | (c[1] << 4 & 0xf0f0f0f0u);
     }
