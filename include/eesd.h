@@ -496,9 +496,9 @@ int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, 
 /* eesd_project_rows for a 4-bit matrix: out[m][r] = sum_k A[m][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A: M rows of a_dtype,
  * lda >= K elements apart; out: M fp32 rows, ldo >= R apart.  scratch: device, 16-byte aligned, eesd_w4_project_scratch_bytes bytes
  * (0 while M * ceil(K / 128) <= 32: then it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.  The same
- * bits on every call.  Activations are taken as fixed-point numbers, one scale for the same 128 columns (128 i .. 128 i + 127) of a
- * row: they are off by at most 2^-22.9 of the largest magnitude there (up to 4 rows: 2^-30.9), as the terms of a sum in fp32 are off by
- * their share of its largest; where that largest is below 2^-96 by up to 2^-127.  The sums of a group are exact, those over groups fp32.
+ * bits on every call.  An activation is taken as two fp16 terms under one power of two for the same 128 columns (128 i .. 128 i + 127) of
+ * a row: it is off by at most 2^-23 of itself, and where it is below 2^-27 of the largest there by at most 2^-50 of that largest.  Products with
+ * (c - z) are exact; sums are fp32 (within a group the tensor core's, which cuts off below 2^-23 of the running sum).
  * A row of A that holds a NaN or an infinity gives NaN; the other rows are not touched by it. */
 size_t eesd_w4_project_scratch_bytes(const eesd_w4 *m, int M);
 int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,

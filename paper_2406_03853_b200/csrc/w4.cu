@@ -5,12 +5,13 @@
 //   out[m][r]   = sum_G s(r, G) * sum_{k in G} (c(r, k) - z(r, G)) * A[m][k]
 //
 // Storage: blocks of 16 rows x 128 columns, the blocks of a row block one after the other along K, so that a warp streams
-// contiguous memory.  A block holds its codes in the register order of the matrix instruction that consumes them (m16n8k32 on bytes: 16
-// weight rows, 32 columns; two tiles of 64 columns, lane l's 16 bytes of a tile together), then its groups' scales, then their zero
+// contiguous memory.  A block holds its codes near the register order of the matrix instruction that consumes them (m16n8k16 on fp16: 16
+// weight rows, 16 columns; two tiles of 64 columns, lane l's 16 bytes of a tile together), then its groups' scales, then their zero
 // points, both [row % 8][row / 8][group]: what a lane needs of them lies together.  Element (r, k) of a tile: lane (r % 8) * 4 + (k %
-// 16) / 4, word k / 16, bits 8 * (k % 4) + 4 * (r / 8) of it: the low nibbles of a word are a fragment register of row r % 8,
-// the high ones that of row r % 8 + 8.
+// 16) / 4, word k / 16, bits 8 * (k % 4) + 4 * (r / 8) of it: a word is a lane's share of one instruction's 16 x 16 codes, the low
+// nibbles of row r % 8, the high ones of row r % 8 + 8.
 #include <cooperative_groups.h>
+#include <cuda_fp16.h>
 
 #include <atomic>
 
@@ -411,39 +412,31 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed
 // to one unit whatever the shape; a warp's first and last row block may be shared with its neighbours and are added up at the end.
 // Weights go straight into registers, kAhead units ahead.
 //
-// The products are integer: a code enters as the signed byte 16 (c - 8), its four bits with the top one flipped in the byte's upper half
-// (one three-input logic operation, for half the registers after one shift), an activation as
-// signed 8-bit digits of a fixed-point number, one power-of-two scale for each token row and 128 columns; a digit is a
-// column of the matrix instruction.  The sums of a group are exact, a zero point is taken off them exactly (16 (z - 8) times the group's
-// sum of digits), and fp32 begins where a group's sum meets its scale.  Up to 4 rows take 4 digits (31 bits of the largest
-// magnitude in the 128 columns), more rows 3 (22.99 bits).  Against fp16 terms (two per fp32 row, 1024 + c minus 1024 + z) this
-// takes 3 instead of 9 operations for 8 codes, half to three quarters of the matrix instructions (both kinds: one per 8
-// cycles and sub-processor, measured), and keeps the sums exact.
+// The products are fp16 with fp32 sums: a code enters as 32 (c - z), exactly (the nibble set into the mantissa of 1024, or of 1024 + 16 c
+// for a high one, and one fused multiply-add that takes the zero point off), an activation as two fp16 terms of 11 bits, hi and 2048 lo,
+// after a power of two for each token row and 128 columns has put the largest magnitude there into [2^14, 2^15).  Each term is a column of
+// the matrix instruction, so the two have sums of their own, joined at the end of a group; each activation keeps its own
+// exponent, so a large one takes nothing from its neighbours: an activation of at least 2^-27 of the largest is off by 2^-23 of itself,
+// a smaller one by 2^-50 of the largest, and one whose code stands for 0 adds nothing.  fp32 begins with the sums: hi terms of like size add
+// up exactly (11 bits and a code's 4), the tensor core cuts off below 2^-23 of the running sum, the scale of a group comes after.
+// Signed 8-bit digits of fixed-point numbers (integer products, exact sums, a third of the expanding operations) were faster at 16 rows but held an
+// activation to 2^-23 or 2^-31 of the largest of its 128 columns, whatever its own size.
 //
 // Measured (a graph of calls, matrices that pass the L2 cache in turn; floor: bytes at the measured copy rate):
-//   15360 x 5120, groups of 128:               M = 1 12.1 us, 4 13.1, 5 14.9, 16 20.5 (floor 6.2)
-//   27648 x 5120, groups of 64, zero points:   M = 1 18.4, 5 23.3, 16 38.2 (floor 11.7)
-//   8192 x 28672, groups of 128, zero points:  M = 1 26.2 (4.7 TB/s), 4 30.0, 8 37.0, 16 52.8 (floor 18.6)
-// Few rows: about 5 us of launch, staging and joining, then memory (in the long case 71 % of its rate).  16 rows: 24 matrix
-// instructions, 16 shared-memory reads and 178 instructions in all for 16 x 128 codes; the matrix pipe is 56 % busy, shared memory 64 %,
-// the issue slots 51 %, none of them alone the bound, and clusters of 4 leave 16 multiprocessors out.  Joining digits 0 and 1 as integers
-// brought 53, from 58.  Two row blocks a warp with half the warps (every activation read serves twice the codes)
-// took 65.8, the tiles of 8 token rows after one another (24 registers fewer) 53.8, the 5th generation tensor core (codes expanded into shared
-// memory, one warp issuing, 8 folding the sums out of tensor memory) 71 to 79 at 16 rows and 51 to 72 at 1: a unit of 128 x 128 costs it some
-// 1000 cycles of hand-overs between the warps, whatever the rows.
+//   15360 x 5120, groups of 128:               M = 1 13.5 us, 4 13.8, 8 17.1, 16 23.6 (floor 6.2)
+//   27648 x 5120, groups of 64, zero points:   M = 1 21.0, 4 21.1, 8 26.2, 16 38.0 (floor 11.7)
+//   8192 x 28672, groups of 128, zero points:  M = 1 29.6 (4.1 TB/s), 4 32.5, 8 42.4, 16 62.9 (floor 18.6)
 constexpr int kWarps = 16;
-// Units a warp's loads run ahead.  Few rows need the bytes in flight (8192 x 28672, M = 1: 2, 3, 4 units 29.0, 27.0, 26.2 us); with more the
-// products leave time, and the registers and the shorter loop are worth more (27648 x 5120, M = 5: 2, 3, 4 units 23.3, 24.6, 24.6; 15360 x 5120,
-// M = 16: 1, 2, 3 units 20.5, 21.7, 21.3).  12, 20 or 24 warps are slower nearly everywhere (M = 16: 55, 60, 66 against 53).
-template <int NT> constexpr int kAhead = NT == 6 ? 1 : NT == 3 ? 2 : 4;
-template <int NT> constexpr int kDigits = NT <= 2 ? 4 : 3;
-template <int NT> constexpr int kTok = NT == 1 ? 2 : NT == 2 ? 4 : NT == 3 ? 8 : 16;   // token rows; column d * kTok + m is digit d of row m
+template <int TOK> constexpr int kAhead = TOK == 16 ? 1 : TOK == 8 ? 2 : 4;   // units a warp's loads run ahead
 constexpr int kMaxRun = 32;     // row blocks of a run
 constexpr int kSmem = 227 * 1024;
-// Staged activations of 128 columns: fragments [step pair][n-tile][lane][4 words], then for each group what its sums become fp32 with.  Up
-// to 4 rows, whose digits lie in several lanes: {sum of the group's digits, unscale} [group][column].  More rows, whose three digits a
-// lane holds: {unscale, sums of digits 0 + 256 * 1, of digits 2, -} [group][row].
-__host__ __device__ constexpr int act_bytes(int NT, int G) { return 1024 * NT + 128 / G * (NT == 3 ? 128 : NT == 6 ? 256 : NT * 64); }
+// A kernel is for up to TOK token rows (1, 2, 4, 8, 16): tiles of the matrix instruction, and columns of a tile that are kept (term j of a
+// tile's row i is its column 2 i + j, so a lane's two results of a weight row are one token row's; 1 and 2 rows fill the tile by repetition)
+__host__ __device__ constexpr int tiles(int TOK) { return TOK <= 4 ? 1 : TOK / 4; }
+__host__ __device__ constexpr int columns(int TOK) { return TOK <= 4 ? 2 * TOK : 8; }
+// Staged activations of 128 columns: fragments [step pair][tile][column][lane % 4][4 words], then the rows' unscales.
+__host__ __device__ constexpr int frag_size(int TOK) { return 256 * tiles(TOK) * columns(TOK); }
+__host__ __device__ constexpr int act_bytes(int TOK) { return frag_size(TOK) + (TOK <= 4 ? 16 : TOK * 4); }
 
 struct ProjArgs {
     const unsigned char *packed;
@@ -473,81 +466,58 @@ __device__ __forceinline__ float4 load_a4(const ProjArgs &p, int m, int k) {
     return make_float4(v[0], v[1], v[2], v[3]);
 }
 
-// A warp turns 128 columns of token row m (lane: columns 4 * lane .. + 3) into digits at dst.  The scale 2^f puts the largest
-// magnitude just below 127.5 * 256^(digits - 1), as far up as signed digits reach; f stops at 126 (so that 2^-f stays normal).
-template <int NT, int G>
+// A warp turns 128 columns of token row m (lane: columns 4 * lane .. + 3) into two fp16 terms each at dst.  The scale 2^f puts the largest
+// magnitude into [2^14, 2^15), so that no sum overflows and 28 binary orders below it are normal numbers; f stops at 126 (2^-f stays normal).
+template <int TOK>
 __device__ __forceinline__ void stage_piece(unsigned char *dst, float4 v, int m) {
-    constexpr int D = kDigits<NT>, TOK = kTok<NT>;
     const int lane = threadIdx.x & 31;
     const uint32_t mx = __reduce_max_sync(0xffffffffu, max(max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu),
                                                            max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu)));
     const bool bad = mx >= 0x7f800000u;   // a NaN or infinity: the row's results are NaN
-    int f = (D == 4 ? 30 : 22) + 127 - (int)(mx >> 23);
-    if (f > 126) f = 126;
-    if (__uint_as_float(mx) * __int_as_float((127 + f) << 23) > (D == 4 ? 2139062016.f : 8355711.f)) f--;   // 0x7f7f7f00, 0x7f7f7f
-    const float sc = bad ? 0.f : __int_as_float((127 + f) << 23);
-    const float un = (bad ? __uint_as_float(0x7fc00000u) : __int_as_float((127 - f) << 23)) * 0.0625f;   // (codes enter 16-fold)
-    constexpr uint32_t bias = D == 4 ? 0x80808080u : 0x00808080u;   // q + bias has the digits + 128 as its bytes
-    uint32_t q[4];
+    const int f = min(14 + 127 - (int)(mx >> 23), 126);
+    const float sc = __int_as_float((127 + f) << 23);
     const float x[4] = {v.x, v.y, v.z, v.w};
+    __half hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) q[i] = ((uint32_t)(bad ? 0 : __float2int_rn(x[i] * sc)) + bias) ^ bias;
-    // word d: digit d of the four columns
-    const uint32_t lo01 = __byte_perm(q[0], q[1], 0x5140), lo23 = __byte_perm(q[2], q[3], 0x5140), hi01 = __byte_perm(q[0], q[1], 0x7362), hi23 = __byte_perm(q[2], q[3], 0x7362);
-    const uint32_t w[4] = {__byte_perm(lo01, lo23, 0x5410), __byte_perm(lo01, lo23, 0x7632), __byte_perm(hi01, hi23, 0x5410), __byte_perm(hi01, hi23, 0x7632)};
-    uint32_t *act = reinterpret_cast<uint32_t *>(dst);
-    const int step = lane >> 3, half = (lane >> 2) & 1, t = lane & 3;
-#pragma unroll
-    for (int d = 0; d < D; d++) {
-        const int col = d * TOK + m;
-        act[(((step >> 1) * NT + (col >> 3)) * 32 + (col & 7) * 4 + t) * 4 + (step & 1) * 2 + half] = w[d];
+    for (int i = 0; i < 4; i++) {
+        const float y = bad ? 0.f : x[i] * sc;
+        hi[i] = __float2half_rn(y);
+        lo[i] = __float2half_rn((y - __half2float(hi[i])) * 2048.f);
     }
-    // sums of a group's digits, two at a time as 16-bit fields of the bytes + 128
-    int sum[D + 1];
-#pragma unroll
-    for (int d = 0; d < D; d += 2) {
-        uint32_t two = __dp4a(w[d] ^ 0x80808080u, 0x01010101u, 0u) | __dp4a(w[d + 1] ^ 0x80808080u, 0x01010101u, 0u) << 16;
-        if (G == 128) two = __reduce_add_sync(0xffffffffu, two);
-        else
-#pragma unroll
-            for (int o = 1; o < G / 4; o <<= 1) two += __shfl_xor_sync(0xffffffffu, two, o);
-        sum[d] = (int)(two & 0xffffu) - 128 * G;
-        sum[d + 1] = (int)(two >> 16) - 128 * G;
-    }
-    if (lane % (G / 4) == 0) {
-        if (NT >= 3) {
-            reinterpret_cast<float4 *>(dst + 1024 * NT)[lane / (G / 4) * TOK + m] = make_float4(un, __int_as_float(sum[0] + 256 * sum[1]), __int_as_float(sum[2]), 0.f);
-        } else {
-            float2 *c = reinterpret_cast<float2 *>(dst + 1024 * NT) + lane / (G / 4) * NT * 8 + m;
-#pragma unroll
-            for (int d = 0; d < D; d++) c[d * TOK] = make_float2(__int_as_float(sum[d]), un * (float)(1u << (8 * d)));
-        }
-    }
+    // operand words: columns 0 and 2, columns 1 and 3 of the lane's four (the order that codes expand in)
+    auto two = [](__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; };
+    const int step = lane >> 2, t = lane & 3;
+    uint2 *act = reinterpret_cast<uint2 *>(dst) + (((step >> 1) * tiles(TOK) + (m >> 2)) * columns(TOK) * 4 + (m & 3) * 8 + t) * 2 + (step & 1);
+    act[0] = make_uint2(two(hi[0], hi[2]), two(hi[1], hi[3]));
+    act[8] = make_uint2(two(lo[0], lo[2]), two(lo[1], lo[3]));
+    if (lane == 0)   // (codes enter 32-fold)
+        reinterpret_cast<float *>(dst + frag_size(TOK))[m] = (bad ? __uint_as_float(0x7fc00000u) : __int_as_float((127 - f) << 23)) * 0.03125f;
 }
 
 // the same for a whole matrix, into global memory (many token rows: staging once costs less than once per block of threads)
-template <int NT, int G>
+template <int TOK>
 __global__ void __launch_bounds__(256) stage_kernel(const ProjArgs p, unsigned char *frag) {
     pdl_wait();      // everything before this launch is complete once the trigger fires: the projection may read the matrix before its own wait
     pdl_trigger();
     const int lane = threadIdx.x & 31, job = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (job >= p.KB * p.M) return;
     const int m = job / p.KB, kb = job % p.KB;
-    stage_piece<NT, G>(frag + (size_t)kb * act_bytes(NT, G), load_a4(p, m, kb * 128 + lane * 4), m);
+    stage_piece<TOK>(frag + (size_t)kb * act_bytes(TOK), load_a4(p, m, kb * 128 + lane * 4), m);
 }
 
-// (x ^ 0x80..) & 0xf0..: in every byte 16 times the code of its upper half less 8 (with both constants known the compiler would
-// take two operations)
-__device__ __forceinline__ uint32_t signed16(uint32_t x, uint32_t flip) {
+// 32 (c - z) of two codes as fp16: the nibbles of x that MASK names, set into the mantissa of 1024, times 2 or 32 and less the zero point's
+// part, exactly (with mask and 1024 both known the compiler would take two operations for the first)
+template <uint32_t MASK> __device__ __forceinline__ uint32_t expand(uint32_t x, uint32_t ones, uint32_t less) {
     uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(x), "r"(flip), "n"(0xf0f0f0f0));   // (a ^ b) & c
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(MASK), "r"(ones));   // (a & b) | c
+    asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(r) : "r"(MASK == 0x000f000fu ? 0x50005000u : 0x40004000u), "r"(less));
     return r;
 }
-// s8 x s8 products onto c (an exact integer sum)
-__device__ __forceinline__ void mma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const int (&c)[4]) {
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
+// fp16 products onto c
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const unsigned char *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -566,9 +536,9 @@ template <int N> __device__ __forceinline__ void load_once(Bytes<N> &d, const un
 
 // shared memory: activations | partial results of shared row blocks | results
 struct Smem { int slots, outs, total; };
-__host__ __device__ inline Smem carve(int NT, int G, int M, int chunk, int run) {
+__host__ __device__ inline Smem carve(int TOK, int M, int chunk, int run) {
     Smem s;
-    s.slots = chunk * act_bytes(NT, G);
+    s.slots = chunk * act_bytes(TOK);
     s.outs = s.slots + kWarps * 2 * M * 64;
     s.total = s.outs + run * M * 64;
     return s;
@@ -577,16 +547,16 @@ __host__ __device__ inline Smem carve(int NT, int G, int M, int chunk, int run) 
 // first unit of warp w
 __device__ __forceinline__ int unit_of(int units, int w) { return (int)(((long long)units * w) / kWarps); }
 
-template <int NT, int G, bool ZP, bool F32S>
+template <int TOK, int G, bool ZP, bool F32S>
 __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs p) {
-    constexpr int NG = 128 / G, kScaleBytes = 2 * NG * (F32S ? 4 : 2), kZeros = 1024 + 8 * kScaleBytes, kRecord = kZeros + (ZP ? NG * 16 : 0), U = kAhead<NT>;
-    constexpr int kAct = act_bytes(NT, G), NA = NT == 6 ? 2 : 1;   // NA: n-tiles that hold different token rows
+    constexpr int NG = 128 / G, kScaleBytes = 2 * NG * (F32S ? 4 : 2), kZeros = 1024 + 8 * kScaleBytes, kRecord = kZeros + (ZP ? NG * 16 : 0), U = kAhead<TOK>;
+    constexpr int kAct = act_bytes(TOK), NT = tiles(TOK), COLS = columns(TOK);
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t = lane & 3;
     const int splits = (int)gridDim.y, split = (int)blockIdx.y, runs = (int)gridDim.x;
     const int rb0 = (int)((long long)p.RB * blockIdx.x / runs), run = (int)((long long)p.RB * (blockIdx.x + 1) / runs) - rb0;
     const int kb0 = (int)((long long)p.KB * split / splits), kbn = (int)((long long)p.KB * (split + 1) / splits) - kb0;
-    const Smem sm = carve(NT, G, p.M, p.chunk, 0);
+    const Smem sm = carve(TOK, p.M, p.chunk, 0);
     unsigned char *act = smem;
     float *slots = reinterpret_cast<float *>(smem + sm.slots), *outs = reinterpret_cast<float *>(smem + sm.outs);
 
@@ -641,93 +611,65 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
 #pragma unroll
                 for (int i = 0; i < kBatch; i++) {
                     const int it = it0 + i * kWarps, m = it / cn;
-                    if (it < p.M * cn) stage_piece<NT, G>(act + (it - m * cn) * kAct, v[i], m);
+                    if (it < p.M * cn) stage_piece<TOK>(act + (it - m * cn) * kAct, v[i], m);
                 }
             }
         }
         __syncthreads();
 
-        float acc[NA][4];
+        float acc[NT][2];   // token row 4 n + t, weight rows g8 and g8 + 8
 #pragma unroll
-        for (int n = 0; n < NA; n++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) acc[n][i] = 0.f;
-        // A single digit's sum starts at the bits of 1.5 * 2^23, so that it reads as 12582912 + sum in fp32 (|sum| <= 2^21, with the zero
-        // point's part below 2^22); digits 0 and 1 of more than 4 rows are joined as integers first (below 2^31)
-        const int start[4] = {0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000}, zero[4] = {0, 0, 0, 0};
-        uint32_t flip;
-        asm volatile("mov.b32 %0, 0x80808080;" : "=r"(flip));
+        for (int n = 0; n < NT; n++) acc[n][0] = acc[n][1] = 0.f;
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t ones;
+        asm volatile("mov.b32 %0, 0x64006400;" : "=r"(ones));
         const unsigned char *bp = act + kp * kAct;
         for (int u = u0; u < u1;) {
 #pragma unroll
             for (int slot = 0; slot < U; slot++) {
                 if (u == u1) break;
                 Unit &r = ring[slot];
-                int g[NT][4];
+                float g[NT][4], un[NT];
 #pragma unroll
-                for (int jp = 0; jp < 2; jp++) {   // 64 columns: a tile, two steps
+                for (int n = 0; n < NT; n++) un[n] = reinterpret_cast<const float *>(bp + frag_size(TOK))[n * 4 + t];
+#pragma unroll
+                for (int jp = 0; jp < 4; jp++) {   // 32 columns: two steps
                     uint4 b[NT];
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) b[nt] = *reinterpret_cast<const uint4 *>(bp + (jp * NT + nt) * 512 + lane * 16);
+                    for (int n = 0; n < NT; n++) b[n] = *reinterpret_cast<const uint4 *>(bp + (jp * NT + n) * COLS * 64 + (COLS == 8 ? lane : lane % (4 * COLS)) * 16);
+                    const int gr = jp * 32 / G;
+                    uint32_t less0 = 0xf800f800u + 8u * 0x00010001u, less1 = 0xe800e800u + 8u * 0x00100010u;   // -32 (1024 + z), -2 (1024 + 16 z)
+                    if (ZP) {   // bytes gr and NG + gr
+                        less0 = 0xf800f800u + (r.z.v[gr / 4] >> (8 * (gr % 4)) & 0xffu) * 0x00010001u;
+                        less1 = 0xe800e800u + (r.z.v[(NG + gr) / 4] >> (8 * ((NG + gr) % 4)) & 0xffu) * 0x00100010u;
+                    }
 #pragma unroll
                     for (int jj = 0; jj < 2; jj++) {
-                        const uint32_t x = r.w[jp].v[jj * 2], y = r.w[jp].v[jj * 2 + 1];
-                        const uint32_t a[4] = {signed16(x << 4, flip), signed16(x, flip), signed16(y << 4, flip), signed16(y, flip)};
-                        const bool first = (jp * 2 + jj) % (G / 32) == 0;
+                        const uint32_t x = r.w[jp >> 1].v[(jp & 1) * 2 + jj], x8 = x >> 8;
+                        const uint32_t a[4] = {expand<0x000f000fu>(x, ones, less0), expand<0x00f000f0u>(x, ones, less1),
+                                               expand<0x000f000fu>(x8, ones, less0), expand<0x00f000f0u>(x8, ones, less1)};
+                        const bool first = (jp * 32 + jj * 16) % G == 0;
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) {
-                            if (first) mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, NT >= 3 && nt < 2 * NA ? zero : start);
-                            else mma(g[nt], a, jj == 0 ? b[nt].x : b[nt].z, jj == 0 ? b[nt].y : b[nt].w, g[nt]);
+                        for (int n = 0; n < NT; n++) {
+                            if (first) mma(g[n], a, jj == 0 ? b[n].x : b[n].z, jj == 0 ? b[n].y : b[n].w, zero);
+                            else mma(g[n], a, jj == 0 ? b[n].x : b[n].z, jj == 0 ? b[n].y : b[n].w, g[n]);
                         }
-                        if ((jp * 64 + jj * 32 + 32) % G != 0) continue;
-                        // the group is complete: digits' sums less z times the activations' to fp32, the digits joined, times the scale
-                        const int gr = (jp * 64 + jj * 32) / G;
-                        float s0, s1;
-                        if (F32S) {
-                            s0 = __uint_as_float(r.s.v[gr]);
-                            s1 = __uint_as_float(r.s.v[NG + gr]);
-                        } else {   // halfwords gr and NG + gr
-                            const uint32_t sa = r.s.v[gr / 2], sb = r.s.v[(NG + gr) / 2];
-                            s0 = __uint_as_float(gr & 1 ? sa & 0xffff0000u : sa << 16);
-                            s1 = __uint_as_float((NG + gr) & 1 ? sb & 0xffff0000u : sb << 16);
-                        }
-                        int z0 = 0, z1 = 0;   // 16 (8 - z)
-                        if (ZP) {   // bytes gr and NG + gr
-                            z0 = 128 - 16 * (int)(r.z.v[gr / 4] >> (8 * (gr % 4)) & 0xffu);
-                            z1 = 128 - 16 * (int)(r.z.v[(NG + gr) / 4] >> (8 * ((NG + gr) % 4)) & 0xffu);
-                        }
-                        if constexpr (NT >= 3) {
-                            const float4 *meta = reinterpret_cast<const float4 *>(bp + 1024 * NT) + gr * kTok<NT> + 2 * t;
+                    }
+                    if ((jp * 32 + 32) % G != 0) continue;
+                    // the group is complete: the two terms' sums joined, unscaled, times the scale
+                    float s0, s1;
+                    if (F32S) {
+                        s0 = __uint_as_float(r.s.v[gr]);
+                        s1 = __uint_as_float(r.s.v[NG + gr]);
+                    } else {   // halfwords gr and NG + gr
+                        const uint32_t sa = r.s.v[gr / 2], sb = r.s.v[(NG + gr) / 2];
+                        s0 = __uint_as_float(gr & 1 ? sa & 0xffff0000u : sa << 16);
+                        s1 = __uint_as_float((NG + gr) & 1 ? sb & 0xffff0000u : sb << 16);
+                    }
 #pragma unroll
-                            for (int n = 0; n < NA; n++) {
-                                const float4 c0 = meta[n * 8], c1 = meta[n * 8 + 1];   // the lane's two columns: token rows n * 8 + 2 t, + 1
-#pragma unroll
-                                for (int i = 0; i < 4; i++) {
-                                    const float4 c = i & 1 ? c1 : c0;
-                                    int lo = g[n][i] + 256 * g[NA + n][i], hi = g[2 * NA + n][i];
-                                    if (ZP) {
-                                        lo += (i < 2 ? z0 : z1) * __float_as_int(c.y);
-                                        hi += (i < 2 ? z0 : z1) * __float_as_int(c.z);
-                                    }
-                                    acc[n][i] = fmaf(fmaf(__int_as_float(hi) - 12582912.f, 65536.f, (float)lo) * c.x, i < 2 ? s0 : s1, acc[n][i]);
-                                }
-                            }
-                        } else {
-                            float h[NA][4];
-#pragma unroll
-                            for (int nt = 0; nt < NT; nt++) {
-                                const float4 c = *reinterpret_cast<const float4 *>(bp + 1024 * NT + (gr * NT + nt) * 64 + t * 16);   // columns 2t, 2t + 1: {sum, unscale}
-#pragma unroll
-                                for (int i = 0; i < 4; i++) {
-                                    const float q = __int_as_float(ZP ? g[nt][i] + (i < 2 ? z0 : z1) * __float_as_int(i & 1 ? c.z : c.x) : g[nt][i]) - 12582912.f, un = i & 1 ? c.w : c.y;
-                                    h[nt % NA][i] = nt < NA ? q * un : fmaf(q, un, h[nt % NA][i]);
-                                }
-                            }
-#pragma unroll
-                            for (int n = 0; n < NA; n++)
-#pragma unroll
-                                for (int i = 0; i < 4; i++) acc[n][i] = fmaf(h[n][i], i < 2 ? s0 : s1, acc[n][i]);
-                        }
+                    for (int n = 0; n < NT; n++) {
+                        acc[n][0] = fmaf(fmaf(g[n][1], 0x1p-11f, g[n][0]) * un[n], s0, acc[n][0]);
+                        acc[n][1] = fmaf(fmaf(g[n][3], 0x1p-11f, g[n][2]) * un[n], s1, acc[n][1]);
                     }
                 }
                 fetch(r);
@@ -739,19 +681,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
                     float *d = first ? slots + warp * 2 * p.M * 16 : last ? slots + (warp * 2 + 1) * p.M * 16 : outs + rbi * p.M * 16;
                     const bool add = !first && !last && c0;
 #pragma unroll
-                    for (int n = 0; n < NA; n++)
+                    for (int n = 0; n < NT; n++) {
+                        const int m = n * 4 + t;
 #pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            float v = acc[n][i];
-                            if (kTok<NT> <= 4) v += __shfl_xor_sync(0xffffffffu, v, 2);   // digits in other lanes of the quad
-                            if (kTok<NT> == 2) v += __shfl_xor_sync(0xffffffffu, v, 1);
-                            const int m = n * 8 + 2 * t + (i & 1);
-                            if (m < kTok<NT> && m < p.M) {
-                                float *o = d + m * 16 + g8 + (i >> 1) * 8;
-                                *o = add ? *o + v : v;
-                            }
+                        for (int i = 0; i < 2; i++) {
+                            float *o = d + m * 16 + g8 + i * 8;
+                            if (m < p.M) *o = add ? *o + acc[n][i] : acc[n][i];
                             acc[n][i] = 0.f;
                         }
+                    }
                     kp = 0;
                     bp = act;
                     rbi++;
@@ -807,7 +745,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
 // choice made here, and up to twice slower (5 rows, 8 slices of 27648 x 5120: 49.8 against 25.7 us).
 struct Cut { int splits, runs, chunk, smem; };
 
-inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
+inline Cut pick_cut(int TOK, int M, int RB, int KB) {
     Cut best = {};
     double cost = 1e300;
     for (int s = 1; s <= 8; s *= 2) {
@@ -816,8 +754,8 @@ inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
         const int waves = (RB + clusters * kMaxRun - 1) / (clusters * kMaxRun);
         const int runs = RB < clusters * waves ? RB : clusters * waves;
         const int run = (RB + runs - 1) / runs, slice = (KB + s - 1) / s;
-        const Smem fixed = carve(NT, G, M, 0, run);
-        int chunk = (kSmem - fixed.total) / act_bytes(NT, G);
+        const Smem fixed = carve(TOK, M, 0, run);
+        int chunk = (kSmem - fixed.total) / act_bytes(TOK);
         if (chunk < 1) continue;
         const int n_chunks = (slice + chunk - 1) / chunk;
         chunk = (slice + n_chunks - 1) / n_chunks;
@@ -825,7 +763,7 @@ inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
         const double c = (double)waves * (run * (double)slice / kWarps + n_chunks * (4.0 + 0.02 * M * chunk) + (s > 1 ? 2.0 + 0.5 * s : 0.0));
         if (c < cost) {
             cost = c;
-            best = {s, runs, chunk, carve(NT, G, M, chunk, run).total};
+            best = {s, runs, chunk, carve(TOK, M, chunk, run).total};
         }
     }
     return best;
@@ -834,13 +772,13 @@ inline Cut pick_cut(int NT, int G, int M, int RB, int KB) {
 // Staged activations: bytes of scratch (0: each block of threads stages for itself).  A launch of its own costs about a microsecond, staging in every
 // block 0.1 us for 4 pieces of 128 columns: 1024 x 256 with 16 rows (32 pieces) 4.1 us in the blocks against 4.9 by a launch, 15360 x
 // 5120 with 4 rows (160 pieces) 16.2 against 13.1.
-inline int n_tiles(int M) { return M <= 2 ? 1 : M <= 4 ? 2 : M <= 8 ? 3 : 6; }
+inline int tokens(int M) { return M <= 2 ? M : M <= 4 ? 4 : M <= 8 ? 8 : 16; }
 inline bool stage_first(int M, int KB) { return M * KB > 32; }
-inline size_t frag_bytes(int M, int KB, int group) { return !stage_first(M, KB) ? 0 : (size_t)KB * act_bytes(n_tiles(M), group); }
+inline size_t frag_bytes(int M, int KB) { return !stage_first(M, KB) ? 0 : (size_t)KB * act_bytes(tokens(M)); }
 
-template <int NT, int G, bool ZP, bool F32S>
+template <int TOK, int G, bool ZP, bool F32S>
 cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
-    auto kernel = project_kernel<NT, G, ZP, F32S>;
+    auto kernel = project_kernel<TOK, G, ZP, F32S>;
     {   // more shared memory than a kernel gets unasked: once per device
         static std::atomic<uint64_t> done{0};
         int dev = 0;
@@ -852,12 +790,12 @@ cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
             if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
         }
     }
-    const Cut cut = pick_cut(NT, G, p.M, p.RB, p.KB);
+    const Cut cut = pick_cut(TOK, p.M, p.RB, p.KB);
     if (!cut.runs) return cudaErrorInvalidConfiguration;
     p.chunk = cut.chunk;
     p.frag = nullptr;
     if (stage_first(p.M, p.KB)) {
-        launch_k(stage_kernel<NT, G>, dim3((p.KB * p.M + 7) / 8), dim3(256), 0, s, pdl_enabled(), p, scratch);
+        launch_k(stage_kernel<TOK>, dim3((p.KB * p.M + 7) / 8), dim3(256), 0, s, pdl_enabled(), p, scratch);
         p.frag = scratch;
     }
     cudaLaunchConfig_t cfg = {};
@@ -884,16 +822,16 @@ cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int NT, int G>
+template <int TOK, int G>
 cudaError_t launch_kind(cudaStream_t s, const ProjArgs &p, bool zp, bool f32s, unsigned char *scratch) {
-    if (zp) return f32s ? launch_project<NT, G, true, true>(s, p, scratch) : launch_project<NT, G, true, false>(s, p, scratch);
-    return f32s ? launch_project<NT, G, false, true>(s, p, scratch) : launch_project<NT, G, false, false>(s, p, scratch);
+    if (zp) return f32s ? launch_project<TOK, G, true, true>(s, p, scratch) : launch_project<TOK, G, true, false>(s, p, scratch);
+    return f32s ? launch_project<TOK, G, false, true>(s, p, scratch) : launch_project<TOK, G, false, false>(s, p, scratch);
 }
-template <int NT>
+template <int TOK>
 cudaError_t launch_group(cudaStream_t s, const ProjArgs &p, int group, bool zp, bool f32s, unsigned char *scratch) {
-    return group == 32 ? launch_kind<NT, 32>(s, p, zp, f32s, scratch)
-           : group == 64 ? launch_kind<NT, 64>(s, p, zp, f32s, scratch)
-                         : launch_kind<NT, 128>(s, p, zp, f32s, scratch);
+    return group == 32 ? launch_kind<TOK, 32>(s, p, zp, f32s, scratch)
+           : group == 64 ? launch_kind<TOK, 64>(s, p, zp, f32s, scratch)
+                         : launch_kind<TOK, 128>(s, p, zp, f32s, scratch);
 }
 
 }  // namespace w4
@@ -1019,7 +957,7 @@ int eesd_w4_unpack(void *cuda_stream, const eesd_w4 *m, const void *packed, size
 
 size_t eesd_w4_project_scratch_bytes(const eesd_w4 *m, int M) {
     if (w4_check(m) || M < 1 || M > EESD_MAX_ROWS) return 0;
-    return w4::frag_bytes(M, (m->K + 127) / 128, m->group);
+    return w4::frag_bytes(M, (m->K + 127) / 128);
 }
 
 int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,
@@ -1031,7 +969,7 @@ int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed
     if (a_dtype != EESD_F32 && a_dtype != EESD_BF16) return EESD_ERR_BADARG;
     const size_t es = a_dtype == EESD_F32 ? 4 : 2;
     if ((uintptr_t)A % es || ((uintptr_t)out & 3)) return EESD_ERR_BADARG;
-    if (const size_t need = w4::frag_bytes(M, l.k_blocks, m->group)) {
+    if (const size_t need = w4::frag_bytes(M, l.k_blocks)) {
         if (!scratch || ((uintptr_t)scratch & 15)) return EESD_ERR_BADARG;
         if (scratch_bytes < need) return EESD_ERR_NOMEM;
     }
@@ -1048,14 +986,15 @@ int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed
     p.M = M;
     p.a_dtype = a_dtype;
     p.vec = ((uintptr_t)A % (4 * es)) == 0 && lda % 4 == 0;
-    const int nt = w4::n_tiles(M);
+    const int tok = w4::tokens(M);
     const bool zp = m->zero_point != 0, f32s = m->scale_dtype == EESD_F32;
     unsigned char *sc = (unsigned char *)scratch;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    const cudaError_t e = nt == 1   ? w4::launch_group<1>(s, p, m->group, zp, f32s, sc)
-                          : nt == 2 ? w4::launch_group<2>(s, p, m->group, zp, f32s, sc)
-                          : nt == 3 ? w4::launch_group<3>(s, p, m->group, zp, f32s, sc)
-                                    : w4::launch_group<6>(s, p, m->group, zp, f32s, sc);
+    const cudaError_t e = tok == 1   ? w4::launch_group<1>(s, p, m->group, zp, f32s, sc)
+                          : tok == 2 ? w4::launch_group<2>(s, p, m->group, zp, f32s, sc)
+                          : tok == 4 ? w4::launch_group<4>(s, p, m->group, zp, f32s, sc)
+                          : tok == 8 ? w4::launch_group<8>(s, p, m->group, zp, f32s, sc)
+                                     : w4::launch_group<16>(s, p, m->group, zp, f32s, sc);
     if (e != cudaSuccess) return EESD_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
