@@ -498,7 +498,8 @@ int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, 
  * (0 while M * ceil(K / 128) <= 32: then it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.  The same
  * bits on every call.  An activation is taken as two fp16 terms under one power of two for the same 128 columns (128 i .. 128 i + 127) of
  * a row: it is off by at most 2^-23 of itself, and where it is below 2^-27 of the largest there by at most 2^-50 of that largest.  Products with
- * (c - z) are exact; sums are fp32 (within a group the tensor core's, which cuts off below 2^-23 of the running sum).
+ * (c - z) are exact; sums are fp32 (within a group the tensor core's, which cuts off below 2^-23 of the running sum), and no step before
+ * them overflows: a finite row gives finite results unless a sum of its terms leaves fp32's range.
  * A row of A that holds a NaN or an infinity gives NaN; the other rows are not touched by it. */
 size_t eesd_w4_project_scratch_bytes(const eesd_w4 *m, int M);
 int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int a_dtype, const void *A, int64_t lda,

@@ -436,7 +436,7 @@ __host__ __device__ constexpr int tiles(int TOK) { return TOK <= 4 ? 1 : TOK / 4
 __host__ __device__ constexpr int columns(int TOK) { return TOK <= 4 ? 2 * TOK : 8; }
 // Staged activations of 128 columns: fragments [step pair][tile][column][lane % 4][4 words], then the rows' unscales.
 __host__ __device__ constexpr int frag_size(int TOK) { return 256 * tiles(TOK) * columns(TOK); }
-__host__ __device__ constexpr int act_bytes(int TOK) { return frag_size(TOK) + (TOK <= 4 ? 16 : TOK * 4); }
+__host__ __device__ constexpr int act_bytes(int TOK) { return frag_size(TOK) + (TOK < 2 ? 16 : TOK * 8); }
 
 struct ProjArgs {
     const unsigned char *packed;
@@ -468,6 +468,8 @@ __device__ __forceinline__ float4 load_a4(const ProjArgs &p, int m, int k) {
 
 // A warp turns 128 columns of token row m (lane: columns 4 * lane .. + 3) into two fp16 terms each at dst.  The scale 2^f puts the largest
 // magnitude into [2^14, 2^15), so that no sum overflows and 28 binary orders below it are normal numbers; f stops at 126 (2^-f stays normal).
+// A group's sum is unscaled by 2^-f, of which at most 2^20 before it meets its scale (the sum is below 2^31, so nothing overflows there that stays
+// in range as a result) and the rest, 1 or more, after.
 template <int TOK>
 __device__ __forceinline__ void stage_piece(unsigned char *dst, float4 v, int m) {
     const int lane = threadIdx.x & 31;
@@ -490,8 +492,11 @@ __device__ __forceinline__ void stage_piece(unsigned char *dst, float4 v, int m)
     uint2 *act = reinterpret_cast<uint2 *>(dst) + (((step >> 1) * tiles(TOK) + (m >> 2)) * columns(TOK) * 4 + (m & 3) * 8 + t) * 2 + (step & 1);
     act[0] = make_uint2(two(hi[0], hi[2]), two(hi[1], hi[3]));
     act[8] = make_uint2(two(lo[0], lo[2]), two(lo[1], lo[3]));
-    if (lane == 0)   // (codes enter 32-fold)
-        reinterpret_cast<float *>(dst + frag_size(TOK))[m] = (bad ? __uint_as_float(0x7fc00000u) : __int_as_float((127 - f) << 23)) * 0.03125f;
+    if (lane == 0) {   // (codes enter 32-fold)
+        const int f1 = max(f, -25);
+        const float u1 = (bad ? __uint_as_float(0x7fc00000u) : __int_as_float((127 - f1) << 23)) * 0.03125f;
+        reinterpret_cast<float2 *>(dst + frag_size(TOK))[m] = make_float2(u1, __int_as_float((127 + f1 - f) << 23));
+    }
 }
 
 // the same for a whole matrix, into global memory (many token rows: staging once costs less than once per block of threads)
@@ -629,9 +634,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
             for (int slot = 0; slot < U; slot++) {
                 if (u == u1) break;
                 Unit &r = ring[slot];
-                float g[NT][4], un[NT];
+                float g[NT][4];
+                float2 un[NT];
 #pragma unroll
-                for (int n = 0; n < NT; n++) un[n] = reinterpret_cast<const float *>(bp + frag_size(TOK))[n * 4 + t];
+                for (int n = 0; n < NT; n++) un[n] = reinterpret_cast<const float2 *>(bp + frag_size(TOK))[n * 4 + t % (TOK < 4 ? TOK : 4)];
 #pragma unroll
                 for (int jp = 0; jp < 4; jp++) {   // 32 columns: two steps
                     uint4 b[NT];
@@ -668,8 +674,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
                     }
 #pragma unroll
                     for (int n = 0; n < NT; n++) {
-                        acc[n][0] = fmaf(fmaf(g[n][1], 0x1p-11f, g[n][0]) * un[n], s0, acc[n][0]);
-                        acc[n][1] = fmaf(fmaf(g[n][3], 0x1p-11f, g[n][2]) * un[n], s1, acc[n][1]);
+                        const float h0 = fmaf(g[n][1], 0x1p-11f, g[n][0]) * un[n].x, h1 = fmaf(g[n][3], 0x1p-11f, g[n][2]) * un[n].x;
+                        acc[n][0] = fmaf(h0 * s0, un[n].y, acc[n][0]);
+                        acc[n][1] = fmaf(h1 * s1, un[n].y, acc[n][1]);
                     }
                 }
                 fetch(r);
