@@ -408,9 +408,11 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed
 
 // ------------------------------------------------------------------------------------ projection
 // A block of threads (one per multiprocessor, kWarps warps) owns a run of row blocks and a slice of K; the slices of a
-// run are one cluster.  Its (row block, 128 columns) units, in storage order, are cut evenly among its warps, so the load is even
-// to one unit whatever the shape; a warp's first and last row block may be shared with its neighbours and are added up at the end.
-// Weights go straight into registers, kAhead units ahead.
+// run are one cluster.  Its (row block, 128 columns) units are cut evenly among its warps, chunk by chunk of the columns whose
+// activations fit with 16 rows, so the load is even to a unit whatever the shape and however few chunks are staged at a time; a
+// warp's first and last row block may be shared with its neighbours and are added up at the end.  Weights go straight into registers,
+// kAhead units ahead.  Where a warp's units lie is written down once for a stage (`segs`): worked out between the units, with the ring of loads
+// unrolled, it cost 8 to 15 % (instructions seldom run, each copy fetched anew).
 //
 // The products are fp16 with fp32 sums: a code enters as 32 (c - z), exactly (the nibble set into the mantissa of 1024, or of 1024 + 16 c
 // for a high one, and one fused multiply-add that takes the zero point off), an activation as two fp16 terms of 11 bits, hi and 2048 lo,
@@ -423,11 +425,14 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char *packed
 // activation to 2^-23 or 2^-31 of the largest of its 128 columns, whatever its own size.
 //
 // Measured (a graph of calls, matrices that pass the L2 cache in turn; floor: bytes at the measured copy rate):
-//   15360 x 5120, groups of 128:               M = 1 13.5 us, 4 13.8, 8 17.1, 16 23.6 (floor 6.2)
-//   27648 x 5120, groups of 64, zero points:   M = 1 21.0, 4 21.1, 8 26.2, 16 38.0 (floor 11.7)
-//   8192 x 28672, groups of 128, zero points:  M = 1 29.6 (4.1 TB/s), 4 32.5, 8 42.4, 16 62.9 (floor 18.6)
+//   15360 x 5120, groups of 128:               M = 1 13.3 us, 4 14.6, 8 17.1, 16 23.4 (floor 6.2)
+//   27648 x 5120, groups of 64, zero points:   M = 1 20.3, 4 21.3, 8 25.5, 16 38.6 (floor 11.7)
+//   8192 x 28672, groups of 128, zero points:  M = 1 30.5 (4.0 TB/s), 4 32.9, 8 40.6, 16 63.5 (floor 18.6)
 constexpr int kWarps = 16;
-template <int TOK> constexpr int kAhead = TOK == 16 ? 1 : TOK == 8 ? 2 : 4;   // units a warp's loads run ahead
+// Units a warp's loads run ahead.  Few rows need the bytes in flight (8192 x 28672, M = 1: 2, 3, 4, 5 units 32.2, 30.7, 30.4, 30.1 us; 5 are slower on short
+// matrices); with more the products leave time, and the registers are worth more (27648 x 5120, M = 8: 1, 2, 3 units 26.2, 25.4, 25.6; 15360 x
+// 5120, M = 16: 1, 2, 3 units 23.4, 23.8, 24.5).
+template <int TOK> constexpr int kAhead = TOK == 16 ? 1 : TOK == 8 ? 2 : 4;
 constexpr int kMaxRun = 32;     // row blocks of a run
 constexpr int kSmem = 227 * 1024;
 // A kernel is for up to TOK token rows (1, 2, 4, 8, 16): tiles of the matrix instruction, and columns of a tile that are kept (term j of a
@@ -444,7 +449,7 @@ struct ProjArgs {
     const unsigned char *frag;   // staged form of A (stage_kernel); null: every block of threads stages for itself
     float *out;
     size_t lda, ldo;
-    int R, K, KB, RB, M, a_dtype, vec, chunk;   // KB, RB: blocks along K, row blocks; chunk: blocks along K staged at a time
+    int R, K, KB, RB, M, a_dtype, vec, chunk, stage;   // KB, RB: blocks along K, row blocks; chunk: blocks along K of a chunk; stage: chunks staged at a time
 };
 
 __device__ __forceinline__ float4 load_a4(const ProjArgs &p, int m, int k) {
@@ -539,11 +544,13 @@ template <int N> __device__ __forceinline__ void load_once(Bytes<N> &d, const un
             asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(d.v[4 * i]), "=r"(d.v[4 * i + 1]), "=r"(d.v[4 * i + 2]), "=r"(d.v[4 * i + 3]) : "l"(p + 16 * i));
 }
 
-// shared memory: activations | partial results of shared row blocks | results
-struct Smem { int slots, outs, total; };
-__host__ __device__ inline Smem carve(int TOK, int M, int chunk, int run) {
+// shared memory: activations of `stage` chunks | the warps' segments of them | partial results of shared row blocks | results
+__host__ __device__ constexpr int segments(int stage) { return 2 * stage + kMaxRun / kWarps + 1; }   // a warp's: two shared row blocks by chunks, whole ones, the end
+struct Smem { int segs, slots, outs, total; };
+__host__ __device__ inline Smem carve(int TOK, int M, int stage, int chunk, int run) {
     Smem s;
-    s.slots = chunk * act_bytes(TOK);
+    s.segs = stage * chunk * act_bytes(TOK);
+    s.slots = s.segs + kWarps * segments(stage) * 16;
     s.outs = s.slots + kWarps * 2 * M * 64;
     s.total = s.outs + run * M * 64;
     return s;
@@ -561,78 +568,118 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
     const int splits = (int)gridDim.y, split = (int)blockIdx.y, runs = (int)gridDim.x;
     const int rb0 = (int)((long long)p.RB * blockIdx.x / runs), run = (int)((long long)p.RB * (blockIdx.x + 1) / runs) - rb0;
     const int kb0 = (int)((long long)p.KB * split / splits), kbn = (int)((long long)p.KB * (split + 1) / splits) - kb0;
-    const Smem sm = carve(TOK, p.M, p.chunk, 0);
+    const Smem sm = carve(TOK, p.M, p.stage, p.chunk, 0);
     unsigned char *act = smem;
     float *slots = reinterpret_cast<float *>(smem + sm.slots), *outs = reinterpret_cast<float *>(smem + sm.outs);
 
     if (!p.frag) pdl_wait();   // (with staged activations the launch before this one is their kernel, and the matrix is complete already)
     pdl_trigger();
 
-    for (int c0 = 0; c0 < kbn; c0 += p.chunk) {
-        const int cn = min(p.chunk, kbn - c0);
-        const int units = run * cn;
-        const int u0 = unit_of(units, warp), u1 = unit_of(units, warp + 1);
-        const int rb_first = u0 / cn;
-        int rbi = rb_first, kp = u0 - rbi * cn;
-        // loads ahead: unit fu at src, fleft units to the end of its row block
+    // The warp's row blocks: a part of `head`, if it begins inside of it, the whole ones from `first` on, a part of `last`.  Their units go one
+    // after the other, those of a shared row block chunk by chunk (the warp's share is the same part of every chunk).
+    const int head = run * warp / kWarps, first = (run * warp + kWarps - 1) / kWarps, last = run * (warp + 1) / kWarps;
+    const bool shares_last = run * (warp + 1) % kWarps != 0 && last >= first;
+    int4 *segs = reinterpret_cast<int4 *>(smem + sm.segs) + warp * segments(p.stage);
+    for (int i = tid * 4; i < kWarps * 2 * p.M * 16; i += kWarps * 128) *reinterpret_cast<float4 *>(slots + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int chunks = (kbn + p.chunk - 1) / p.chunk;
+    for (int c0 = 0; c0 < chunks; c0 += p.stage) {
+        const int c1 = min(c0 + p.stage, chunks), k0 = c0 * p.chunk, staged = min(kbn, c1 * p.chunk) - k0;
+        // Segments: runs of units in storage order, {first, from the first staged of row block 0; its block of 128 columns; units; where in
+        // shared memory the row block's sums go on: in the results where the warp has all of it, else in the warp's slot for its first or last row block}
+        {
+            const int nc = c1 - c0, nh = first != head ? nc : 0, nw = max(last - first, 0), total = nh + nw + (shares_last ? nc : 0);
+            int n = 0;
+            for (int j0 = 0; j0 < total; j0 += 32) {
+                const int j = j0 + lane, rb = j < nh ? head : min(first + j - nh, last);
+                const bool whole = j >= nh && j < nh + nw;
+                const int c = j < nh ? j : j - nh - nw;   // (of a shared one)
+                int k = 0, units = staged;
+                if (!whole) {
+                    const int cn = min(p.chunk, kbn - (c0 + c) * p.chunk), lo = max(unit_of(run * cn, warp) - rb * cn, 0);
+                    units = min(unit_of(run * cn, warp + 1) - rb * cn, cn) - lo;
+                    k = c * p.chunk + lo;
+                }
+                const bool any = j < total && units > 0;
+                const uint32_t those = __ballot_sync(0xffffffffu, any);
+                if (any) segs[n + __popc(those & ((1u << lane) - 1))] = make_int4(rb * p.KB + k, k, units, (whole ? sm.outs / 4 + rb * p.M * 16 : sm.slots / 4 + (warp * 2 + (rb != head)) * p.M * 16));
+                n += __popc(those);
+            }
+            if (lane == 0) segs[n] = make_int4(0, 0, 0, 0);
+            __syncwarp();
+        }
         struct Unit {
             Bytes<16> w[2];
             Bytes<kScaleBytes> s;
             Bytes<2 * NG> z;
         } ring[U];
-        const unsigned char *src = p.packed + ((size_t)(rb0 + rbi) * p.KB + kb0 + c0 + kp) * kRecord;
-        const size_t jump = (size_t)(p.KB - cn) * kRecord;
-        int fleft = cn - kp, fu = u0;
+        // loads ahead
+        const unsigned char *base = p.packed + ((size_t)rb0 * p.KB + kb0 + k0) * kRecord, *src;
+        const int4 *fnext = segs;
+        int fleft;
+        auto follow = [&]() {
+            const int4 e = *fnext++;
+            src = base + (size_t)e.x * kRecord;
+            fleft = e.z;
+        };
+        follow();
         auto fetch = [&](Unit &r) {
-            if (fu < u1) {
+            if (fleft > 0) {
                 load_once(r.w[0], src + lane * 16);
                 load_once(r.w[1], src + 512 + lane * 16);
                 load_once(r.s, src + 1024 + g8 * kScaleBytes);
                 if (ZP) load_once(r.z, src + kZeros + g8 * 2 * NG);
             }
-            fu++;
             src += kRecord;
-            if (--fleft == 0) { fleft = cn; src += jump; }
+            if (--fleft == 0) follow();   // (after the last segment it goes on below 0)
         };
 #pragma unroll
         for (int s = 0; s < U; s++) fetch(ring[s]);
 
-        if (c0) __syncthreads();   // the previous chunk's activations are used up
+        if (c0) __syncthreads();   // the activations staged before are used up
         if (p.frag) {
             if (!c0) pdl_wait();
-            const unsigned char *f = p.frag + (size_t)(kb0 + c0) * kAct;
+            const unsigned char *from = p.frag + (size_t)(kb0 + k0) * kAct;
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(act);
-            for (int i = tid * 16; i < cn * kAct; i += kWarps * 512) copy16(at + i, f + i);
+            for (int i = tid * 16; i < staged * kAct; i += kWarps * 512) copy16(at + i, from + i);
             asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         } else {
             constexpr int kBatch = 4;
-            for (int it0 = warp; it0 < p.M * cn; it0 += kWarps * kBatch) {
+            for (int it0 = warp; it0 < p.M * staged; it0 += kWarps * kBatch) {
                 float4 v[kBatch];
 #pragma unroll
                 for (int i = 0; i < kBatch; i++) {
-                    const int it = it0 + i * kWarps, m = it / cn, k = (kb0 + c0 + it - m * cn) * 128 + lane * 4;
-                    v[i] = it < p.M * cn ? load_a4(p, m, k) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const int it = it0 + i * kWarps, m = it / staged, k = (kb0 + k0 + it - m * staged) * 128 + lane * 4;
+                    v[i] = it < p.M * staged ? load_a4(p, m, k) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
 #pragma unroll
                 for (int i = 0; i < kBatch; i++) {
-                    const int it = it0 + i * kWarps, m = it / cn;
-                    if (it < p.M * cn) stage_piece<TOK>(act + (it - m * cn) * kAct, v[i], m);
+                    const int it = it0 + i * kWarps, m = it / staged;
+                    if (it < p.M * staged) stage_piece<TOK>(act + (it - m * staged) * kAct, v[i], m);
                 }
             }
         }
         __syncthreads();
 
         float acc[NT][2];   // token row 4 n + t, weight rows g8 and g8 + 8
-#pragma unroll
-        for (int n = 0; n < NT; n++) acc[n][0] = acc[n][1] = 0.f;
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
         uint32_t ones;
         asm volatile("mov.b32 %0, 0x64006400;" : "=r"(ones));
-        const unsigned char *bp = act + kp * kAct;
-        for (int u = u0; u < u1;) {
+        float *sums = reinterpret_cast<float *>(smem) + t * 16 + g8;
+        auto resume = [&](int d) {
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) acc[n][i] = c0 && n * 4 + t < p.M ? sums[d + n * 64 + i * 8] : 0.f;
+        };
+        const int4 *next = segs;
+        int4 e = *next;
+        resume(e.w);
+        int left = e.z;
+        const unsigned char *bp = act + e.y * kAct;
+        while (left) {
 #pragma unroll
             for (int slot = 0; slot < U; slot++) {
-                if (u == u1) break;
+                if (!left) break;
                 Unit &r = ring[slot];
                 float g[NT][4];
                 float2 un[NT];
@@ -680,52 +727,41 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
                     }
                 }
                 fetch(r);
-                u++;
                 bp += kAct;
-                if (++kp == cn || u == u1) {
-                    // the row block's sums: to the results where the warp had all of it, else to the warp's slot for its first or last row block
-                    const bool first = rbi == rb_first, last = u == u1;
-                    float *d = first ? slots + warp * 2 * p.M * 16 : last ? slots + (warp * 2 + 1) * p.M * 16 : outs + rbi * p.M * 16;
-                    const bool add = !first && !last && c0;
+                if (--left == 0) {
+                    const int d = next->w;
+                    e = *++next;
+                    left = e.z;
+                    bp = act + e.y * kAct;
+                    if (e.w != d) {   // (0 at the end)
 #pragma unroll
-                    for (int n = 0; n < NT; n++) {
-                        const int m = n * 4 + t;
+                        for (int n = 0; n < NT; n++)
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            float *o = d + m * 16 + g8 + i * 8;
-                            if (m < p.M) *o = add ? *o + acc[n][i] : acc[n][i];
-                            acc[n][i] = 0.f;
-                        }
+                            for (int i = 0; i < 2; i++)
+                                if (n * 4 + t < p.M) sums[d + n * 64 + i * 8] = acc[n][i];
+                        resume(e.w);
                     }
-                    kp = 0;
-                    bp = act;
-                    rbi++;
                 }
             }
         }
-        __syncthreads();
-        // shared row blocks: the warps' parts in order
-        for (int i = warp; i < run; i += kWarps) {
-            const int a0 = i * cn, a1 = a0 + cn;
-            int w = (int)(((long long)a0 * kWarps) / units);   // next to the warp that holds unit a0
-            while (unit_of(units, w) > a0) w--;
-            while (unit_of(units, w + 1) <= a0) w++;
-            const int b0 = unit_of(units, w), b1 = unit_of(units, w + 1);
-            if (b0 < a0 && b1 > a1) continue;                  // inside one warp's range: already in the results
-            float v[EESD_MAX_ROWS / 2];
+    }
+    __syncthreads();
+    // shared row blocks: the warps' parts in order
+    for (int i = warp; i < run; i += kWarps) {
+        int x = kWarps * i / run;                            // the last warp that begins at or before the row block
+        if (kWarps * (i + 1) <= run * (x + 1)) continue;     // it has the whole: already in the results
+        float v[EESD_MAX_ROWS / 2];
 #pragma unroll
-            for (int j = 0; j < EESD_MAX_ROWS / 2; j++) v[j] = c0 && j * 32 + lane < p.M * 16 ? outs[i * p.M * 16 + j * 32 + lane] : 0.f;
-            for (int x0 = b0; x0 < a1; w++, x0 = unit_of(units, w)) {
-                if (unit_of(units, w + 1) == x0) continue;     // a warp without units
-                const float *part = slots + (w * 2 + (x0 < a0)) * p.M * 16 + lane;   // its first row block, or (begun before this one) its last
-#pragma unroll
-                for (int j = 0; j < EESD_MAX_ROWS / 2; j++)
-                    if (j * 32 + lane < p.M * 16) v[j] += part[j * 32];
-            }
+        for (int j = 0; j < EESD_MAX_ROWS / 2; j++) v[j] = 0.f;
+        for (; x < kWarps && run * x < kWarps * (i + 1); x++) {
+            const float *part = slots + (x * 2 + (i != run * x / kWarps)) * p.M * 16 + lane;
 #pragma unroll
             for (int j = 0; j < EESD_MAX_ROWS / 2; j++)
-                if (j * 32 + lane < p.M * 16) outs[i * p.M * 16 + j * 32 + lane] = v[j];
+                if (j * 32 + lane < p.M * 16) v[j] += part[j * 32];
         }
+#pragma unroll
+        for (int j = 0; j < EESD_MAX_ROWS / 2; j++)
+            if (j * 32 + lane < p.M * 16) outs[i * p.M * 16 + j * 32 + lane] = v[j];
     }
 
     // the slices of K are one cluster: every block adds up its share of the row blocks over all of them, in slice order
@@ -745,14 +781,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) project_kernel(const ProjArgs 
     if (splits > 1) cg::this_cluster().sync();   // nobody leaves while its results are still being read
 }
 
-// How a projection is cut: `splits` slices of K (a cluster of 1, 2, 4 or 8 blocks), `runs` runs of row blocks, `chunk` blocks of
-// 128 columns staged at a time.
-// How the matrix is cut: slices of K (a cluster's blocks), runs of row blocks, columns staged at a time.  The cost is in units of 16 x
-// 128 codes a warp streams.  Forced to 1, 2, 4 or 8 slices, 5120 to 28672 columns and 5 to 16 rows never ran more than 1 % faster than the
-// choice made here, and up to twice slower (5 rows, 8 slices of 27648 x 5120: 49.8 against 25.7 us).
-struct Cut { int splits, runs, chunk, smem; };
+// How a matrix is cut: `splits` slices of K (a cluster of 1, 2, 4 or 8 blocks), `runs` runs of row blocks (of at most `run`), chunks of `chunk`
+// blocks of 128 columns.  The order of every addition follows from it, so it looks at the matrix alone: a token row has the same
+// result however many rows go with it.  A chunk is what fits with 16 rows; fewer rows stage several at a time.  Forced to 1, 2, 4 or 8 slices, 12
+// matrices from 1024 x 4096 to 128256 x 8192 with 1, 4 and 16 rows ran at most 5 % faster than with the choice made here (most of them
+// none), and up to twice slower.
+struct Cut { int splits, runs, run, chunk; };
 
-inline Cut pick_cut(int TOK, int M, int RB, int KB) {
+inline int chunks_staged(int TOK, int M, const Cut &c, int KB) {
+    const int slice = (KB + c.splits - 1) / c.splits, chunks = (slice + c.chunk - 1) / c.chunk;
+    int most = 1;
+    while (most < chunks && carve(TOK, M, most + 1, c.chunk, c.run).total <= kSmem) most++;
+    const int stages = (chunks + most - 1) / most;
+    return (chunks + stages - 1) / stages;
+}
+
+// The cost estimates the time of 1 row and of 16 rows together, about in microseconds: a unit of 16 x 128 codes a warp (0.5 and 1), staging 16
+// rows by block and by chunk, joining a cluster.
+inline Cut pick_cut(int RB, int KB) {
     Cut best = {};
     double cost = 1e300;
     for (int s = 1; s <= 8; s *= 2) {
@@ -761,27 +807,24 @@ inline Cut pick_cut(int TOK, int M, int RB, int KB) {
         const int waves = (RB + clusters * kMaxRun - 1) / (clusters * kMaxRun);
         const int runs = RB < clusters * waves ? RB : clusters * waves;
         const int run = (RB + runs - 1) / runs, slice = (KB + s - 1) / s;
-        const Smem fixed = carve(TOK, M, 0, run);
-        int chunk = (kSmem - fixed.total) / act_bytes(TOK);
-        if (chunk < 1) continue;
+        int chunk = (kSmem - carve(16, 16, 1, 0, run).total) / act_bytes(16);
         const int n_chunks = (slice + chunk - 1) / chunk;
         chunk = (slice + n_chunks - 1) / n_chunks;
-        // units a warp streams, plus what staging a chunk and joining a cluster take in units of time
-        const double c = (double)waves * (run * (double)slice / kWarps + n_chunks * (4.0 + 0.02 * M * chunk) + (s > 1 ? 2.0 + 0.5 * s : 0.0));
+        const double c = waves * (1.5 * run * slice / kWarps + 0.07 * slice + 0.6 * n_chunks + (s > 1 ? 0.8 + 0.09 * run : 0.0));
         if (c < cost) {
             cost = c;
-            best = {s, runs, chunk, carve(TOK, M, chunk, run).total};
+            best = {s, runs, run, chunk};
         }
     }
     return best;
 }
 
-// Staged activations: bytes of scratch (0: each block of threads stages for itself).  A launch of its own costs about a microsecond, staging in every
-// block 0.1 us for 4 pieces of 128 columns: 1024 x 256 with 16 rows (32 pieces) 4.1 us in the blocks against 4.9 by a launch, 15360 x
-// 5120 with 4 rows (160 pieces) 16.2 against 13.1.
+// Staged activations: bytes of scratch, and whether a launch of its own stages them there.  That launch costs about 0.9 us, staging in every block 0.3 us for
+// 16 pieces of 128 columns: in the blocks and by a launch 1024 x 256 with 16 rows (32 pieces a block) 5.5 and 6.0 us, 15360 x 5120 with 2 rows
+// (40) 13.7 and 14.3, with 4 rows (80) 15.1 and 14.6, 1024 x 1024 with 16 rows 8.0 and 6.5.
 inline int tokens(int M) { return M <= 2 ? M : M <= 4 ? 4 : M <= 8 ? 8 : 16; }
-inline bool stage_first(int M, int KB) { return M * KB > 32; }
-inline size_t frag_bytes(int M, int KB) { return !stage_first(M, KB) ? 0 : (size_t)KB * act_bytes(tokens(M)); }
+inline size_t frag_bytes(int M, int KB) { return M * KB <= 32 ? 0 : (size_t)KB * act_bytes(tokens(M)); }
+inline bool stage_first(int M, int slice) { return M * slice > 48; }   // (never where there is no scratch)
 
 template <int TOK, int G, bool ZP, bool F32S>
 cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
@@ -797,18 +840,18 @@ cudaError_t launch_project(cudaStream_t s, ProjArgs p, unsigned char *scratch) {
             if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
         }
     }
-    const Cut cut = pick_cut(TOK, p.M, p.RB, p.KB);
-    if (!cut.runs) return cudaErrorInvalidConfiguration;
+    const Cut cut = pick_cut(p.RB, p.KB);
     p.chunk = cut.chunk;
+    p.stage = chunks_staged(TOK, p.M, cut, p.KB);
     p.frag = nullptr;
-    if (stage_first(p.M, p.KB)) {
+    if (stage_first(p.M, (p.KB + cut.splits - 1) / cut.splits)) {
         launch_k(stage_kernel<TOK>, dim3((p.KB * p.M + 7) / 8), dim3(256), 0, s, pdl_enabled(), p, scratch);
         p.frag = scratch;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(cut.runs, cut.splits);
     cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = cut.smem;
+    cfg.dynamicSmemBytes = carve(TOK, p.M, p.stage, p.chunk, cut.run).total;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int na = 0;

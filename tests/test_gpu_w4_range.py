@@ -111,3 +111,18 @@ def test_nothing_overflows_before_the_scale():
                 bound = bound_of(A[i:i + 1], value, group, True)[0] + scales.double().sum(1) * 2.0 ** -149   # (a group's sum below 2^-126)
                 assert bool(out.isfinite().all()), (name, group, len(rows))
                 assert bool(((out - ref).abs() <= bound).all()), (name, group, len(rows), float(((out - ref).abs() / bound).max()))
+
+
+@pytest.mark.parametrize("R,K,group", [(40, 300, 32), (300, 9000, 32), (4100, 5120, 64), (1000, 13824, 128), (64, 28672, 128), (8192, 28672, 128)])
+def test_a_row_does_not_depend_on_the_rows_beside_it(R, K, group):
+    g = torch.Generator(device="cuda").manual_seed(R)
+    G = -(-K // group)
+    m, _ = matrix(torch.randint(0, 16, (R, K), generator=g, device="cuda", dtype=torch.uint8), 0.01 * torch.exp(torch.randn(R, G, generator=g, device="cuda")),
+                  torch.randint(0, 16, (R, G), generator=g, device="cuda", dtype=torch.uint8), group)
+    A = torch.randn(16, K, generator=g, device="cuda")
+    alone = torch.cat([eesd.project_rows(A[i:i + 1], m) for i in range(16)])
+    for M in range(2, 17):
+        assert torch.equal(eesd.project_rows(A[:M], m), alone[:M]), M
+        assert torch.equal(eesd.project_rows(A[16 - M:], m), alone[16 - M:]), M
+    order = torch.randperm(16, generator=g, device="cuda")
+    assert torch.equal(eesd.project_rows(A[order], m), alone[order])
