@@ -46,12 +46,19 @@ __device__ __forceinline__ float round_scale(float x, float by, int scale_dtype)
     if (__fmaf_rn(-f, by, x) != 0.f) f = __uint_as_float(__float_as_uint(f) | 1u);
     return __bfloat162float(__float2bfloat16_rn(f));
 }
-__device__ __forceinline__ float round_scale(double x, double by, int scale_dtype) {   // (x: a difference that fp32 does not hold)
-    x /= by;
-    if (scale_dtype == EESD_F32) return __double2float_rn(x);
-    float f = __double2float_rz(x);
-    if ((double)f != x) f = __uint_as_float(__float_as_uint(f) | 1u);
-    return __bfloat162float(__float2bfloat16_rn(f));
+// (hi - lo) / 15 with hi >= 0 >= lo, likewise.  The difference may take more than the 53 bits of a double and its quotient more again: both
+// remainders are exact, and they tell the side where the rounded quotient lies on the border between two scales (the true one lies on
+// the same side of a border as the rounded one, or that is the border itself, since rounding keeps order and a border times 15 is a double).
+__device__ __forceinline__ float round_range(float hi, float lo, int scale_dtype) {
+    const double a = fmax((double)hi, -(double)lo), b = fmin((double)hi, -(double)lo);
+    const double sum = a + b, lost = b - (sum - a);
+    const double q = sum / 15.0, rest = fma(-q, 15.0, sum) + lost;
+    const uint32_t step = scale_dtype == EESD_F32 ? 1u : 0x10000u;
+    const uint32_t below = __float_as_uint(__double2float_rz(q)) & ~(step - 1u);   // the scale at or below q
+    const double at = __uint_as_float(below), next = __uint_as_float(below + step);
+    double side = q - (at + next) * 0.5;
+    if (side == 0.0) side = rest;
+    return __uint_as_float(side > 0.0 || (side == 0.0 && (below & step)) ? below + step : below);
 }
 
 // nearest integer (ties to even) to the exact quotient x / s.  The rounded quotient can only be off by one, and only when x / s
@@ -205,7 +212,7 @@ __global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 4 : 2) quantize_kernel(
             hi[i] = max_nan(hi[i], 0.f);
             lo[i] = min_nan(lo[i], 0.f);
         }
-        float s = ZP ? round_scale((double)hi[i] - (double)lo[i], 15.0, q.scale_dtype) : round_scale(hi[i], 7.f, q.scale_dtype);
+        float s = ZP ? round_range(hi[i], lo[i], q.scale_dtype) : round_scale(hi[i], 7.f, q.scale_dtype);
         // a NaN or infinity among the weights: the whole group reads back as NaN
         if (!(hi[i] <= 3.402823466e38f) || (ZP && !(lo[i] >= -3.402823466e38f))) s = __uint_as_float(0x7fc00000u);
         const bool fine = s >= 0x1p-100f;
