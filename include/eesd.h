@@ -516,6 +516,7 @@ int eesd_w4_project_rows(void *cuda_stream, const eesd_w4 *m, const void *packed
  * logit was (NaN and infinities included).  A row whose mask leaves nothing is -inf throughout; eesd_sample_rows and
  * eesd_accept_resample answer -1 for a row without any logit above -inf. */
 #define EESD_MAX_RULE_ROWS 256
+#define EESD_MAX_RULE_LENGTH (1 << 30)   /* of V, history_len and n_bias (UNSUPPORTED beyond) */
 typedef struct eesd_logit_rules {              /* device pointers */
     const int32_t *history;                    /* [B] rows of history_len tokens, history_stride apart          */
     int64_t history_stride;

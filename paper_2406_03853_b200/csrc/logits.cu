@@ -282,6 +282,8 @@ extern "C" int eesd_process_logits(void *cuda_stream, const float *logits, int64
     if (r->drafted && r->drafted_stride < rows - 1) return EESD_ERR_BADARG;
     if (r->n_bias < 0 || (r->n_bias > 0 && (!r->bias_start || !r->bias_ids || !r->bias_values))) return EESD_ERR_BADARG;
     if (r->mask && r->mask_stride < ((int64_t)V + 31) / 32) return EESD_ERR_BADARG;
+    // (the kernel's 32-bit indices pass an end by less than a block's columns, or its threads' tokens)
+    if (V > EESD_MAX_RULE_LENGTH || (r->history && r->history_len > EESD_MAX_RULE_LENGTH) || r->n_bias > EESD_MAX_RULE_LENGTH) return EESD_ERR_UNSUPPORTED;
     const long long n_rows = (long long)B * rows;
     if (n_rows > 0x7fffffffLL) return EESD_ERR_UNSUPPORTED;
     // in place means exactly in place; any other overlap would read rows that are already processed

@@ -1,10 +1,13 @@
 """Logit rules: the repetition penalty over the whole range of fp32.  One rounding of a quotient or product of two fp32 numbers, so results are
 compared for equality with numpy's."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2406_03853_b200 as eesd
+from paper_2406_03853_b200 import binding as b
 
 
 @pytest.mark.gpu
@@ -28,3 +31,25 @@ def test_quotients_of_every_size_are_rounded_once(V):
     got = eesd.process_logits(torch.from_numpy(x).cuda(), r).cpu().numpy()
     same = (got == want) | (np.isnan(got) & np.isnan(want))
     assert same.all(), [(x[tuple(i)], rhos[i[0]], got[tuple(i)], want[tuple(i)]) for i in np.argwhere(~same)[:5]]
+
+
+def refused(**kw):
+    """eesd_process_logits with addresses that are never dereferenced: what it answers on the host"""
+    r = b.RulesStruct()
+    a = dict(V=8, li=None, B=1, rows=1)
+    for k, v in kw.items():
+        if k in a:
+            a[k] = v
+        else:
+            setattr(r, k, v)
+    ld = a["V"] if a["li"] is None else a["li"]
+    return eesd.lib().eesd_process_logits(None, 1 << 20, ld, 1 << 45, ld, a["B"], a["rows"], a["V"], C.addressof(r))
+
+
+def test_lengths_that_32_bits_do_not_count_past_are_refused():
+    # a block's column, token and bias indices go a few thousand past the end
+    far = 2 ** 31 - 1
+    for n in (2 ** 30 + 1, far - 4096, far):
+        assert refused(V=n) == -8
+        assert refused(history=1 << 20, history_len=n, history_stride=n, repetition=1 << 20) == -8
+        assert refused(bias_start=1 << 20, bias_ids=1 << 20, bias_values=1 << 20, n_bias=n) == -8
