@@ -532,8 +532,8 @@ typedef struct eesd_logit_rules {              /* device pointers */
     const int32_t *mask;                       /* [B * rows] rows of words, mask_stride apart; bit v % 32 of word v / 32: allowed */
     int64_t mask_stride;
 } eesd_logit_rules;
-/* logits: B * rows rows of V fp32, ld_logits apart; out likewise.  out may be logits (same ld); any other overlap is BADARG.
- * rows <= EESD_MAX_RULE_ROWS.  Asynchronous, one launch, no scratch. */
+/* logits: B * rows rows of V fp32, ld_logits apart; out likewise.  out may be logits (same ld); any other overlap of the two is
+ * BADARG, and so is an address that is not a multiple of 4; out overlaps none of the rules' lists.  rows <= EESD_MAX_RULE_ROWS.  Asynchronous, one launch, no scratch. */
 int eesd_process_logits(void *cuda_stream, const float *logits, int64_t ld_logits, float *out, int64_t ld_out, int B, int rows, int V,
                         const eesd_logit_rules *rules);
 

@@ -277,7 +277,9 @@ using namespace eesd;
 extern "C" int eesd_process_logits(void *cuda_stream, const float *logits, int64_t ld_logits, float *out, int64_t ld_out, int B, int rows, int V,
                                    const eesd_logit_rules *r) {
     if (!logits || !out || !r || B < 1 || rows < 1 || rows > EESD_MAX_RULE_ROWS || V < 1 || ld_logits < V || ld_out < V) return EESD_ERR_BADARG;
-    if (((uintptr_t)logits | (uintptr_t)out) & 3) return EESD_ERR_BADARG;
+    const void *const words[] = {logits, out, r->history, r->n_history, r->n_prompt, r->drafted, r->repetition, r->frequency, r->presence, r->bias_start, r->bias_ids, r->bias_values, r->mask};
+    for (const void *p : words)
+        if ((uintptr_t)p & 3) return EESD_ERR_BADARG;
     if (r->history && (r->history_len < 0 || r->history_stride < r->history_len)) return EESD_ERR_BADARG;
     if (r->drafted && r->drafted_stride < rows - 1) return EESD_ERR_BADARG;
     if (r->n_bias < 0 || (r->n_bias > 0 && (!r->bias_start || !r->bias_ids || !r->bias_values))) return EESD_ERR_BADARG;

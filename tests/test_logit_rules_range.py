@@ -53,3 +53,16 @@ def test_lengths_that_32_bits_do_not_count_past_are_refused():
         assert refused(V=n) == -8
         assert refused(history=1 << 20, history_len=n, history_stride=n, repetition=1 << 20) == -8
         assert refused(bias_start=1 << 20, bias_ids=1 << 20, bias_values=1 << 20, n_bias=n) == -8
+
+
+def test_misaligned_lists_are_refused():
+    at = (1 << 20) + 2
+    assert refused(history=at, history_len=4, history_stride=4, repetition=1 << 20) == -1
+    for name in ("n_history", "n_prompt"):
+        assert refused(history=1 << 20, history_len=4, history_stride=4, repetition=1 << 20, **{name: at}) == -1
+    for name in ("repetition", "frequency", "presence"):
+        assert refused(history=1 << 20, history_len=4, history_stride=4, **{name: at}) == -1
+    assert refused(rows=3, drafted=at, drafted_stride=2, repetition=1 << 20) == -1
+    for name in ("bias_start", "bias_ids", "bias_values"):
+        assert refused(n_bias=3, **{**dict(bias_start=1 << 20, bias_ids=1 << 20, bias_values=1 << 20), name: at}) == -1
+    assert refused(mask=at, mask_stride=1) == -1
