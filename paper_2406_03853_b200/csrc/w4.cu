@@ -169,7 +169,7 @@ template <int G, Extreme E> __device__ __forceinline__ void row_extremes(const F
 // across a half: the exact remainder (one fused multiply-add) tells, and a row where some remainder reaches half a scale is put
 // right (common only as ties: bf16 weights over bf16 scales, 3 us of the 37).  Scales below 2^-100, whose reciprocal would not
 // do, are left to nearest_quotient at the end.
-// Measured, 5120 x 13824: fp32 weights 46 to 55 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 34 to 49 us
+// Measured, 5120 x 13824: fp32 weights 45 to 56 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 34 to 52 us
 // (floor 27: bound by issue, 14 instructions for a lane's weight, 2.8 of 4 a cycle with 3 blocks a multiprocessor; 4 blocks took it from
 // 40 to 37 us with groups of 128 and bf16 scales).  Columns 16 to a lane (one lane a scale, no exchange) reads in
 // pieces of 32 bytes and took 167 to 184 us.
