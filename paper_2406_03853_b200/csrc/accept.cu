@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kAccThreads) accept_kernel(const float *p_logi
         if (K <= EESD_MAX_ROWS) {
             while (j < K && s_ok[j]) j++;
         } else if (greedy) {
-            while (j < K && x[j] == ld_stat(&st[j]).arg) j++;
+            while (j < K && x[j] >= 0 && x[j] < V && x[j] == ld_stat(&st[j]).arg) j++;   // (kNoToken is no token either)
         } else {
             for (; j < K; j++) {
                 const int t = x[j];
