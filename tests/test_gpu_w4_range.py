@@ -126,3 +126,15 @@ def test_a_row_does_not_depend_on_the_rows_beside_it(R, K, group):
         assert torch.equal(eesd.project_rows(A[16 - M:], m), alone[16 - M:]), M
     order = torch.randperm(16, generator=g, device="cuda")
     assert torch.equal(eesd.project_rows(A[order], m), alone[order])
+
+
+@pytest.mark.parametrize("R,K,group", [(80011, 200, 32), (200000, 64, 64)])
+def test_more_row_blocks_than_one_round_of_blocks_takes(R, K, group):
+    g = torch.Generator(device="cuda").manual_seed(K)
+    G = -(-K // group)
+    m, value = matrix(torch.randint(0, 16, (R, K), generator=g, device="cuda", dtype=torch.uint8), 0.01 * torch.exp(torch.randn(R, G, generator=g, device="cuda")), None, group)
+    A = torch.randn(16, K, generator=g, device="cuda")
+    for M in (1, 4, 7, 16):
+        out = eesd.project_rows(A[:M], m)
+        off = (out.double() - A[:M].double() @ value.t()).abs() / bound_of(A[:M], value, group, True)
+        assert float(off.max()) <= 1, (M, float(off.max()))
