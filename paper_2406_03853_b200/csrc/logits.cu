@@ -15,9 +15,9 @@
 // per sequence and not once per row; a draft adds to the count of the one thread that owns its column.
 //
 // Measured (a graph of calls over inputs that pass the L2 cache in turn; floor: bytes at the measured copy rate):
-//   64 sequences x 17 rows x 32000: mask alone 50 us, penalties alone 57, all rules 69 (floor 43)
-//   64 x 1 x 128256, all rules: 27.8 (floor 10.2: every block counts 2048 tokens for 4096 columns of one row)
-//   16 x 5 x 50257, biases and mask: 12.4 (floor 5.0);  8 x 2 x 32000, all rules: 4.7;  1 x 1 x 32000, penalties: 3.1 (latency)
+//   64 sequences x 17 rows x 32000: mask alone 51 us, penalties alone 57, all rules 69 (floor 43)
+//   64 x 1 x 128256, all rules: 28.1 (floor 10.2: every block counts 2048 tokens for 4096 columns of one row)
+//   16 x 5 x 50257, biases and mask: 12.3 (floor 5.0);  8 x 2 x 32000, all rules: 4.7;  1 x 1 x 32000, penalties: 3.1 (latency)
 // With everything on, the one round of blocks counts first (about 7 us of dependent reads) and then streams, with two items a
 // thread in flight in 64 registers; a ring of 3 spills (77 us), 3 blocks a multiprocessor make two rounds (107), and a ring of 4 in shared memory
 // takes the L1 cache that masks and drafts are read through (80).
@@ -309,8 +309,10 @@ extern "C" int eesd_process_logits(void *cuda_stream, const float *logits, int64
     a.spans_per_block = 1;
     a.row_split = 1;
     // Few sequences split their rows among blocks until the machine is full (8 x 17 x 32000: 15.3 us, 17.2 without); many take
-    // several spans a block, so that a sequence's tokens are counted by fewer blocks (64 x 1 x 128256: 1, 2, 4 spans 51, 34, 28 us; 16 x 5 x
-    // 50257, which 4 spans would leave half the machine for: 16.1, 14.9, 21.8).
+    // several spans a block, so that a sequence's tokens are counted by fewer blocks (64 x 1 x 128256: 1, 2, 4 spans 51, 34, 28 us), as long as
+    // they fill most of the machine.  On either side of the border, 1, 2, 4 spans: 12 x 5 x 50257 10.0, 11.3, 16.9; 15 x 5 x 50257 12.3, 12.2, 17.5; 17 x 5
+    // x 50257 12.9, 12.6, 18.1; 24 x 5 x 32000 14.4, 13.6, 19.1; 26 x 5 x 32000 14.8, 13.7, 19.3; 49 x 4 x 32000 19.9, 20.6, 19.3; 51 x 4 x 32000 20.4,
+    // 20.9, 19.5.
     while (a.row_split * 2 <= rows && (long long)B * a.spans * a.row_split < 4 * 148) a.row_split *= 2;
     if (a.row_split == 1)
         while (a.spans_per_block < 4 && (long long)B * a.spans / (a.spans_per_block * 2) >= 400) a.spans_per_block *= 2;

@@ -170,8 +170,8 @@ template <int G, Extreme E> __device__ __forceinline__ void row_extremes(const F
 // right (common only as ties: bf16 weights over bf16 scales, 3 us of the 37).  Scales below 2^-100, whose reciprocal would not
 // do, are left to nearest_quotient at the end.
 // Measured, 5120 x 13824: fp32 weights 45 to 56 us (floor 48.5: bound by memory, with zero points by issue), bf16 weights 34 to 52 us
-// (floor 27: bound by issue, 14 instructions for a lane's weight, 2.8 of 4 a cycle with 3 blocks a multiprocessor; 4 blocks took it from
-// 40 to 37 us with groups of 128 and bf16 scales).  Columns 16 to a lane (one lane a scale, no exchange) reads in
+// (floor 27: bound by issue, 14 instructions for a lane's weight, 3.1 of 4 a cycle with 4 blocks a multiprocessor, although most of these kernels
+// spill a few registers then; 3 blocks 40 us, 4 blocks 37, with groups of 128 and bf16 scales).  Columns 16 to a lane (one lane a scale, no exchange) reads in
 // pieces of 32 bytes and took 167 to 184 us.
 template <typename WT, int G, bool ZP>
 __global__ void __launch_bounds__(256, sizeof(WT) == 2 ? 4 : 2) quantize_kernel(const WT *W, size_t ldw, unsigned char *packed, const Geom q, size_t jobs, bool vec) {
