@@ -494,7 +494,7 @@ int eesd_w4_unpack(void *cuda_stream, const eesd_w4 *m, const void *packed, size
 int eesd_w4_dequantize(void *cuda_stream, const eesd_w4 *m, const void *packed, size_t packed_bytes, int out_dtype, void *out, int64_t ldo);
 
 /* eesd_project_rows for a 4-bit matrix: out[m][r] = sum_k A[m][k] * value(r, k) for M <= EESD_MAX_ROWS rows.  A: M rows of a_dtype,
- * lda >= K elements apart; out: M fp32 rows, ldo >= R apart.  scratch: device, 16-byte aligned, eesd_w4_project_scratch_bytes bytes
+ * lda >= K elements apart; out: M fp32 rows, ldo >= R apart, that overlap no input.  scratch: device, 16-byte aligned, eesd_w4_project_scratch_bytes bytes
  * (0 while M * ceil(K / 128) <= 32: then it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.  A
  * row's result has the same bits on every call, however many rows and whichever go with it.  An activation is taken as two fp16 terms under one power of two for the same 128 columns (128 i .. 128 i + 127) of
  * a row: it is off by at most 2^-23 of itself, and where it is below 2^-27 of the largest there by at most 2^-50 of that largest.  Products with
