@@ -537,6 +537,83 @@ typedef struct eesd_logit_rules {              /* device pointers */
 int eesd_process_logits(void *cuda_stream, const float *logits, int64_t ld_logits, float *out, int64_t ld_out, int B, int rows, int V,
                         const eesd_logit_rules *rules);
 
+/* ---- key / value cache in 4 bits ---------------------------------------------------------------------
+ * A paged cache of keys and values for callers that assemble a round themselves: rows are quantised as they are written, and attention
+ * reads the codes.  A head's head_dim values of a token are held in groups of `group` neighbours, each with a scale and a zero point:
+ *   value = (c - z) * s,  c = 0..15, z = 0..15,  s bf16.
+ * The paper stores 16-bit caches; this is an extension for contexts (or batches) whose cache bounds a pass. */
+typedef struct eesd_kv4 {
+    int32_t n_pages;      /* pages of the pool                                                     */
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* 64 or 128 (UNSUPPORTED otherwise)                                     */
+    int32_t page_tokens;  /* 16, 32, 64 or 128 (UNSUPPORTED otherwise)                             */
+    int32_t group;        /* 32, 64 or 128, at most head_dim (UNSUPPORTED otherwise)               */
+} eesd_kv4;
+
+/* The one device buffer (16-byte aligned) that holds the pool: [n_pages][n_kv_heads][page_tokens / 16] tiles of 16 tokens, tile_bytes each.
+ * In a tile, with D = head_dim and G = D / group:
+ *   at 0         keys, D / 2 bytes a token: nibble i (0..7, low first) of the 32-bit word (token, t, j) at token * D / 2 + t * D / 8 + j * 4 is
+ *                dimension 32 j + 8 t + i
+ *   at v_codes   values: nibble i of the word ((w * 8 + g) * 4 + t) * 4 + 2 h + e is dimension 64 w + 8 i + g of token 8 h + 2 t + e
+ *   at scales    [G][16 tokens] words: the key's scale (bf16) in the low half, the value's in the high one
+ *   at k_zeros   [G][16 tokens] bytes, the keys' zero points;  at v_zeros  the values'. */
+typedef struct eesd_kv4_layout {
+    size_t v_codes, scales, k_zeros, v_zeros, tile_bytes, page_bytes, total_bytes;
+} eesd_kv4_layout;
+int eesd_kv4_layout_of(const eesd_kv4 *c, eesd_kv4_layout *out);
+
+/* The sequences of a call (device pointers; they are read when the kernels run).  Position p of sequence b lies in page
+ * page_table[b * table_stride + p / page_tokens].  Positions below 0, past the table or in a page outside 0 .. n_pages - 1 do not exist:
+ * nothing is written there, reading gives 0, and no row sees them. */
+typedef struct eesd_kv4_rows {
+    const int32_t *page_table;
+    int64_t table_stride;
+    int32_t max_pages;         /* entries of a sequence's table                                       */
+    int32_t B, rows;           /* B <= EESD_KV4_MAX_BATCH                                             */
+    int32_t n_rope;            /* positions of the rope table                                         */
+    const int32_t *at;         /* [B] see the calls                                                   */
+    const int32_t *n_rows;     /* [B] rows of each sequence, cut to 0 .. rows; NULL: rows             */
+    const float *rope;         /* [n_rope][head_dim / 2] (cos, sin); NULL: nothing is turned          */
+    const int32_t *positions;  /* [B][rows] the positions that rows are turned by; NULL: where they lie.  Cut to 0 .. n_rope - 1 */
+} eesd_kv4_rows;
+/* Rows [B][rows][heads][head_dim] with those distances in elements between sequences, rows and heads (a head's values lie together) */
+typedef struct eesd_kv4_tensor {
+    const void *data;
+    int64_t stride_b, stride_row, stride_head;
+} eesd_kv4_tensor;
+#define EESD_KV4_MAX_BATCH 1024
+
+/* The calls are asynchronous on `cuda_stream`; `pool` holds at least eesd_kv4_layout.total_bytes (NOMEM otherwise).  Errors: BADARG, NOMEM,
+ * UNSUPPORTED (also: grids past 2^31 blocks), CUDA.
+ *
+ * eesd_kv4_append: row m of sequence b is written to position at[b] + m.  Keys are turned first: pair (2i, 2i + 1) = (x, y) becomes
+ * (x cos - y sin, x sin + y cos), each product and each sum rounded to fp32.  Then, for each group of the keys and of the values,
+ *   lo = min(w, 0), hi = max(w, 0), s = (hi - lo) / 15, z = clamp(-lo / s, 0, 15), c = clamp(w / s + z, 0, 15)
+ * with s rounded to the nearest bf16 and quotients to the nearest integer, ties to even, as if computed exactly.  A group of zeros (or one
+ * whose scale rounds to 0) reads back as zeros, a group that holds a NaN or an infinity as NaN.  No two rows of a call may have the
+ * same place in the pool.  dtype: EESD_F32 or EESD_BF16, of k and v. */
+int eesd_kv4_append(void *cuda_stream, const eesd_kv4 *c, void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *k,
+                    const eesd_kv4_tensor *v);
+/* eesd_kv4_read: the values at positions at[b] + m (at NULL: 0 + m), m < rows, into k and v (either may be NULL), contiguous
+ * [B][rows][n_kv_heads][head_dim] in out_dtype; 0 where the position does not exist or is not below n_ctx[b] (NULL: no such bound). r's n_rows, rope
+ * and positions are not looked at. */
+int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, const int32_t *n_ctx, int out_dtype, void *k,
+                  void *v);
+/* eesd_kv4_attend: rows <= EESD_MAX_ROWS query rows of each sequence, the last n = n_rows[b] positions of its at[b] tokens (which are in the
+ * cache already), each with n_heads heads of which n_heads / n_kv_heads neighbours share a key / value head.  Row m (position at[b] - n + m):
+ *   out = sum_p exp(x_p - max x) v_p / sum_p exp(x_p - max x),  x_p = scale * (turned q . k_p)
+ * over the positions p <= at[b] - n + m or, with `visible` ([B][rows], device), over p < at[b] - n and those of the n new ones at[b] - n + j whose
+ * bit j of visible[b][m] is set (a tree).  What a row does not see has no effect on it, NaN and infinities included.  A row that sees nothing and rows
+ * from n on are 0.  Row m's new key is not among what it sees by itself: a tree's mask sets the row's own bit.
+ * q in dtype, out contiguous [B][rows][n_heads][head_dim] in dtype, overlapping no input.  scratch: device, 16-byte aligned, eesd_kv4_attend_scratch_bytes
+ * bytes (0: it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.
+ * Arithmetic: sums, maxima and exponentials are fp32.  A query is taken as two fp16 terms (dtype EESD_BF16: one) under a power of two of its row and head:
+ * off by at most 2^-22 (2^-11) of itself, and where it is below 2^-17 (2^-28) of the largest there by at most 2^-39 of that.  So is a softmax numerator
+ * times its value's scale, with 2^-33 of the row's largest. */
+size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads, int dtype);
+int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *q,
+                    int n_heads, float scale, const int32_t *visible, void *out, void *scratch, size_t scratch_bytes);
+
 #ifdef __cplusplus
 }
 #endif

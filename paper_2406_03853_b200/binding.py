@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence
 
@@ -84,6 +85,14 @@ class W4Desc(C.Structure):
 class W4Layout(C.Structure):
     _fields_ = [("scales", C.c_size_t), ("zeros", C.c_size_t), ("block_bytes", C.c_size_t), ("total_bytes", C.c_size_t),
                 ("row_blocks", C.c_int32), ("k_blocks", C.c_int32), ("groups", C.c_int32)]
+
+
+class KV4Desc(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("group", C.c_int32)]
+
+
+class KV4Layout(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("v_codes", "scales", "k_zeros", "v_zeros", "tile_bytes", "page_bytes", "total_bytes")]
 
 
 class RulesStruct(C.Structure):
@@ -166,6 +175,12 @@ def lib():
         L.eesd_w4_project_scratch_bytes.argtypes = [vp, C.c_int]
         L.eesd_w4_project_rows.argtypes = [vp, vp, vp, sz, C.c_int, vp, i64, vp, i64, C.c_int, vp, sz]
         L.eesd_process_logits.argtypes = [vp, vp, i64, vp, i64, C.c_int, C.c_int, C.c_int, vp]
+        L.eesd_kv4_layout_of.argtypes = [vp, vp]
+        L.eesd_kv4_append.argtypes = [vp, vp, vp, sz, vp, C.c_int, vp, vp]
+        L.eesd_kv4_read.argtypes = [vp, vp, vp, sz, vp, vp, C.c_int, vp, vp]
+        L.eesd_kv4_attend_scratch_bytes.restype = sz
+        L.eesd_kv4_attend_scratch_bytes.argtypes = [vp, vp, C.c_int, C.c_int]
+        L.eesd_kv4_attend.argtypes = [vp, vp, vp, sz, vp, C.c_int, vp, C.c_int, C.c_float, vp, vp, vp, sz]
         _lib = L
     return _lib
 
@@ -862,4 +877,157 @@ def process_logits(logits: torch.Tensor, rules: LogitRules, out: Optional[torch.
             raise ValueError("out: wanted the shape of logits")
         ld_out = _row_stride(out, "out")
     _call(lib().eesd_process_logits, "eesd_process_logits", index, logits.data_ptr(), ld, out.data_ptr(), ld_out, B, rows, V, rules._ptr)
+    return out
+
+
+# ---- key / value cache in 4 bits
+_kv4_rows = struct.Struct("PqiiiiPPPP").pack      # eesd_kv4_rows
+_kv4_tensor = struct.Struct("Pqqq").pack          # eesd_kv4_tensor
+
+
+def _kv4_vector(t, name: str, B: int, index: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype is not _I32 or not t.is_cuda or t.get_device() != index or t.shape != (B,) or not t.is_contiguous():
+        raise ValueError(f"{name}: wanted a contiguous tensor of torch.int32 [{B}] on device {index}")
+    return t.data_ptr()
+
+
+class KV4Cache:
+    """A paged cache of keys and values in 4 bits with a scale and a zero point per group of `group` values of a head (eesd_kv4): `append` writes
+    rows into it, `read` gives the values back, attend_rows attends over it.  The caller deals the pages out: a call's page_table [B, pages] int32 names
+    the pages of each sequence, position p in page p // page_tokens of its table; positions outside the table or in a page that does not exist
+    are not written and not seen.  Storage: one uint8 tensor of `page_bytes` * n_pages bytes (`buffer`; the caller's own where given)."""
+
+    def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int = 16, group: int = 64, device="cuda", buffer: Optional[torch.Tensor] = None):
+        self.n_pages, self.n_kv_heads, self.head_dim, self.page_tokens, self.group = n_pages, n_kv_heads, head_dim, page_tokens, group
+        self._desc, self.layout = KV4Desc(n_pages, n_kv_heads, head_dim, page_tokens, group), KV4Layout()
+        self._desc_ptr = C.addressof(self._desc)
+        st = lib().eesd_kv4_layout_of(self._desc_ptr, C.addressof(self.layout))
+        if st:
+            raise EesdError(st, "eesd_kv4_layout_of")
+        self.page_bytes = self.layout.page_bytes
+        if buffer is None:
+            buffer = torch.zeros(self.layout.total_bytes, dtype=_U8, device=device)
+        self._index = _check_tensor(buffer, "buffer", (_U8,))
+        if buffer.dim() != 1 or not buffer.is_contiguous() or buffer.numel() < self.layout.total_bytes:
+            raise ValueError(f"buffer: wanted {self.layout.total_bytes} contiguous bytes")
+        self.buffer, self._ptr, self._bytes = buffer, buffer.data_ptr(), buffer.numel()
+
+    @property
+    def device(self) -> torch.device:
+        return self.buffer.device
+
+    def _rows(self, page_table, B: int, rows: int, at, at_name: str, n_rows, rope, positions) -> bytes:
+        """eesd_kv4_rows of a call, its tensors checked"""
+        index = self._index
+        if not isinstance(page_table, torch.Tensor) or page_table.dtype is not _I32 or not page_table.is_cuda or page_table.get_device() != index:
+            raise ValueError(f"page_table: wanted a tensor of torch.int32 on device {index}")
+        if page_table.dim() != 2 or page_table.shape[0] != B or page_table.shape[1] < 1 or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+            raise ValueError(f"page_table: wanted [{B}, pages] with the pages of a sequence next to each other")
+        pages = page_table.shape[1]
+        stride = page_table.stride(0) if B > 1 else pages
+        if stride < pages:
+            raise ValueError("page_table: the tables of two sequences overlap")
+        n_rope = rope_ptr = pos_ptr = 0
+        if rope is not None:
+            _check_tensor(rope, "rope", (_F32,), index)
+            if rope.dim() != 3 or rope.shape[0] < 1 or rope.shape[1] != self.head_dim // 2 or rope.shape[2] != 2 or not rope.is_contiguous():
+                raise ValueError(f"rope: wanted contiguous [positions, {self.head_dim // 2}, 2]")
+            n_rope, rope_ptr = rope.shape[0], rope.data_ptr()
+        if positions is not None:
+            _check_tensor(positions, "positions", (_I32,), index)
+            if positions.shape != (B, rows) or not positions.is_contiguous():
+                raise ValueError(f"positions: wanted contiguous [{B}, {rows}]")
+            pos_ptr = positions.data_ptr()
+        return _kv4_rows(page_table.data_ptr(), stride, pages, B, rows, n_rope, 0 if at is None else _kv4_vector(at, at_name, B, index),
+                         0 if n_rows is None else _kv4_vector(n_rows, "n_rows", B, index), rope_ptr, pos_ptr)
+
+    def _tensor(self, t, name: str, dtypes, heads: Optional[int] = None) -> bytes:
+        """eesd_kv4_tensor of [B, rows, heads, head_dim]"""
+        _check_tensor(t, name, dtypes, self._index)
+        shape = t.shape
+        if len(shape) != 4 or shape[3] != self.head_dim or t.stride(3) != 1 or not shape[0] or not shape[1] or not shape[2] or (heads and shape[2] != heads):
+            raise ValueError(f"{name}: wanted [B, rows, {heads or 'heads'}, {self.head_dim}] with a head's values next to each other")
+        s = t.stride()
+        return _kv4_tensor(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, start: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
+               rope: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None) -> None:
+        """eesd_kv4_append: rows k, v [B, rows, n_kv_heads, head_dim] fp32 or bf16 (any strides over sequences, rows and heads) quantised into
+        positions start[b] + m.  start, n_rows [B] int32: the first row's position, and how many of the rows a sequence has (left out: all), read on
+        the device.  rope [positions, head_dim / 2, 2] fp32: (cos, sin) by which the keys are turned first, at the rows' places or at
+        positions [B, rows] int32.  No two rows of a call may have the same place."""
+        kt, vt = self._tensor(k, "k", _DTYPES, self.n_kv_heads), self._tensor(v, "v", (k.dtype,), self.n_kv_heads)
+        if v.shape != k.shape:
+            raise ValueError("k and v: wanted the same shape")
+        if start is None:
+            raise ValueError("start: wanted a tensor")
+        r = self._rows(page_table, k.shape[0], k.shape[1], start, "start", n_rows, rope, positions)
+        _call(lib().eesd_kv4_append, "eesd_kv4_append", self._index, self._desc_ptr, self._ptr, self._bytes, r, _DTYPES[k.dtype], kt, vt)
+
+    def read(self, page_table: torch.Tensor, count: int, start: Optional[torch.Tensor] = None, n_ctx: Optional[torch.Tensor] = None,
+             dtype: torch.dtype = torch.float32):
+        """eesd_kv4_read: (k, v), each [B, count, n_kv_heads, head_dim] fp32 or bf16: the values at positions start[b] + m (left out: 0 + m), 0 where the
+        position does not exist or is not below n_ctx[b]."""
+        if dtype not in _DTYPES:
+            raise ValueError("dtype: torch.float32 or torch.bfloat16")
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or not page_table.shape[0]:
+            raise ValueError("page_table: wanted [B, pages]")
+        B = page_table.shape[0]
+        if count < 1:
+            raise ValueError("count: at least one position")
+        r = self._rows(page_table, B, count, start, "start", None, None, None)
+        n = None if n_ctx is None else _kv4_vector(n_ctx, "n_ctx", B, self._index)
+        k = self.buffer.new_empty((B, count, self.n_kv_heads, self.head_dim), dtype=dtype)
+        v = torch.empty_like(k)
+        _call(lib().eesd_kv4_read, "eesd_kv4_read", self._index, self._desc_ptr, self._ptr, self._bytes, r, n, _DTYPES[dtype], k.data_ptr(), v.data_ptr())
+        return k, v
+
+
+def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ctx: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
+                scale: Optional[float] = None, visible: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
+                positions: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """eesd_kv4_attend: q [B, rows, heads, head_dim] fp32 or bf16, rows <= MAX_ROWS: the last rows (n_rows[b] of them, left out: all) of each sequence's
+    n_ctx[b] tokens, whose keys and values are in the cache already; returns [B, rows, heads, head_dim] of q's type, rows past n_rows[b] 0.
+    A row sees the positions up to its own, or with visible [B, rows] int32 those before the new rows and the new rows whose bit is set (its own
+    among them).  scale: 1 / sqrt(head_dim) where left out.  rope, positions: as in KV4Cache.append, for the queries.  n_ctx, n_rows, visible, positions and
+    page_table are read on the device.  out, scratch: contiguous, made for the call when left out; calls that may overlap need their own."""
+    if not isinstance(cache, KV4Cache):
+        raise ValueError("cache: wanted a KV4Cache")
+    index, D = cache._index, cache.head_dim
+    qt = cache._tensor(q, "q", _DTYPES)
+    B, rows, H, _ = q.shape
+    if rows > MAX_ROWS:
+        raise ValueError(f"q: 1 to {MAX_ROWS} rows, not {rows}")
+    if H % cache.n_kv_heads:
+        raise ValueError(f"q: {H} heads do not share {cache.n_kv_heads}")
+    if n_ctx is None:
+        raise ValueError("n_ctx: wanted a tensor")
+    r = cache._rows(page_table, B, rows, n_ctx, "n_ctx", n_rows, rope, positions)
+    vis = None
+    if visible is not None:
+        _check_tensor(visible, "visible", (_I32,), index)
+        if visible.shape != (B, rows) or not visible.is_contiguous():
+            raise ValueError(f"visible: wanted contiguous [{B}, {rows}]")
+        vis = visible.data_ptr()
+    if scale is None:
+        scale = D ** -0.5
+    dt = _DTYPES[q.dtype]
+    L, ptr = lib(), None
+    if scratch is not None:
+        _check_tensor(scratch, "scratch", (_U8,), index)
+        if not scratch.is_contiguous():
+            raise ValueError("scratch: wanted contiguous")
+        ptr, size = scratch.data_ptr(), scratch.numel()
+    else:
+        size = L.eesd_kv4_attend_scratch_bytes(cache._desc_ptr, r, H, dt)
+        if size:
+            scratch = q.new_empty(size, dtype=_U8)
+            ptr = scratch.data_ptr()
+    if out is None:
+        out = q.new_empty((B, rows, H, D))
+    else:
+        _check_tensor(out, "out", (q.dtype,), index)
+        if out.shape != q.shape or not out.is_contiguous():
+            raise ValueError("out: wanted contiguous, of q's shape")
+    _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, r, dt, qt, H, scale, vis, out.data_ptr(), ptr, size)
     return out

@@ -1,0 +1,341 @@
+// Key / value cache in 4 bits: rows quantised as they are written, and read back (sm_100a).
+//
+//   group of a head's values w:  s = bf16((hi - lo) / 15), z = rn(-lo / s), c = rn(w / s) + z;  value = (c - z) s
+//
+// Storage: tiles of 16 tokens of one head (Tile), laid out so that attention's matrix instruction (m16n8k16 on fp16) finds a lane's
+// share of a tile in one 16-byte piece: keys as rows of 16 tokens x 16 dimensions, values as rows of 16 dimensions x 16 tokens.
+#include "kernels.cuh"
+#include "kv4.cuh"
+#include "quant4.cuh"
+
+namespace eesd {
+namespace kv4 {
+
+constexpr int kThreads = 256;
+
+struct Rows {
+    const int32_t *at, *n_rows;
+    int rows, tiles;   // tiles: those that a sequence's rows may touch
+};
+
+// N neighbouring values of a row
+template <int N, typename T> __device__ __forceinline__ void load(const T *p, bool vec, float (&x)[N]) {
+    if (vec) {
+        if constexpr (sizeof(T) == 4 && N == 4) {
+            const float4 v = __ldcs(reinterpret_cast<const float4 *>(p));
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else if constexpr (sizeof(T) == 4) {
+            const float2 v = __ldcs(reinterpret_cast<const float2 *>(p));
+            x[0] = v.x, x[1] = v.y;
+        } else {
+            uint32_t w[N / 2];
+            if constexpr (N == 4) {
+                const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(p));
+                w[0] = v.x, w[1] = v.y;
+            } else {
+                w[0] = __ldcs(reinterpret_cast<const uint32_t *>(p));
+            }
+#pragma unroll
+            for (int i = 0; i < N / 2; i++) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = to_f(p[i]);
+    }
+}
+
+struct AppendArgs {
+    Cache c;
+    Rows r;
+    const void *k, *v;
+    int64_t ks[3], vs[3];
+    const float *rope;
+    const int32_t *positions;
+    int n_rope;
+    bool vec;
+};
+
+// One block: a tile of 16 tokens of one head, as far as the call's rows fill it; one warp a token's keys or values, N = D / 32 neighbours a
+// lane.  The codes meet in shared memory and go out as the tile's bytes, whole where the tile is.
+template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
+    constexpr int N = D / 32, GL = 32 / G;   // GL: lanes of a group
+    using L = Tile<D, G>;
+    __shared__ __align__(16) unsigned char tile[L::BYTES];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned int blk = blockIdx.x;
+    const int h = blk % a.c.Hkv;
+    blk /= a.c.Hkv;
+    const int x = blk % a.r.tiles, b = blk / a.r.tiles;
+    const int64_t start = a.r.at[b], ti = (start >> 4) + x;   // (>> rounds down)
+    const int n = a.r.n_rows ? min(max(a.r.n_rows[b], 0), a.r.rows) : a.r.rows;
+    const int64_t first = start - ti * 16, past = first + n;   // the rows' places in the tile
+    const int lo = first > 0 ? (int)first : 0, hi = past < 16 ? (int)past : 16;
+    if (ti < 0 || lo >= hi) return;
+    unsigned char *dst = tile_at(a.c, b, h, ti, L::BYTES);
+    if (!dst) return;
+    for (int task = warp; task < 2 * (hi - lo); task += kThreads / 32) {
+        const bool is_v = task & 1;
+        const int tok = lo + (task >> 1), m = (int)(tok - first);
+        float w[N];
+        if (is_v) load<N>((const T *)a.v + b * a.vs[0] + m * a.vs[1] + h * a.vs[2] + lane * N, a.vec, w);
+        else load<N>((const T *)a.k + b * a.ks[0] + m * a.ks[1] + h * a.ks[2] + lane * N, a.vec, w);
+        if (!is_v && a.rope) {
+            const int64_t pos = a.positions ? (int64_t)a.positions[(int64_t)b * a.r.rows + m] : ti * 16 + tok;
+            const int64_t row = min(max(pos, (int64_t)0), (int64_t)(a.n_rope - 1));
+            const float2 *cs = reinterpret_cast<const float2 *>(a.rope) + row * (D / 2) + lane * (N / 2);
+#pragma unroll
+            for (int i = 0; i < N / 2; i++) {
+                const float2 y = turn(w[2 * i], w[2 * i + 1], cs[i]);
+                w[2 * i] = y.x, w[2 * i + 1] = y.y;
+            }
+        }
+        float most = 0.f, least = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; i++) most = max_nan(most, w[i]), least = min_nan(least, w[i]);
+#pragma unroll
+        for (int o = 1; o < GL; o <<= 1) {
+            most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+            least = min_nan(least, __shfl_xor_sync(0xffffffffu, least, o));
+        }
+        float s = round_range(most, least, EESD_BF16);
+        if (!(most <= 3.402823466e38f) || !(least >= -3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
+        const bool plain = s > 0.f;   // (neither 0 nor NaN)
+        const float z = plain ? fminf(nearest_quotient(-least, s), 15.f) : 0.f;
+        uint32_t c[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) c[i] = plain ? (uint32_t)fminf(fmaxf(nearest_quotient(w[i], s) + z, 0.f), 15.f) : 0u;
+        if (lane % GL == 0) {
+            const int gi = lane / GL;
+            reinterpret_cast<uint16_t *>(tile + L::SCALES)[(gi * 16 + tok) * 2 + is_v] = __bfloat16_as_ushort(__float2bfloat16_rn(s));
+            tile[(is_v ? L::VZ : L::KZ) + gi * 16 + tok] = (unsigned char)z;
+        }
+        if (!is_v) {
+            const int d = lane * N, at = tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4 + d % 8 / 2;
+            if constexpr (N == 4) *reinterpret_cast<uint16_t *>(tile + at) = (uint16_t)(c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12);
+            else tile[at] = (unsigned char)(c[0] | c[1] << 4);
+        } else {
+            // a word takes one nibble of each of 8 lanes: N words, halved among the lanes at each exchange
+            const int d = lane * N, shift = 4 * (d % 64 / 8), t = tok % 8 / 2, he = tok / 8 * 2 + tok % 2;
+            int word;
+            uint32_t v;
+            if constexpr (N == 4) {
+                const bool up1 = lane & 2, up2 = lane & 4;
+                const uint32_t s0 = up1 ? c[0] : c[2], s1 = up1 ? c[1] : c[3];
+                uint32_t k0 = (up1 ? c[2] : c[0]) << shift, k1 = (up1 ? c[3] : c[1]) << shift;
+                k0 |= __shfl_xor_sync(0xffffffffu, s0 << shift, 2);
+                k1 |= __shfl_xor_sync(0xffffffffu, s1 << shift, 2);
+                v = (up2 ? k1 : k0) | __shfl_xor_sync(0xffffffffu, up2 ? k0 : k1, 4);
+                v |= __shfl_xor_sync(0xffffffffu, v, 8);
+                word = up1 * 2 + up2;
+            } else {
+                const bool up = lane & 4;
+                v = ((up ? c[1] : c[0]) << shift) | __shfl_xor_sync(0xffffffffu, (up ? c[0] : c[1]) << shift, 4);
+                v |= __shfl_xor_sync(0xffffffffu, v, 8);
+                v |= __shfl_xor_sync(0xffffffffu, v, 16);
+                word = up;
+            }
+            if (N == 4 ? !(lane & 8) : !(lane & 24)) reinterpret_cast<uint32_t *>(tile + L::V)[((d / 64 * 8 + d % 8 + word) * 4 + t) * 4 + he] = v;
+        }
+    }
+    __syncthreads();
+    if (hi - lo == 16) {
+        for (int i = threadIdx.x; i < L::BYTES / 16; i += kThreads) reinterpret_cast<uint4 *>(dst)[i] = reinterpret_cast<const uint4 *>(tile)[i];
+        return;
+    }
+    for (int i = threadIdx.x; i < L::KZ / 4; i += kThreads) {
+        const int at = i * 4;
+        const int tok = at < L::V ? at / (D / 2) : at < L::SCALES ? (i & 2) * 4 + (i >> 2 & 3) * 2 + (i & 1) : i - L::SCALES / 4 & 15;
+        if (tok >= lo && tok < hi) reinterpret_cast<uint32_t *>(dst)[i] = reinterpret_cast<const uint32_t *>(tile)[i];
+    }
+    for (int i = L::KZ + threadIdx.x; i < L::BYTES; i += kThreads)
+        if ((i & 15) >= lo && (i & 15) < hi) dst[i] = tile[i];
+}
+
+struct ReadArgs {
+    Cache c;
+    Rows r;
+    const int32_t *n_ctx;
+    void *k, *v;
+};
+
+// One block: a tile, brought into shared memory; one warp a token's keys or values, N = D / 32 neighbours a lane.
+template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a) {
+    constexpr int N = D / 32, GL = 32 / G;
+    using L = Tile<D, G>;
+    __shared__ __align__(16) unsigned char tile[L::BYTES];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned int blk = blockIdx.x;
+    const int h = blk % a.c.Hkv;
+    blk /= a.c.Hkv;
+    const int x = blk % a.r.tiles, b = blk / a.r.tiles;
+    const int64_t start = a.r.at ? a.r.at[b] : 0, ti = (start >> 4) + x, first = start - ti * 16, past = first + a.r.rows;
+    const int lo = first > 0 ? (int)first : 0, hi = past < 16 ? (int)past : 16;
+    if (lo >= hi) return;
+    const int64_t left = a.n_ctx ? (int64_t)a.n_ctx[b] - ti * 16 : 16;
+    const unsigned char *src = ti < 0 || left <= lo ? nullptr : tile_at(a.c, b, h, ti, L::BYTES);
+    if (src)
+        for (int i = threadIdx.x; i < L::BYTES / 16; i += kThreads) reinterpret_cast<uint4 *>(tile)[i] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
+    __syncthreads();
+    const int gi = lane / GL, d = lane * N;
+    for (int task = warp; task < 2 * (hi - lo); task += kThreads / 32) {
+        const bool is_v = task & 1;
+        const int tok = lo + (task >> 1);
+        T *out = (T *)(is_v ? a.v : a.k);
+        if (!out) continue;
+        float w[N];
+        if (src && tok < left) {
+            const uint32_t word = reinterpret_cast<const uint32_t *>(tile + L::SCALES)[gi * 16 + tok];
+            const float s = __uint_as_float(is_v ? word & 0xffff0000u : word << 16);
+            const int z = tile[(is_v ? L::VZ : L::KZ) + gi * 16 + tok];
+            if (!is_v) {
+                const uint32_t c = reinterpret_cast<const uint32_t *>(tile)[(tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4) / 4] >> 4 * (d % 8);
+#pragma unroll
+                for (int i = 0; i < N; i++) w[i] = __fmul_rn((float)((int)(c >> 4 * i & 15) - z), s);
+            } else {
+                const uint32_t *at = reinterpret_cast<const uint32_t *>(tile + L::V) + ((d / 64 * 8 + d % 8) * 4 + tok % 8 / 2) * 4 + tok / 8 * 2 + tok % 2;
+#pragma unroll
+                for (int i = 0; i < N; i++) w[i] = __fmul_rn((float)((int)(at[i * 16] >> 4 * (d % 64 / 8) & 15) - z), s);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) w[i] = 0.f;
+        }
+        out += (((size_t)b * a.r.rows + (size_t)(tok - first)) * a.c.Hkv + h) * D + d;
+        if constexpr (sizeof(T) == 4) {
+            if constexpr (N == 4) __stcs(reinterpret_cast<float4 *>(out), make_float4(w[0], w[1], w[2], w[3]));
+            else __stcs(reinterpret_cast<float2 *>(out), make_float2(w[0], w[1]));
+        } else {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(w[0], w[1]);
+            if constexpr (N == 4) {
+                const __nv_bfloat162 q = __floats2bfloat162_rn(w[2], w[3]);
+                __stcs(reinterpret_cast<uint2 *>(out), make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q)));
+            } else {
+                __stcs(reinterpret_cast<uint32_t *>(out), *reinterpret_cast<const uint32_t *>(&p));
+            }
+        }
+    }
+}
+
+template <typename T> void (*pick_append(int D, int G))(AppendArgs) {
+    if (D == 64) return G == 1 ? append_kernel<64, 1, T> : append_kernel<64, 2, T>;
+    return G == 1 ? append_kernel<128, 1, T> : G == 2 ? append_kernel<128, 2, T> : append_kernel<128, 4, T>;
+}
+template <typename T> void (*pick_read(int D, int G))(ReadArgs) {
+    if (D == 64) return G == 1 ? read_kernel<64, 1, T> : read_kernel<64, 2, T>;
+    return G == 1 ? read_kernel<128, 1, T> : G == 2 ? read_kernel<128, 2, T> : read_kernel<128, 4, T>;
+}
+
+}  // namespace kv4
+
+int kv4_open(const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, kv4::Cache *out, eesd_kv4_layout *l) {
+    const int st = eesd_kv4_layout_of(c, l);
+    if (st) return st;
+    if (!pool || ((uintptr_t)pool & 15) || !r || !r->page_table || r->max_pages < 1 || r->table_stride < r->max_pages || r->B < 1 || r->rows < 1) return EESD_ERR_BADARG;
+    const void *const words[] = {r->page_table, r->at, r->n_rows, r->positions};
+    for (const void *p : words)
+        if ((uintptr_t)p & 3) return EESD_ERR_BADARG;
+    if (r->rope && (((uintptr_t)r->rope & 7) || r->n_rope < 1)) return EESD_ERR_BADARG;
+    if (pool_bytes < l->total_bytes) return EESD_ERR_NOMEM;
+    if (r->B > EESD_KV4_MAX_BATCH) return EESD_ERR_UNSUPPORTED;
+    out->pool = (unsigned char *)pool;
+    out->table = r->page_table;
+    out->table_stride = r->table_stride;
+    out->n_pages = c->n_pages;
+    out->max_pages = r->max_pages;
+    out->Hkv = c->n_kv_heads;
+    out->shift = c->page_tokens == 16 ? 0 : c->page_tokens == 32 ? 1 : c->page_tokens == 64 ? 2 : 3;
+    return EESD_OK;
+}
+
+int kv4_rows_check(const eesd_kv4_tensor *t, int dtype) {
+    if (!t || !t->data || t->stride_b < 0 || t->stride_row < 0 || t->stride_head < 0) return EESD_ERR_BADARG;
+    return (uintptr_t)t->data % (dtype == EESD_F32 ? 4 : 2) ? EESD_ERR_BADARG : EESD_OK;
+}
+
+}  // namespace eesd
+
+using namespace eesd;
+
+namespace {
+// blocks for the tiles that `rows` positions may touch, wherever they begin
+bool kv4_grid(const eesd_kv4_rows *r, int Hkv, kv4::Rows *out, unsigned int *blocks) {
+    out->at = r->at;
+    out->n_rows = r->n_rows;
+    out->rows = r->rows;
+    out->tiles = (int)(((int64_t)r->rows + 14) / 16 + 1);
+    const double n = (double)out->tiles * Hkv * r->B;
+    if (n > 2147483647.0) return false;
+    *blocks = (unsigned int)n;
+    return true;
+}
+bool whole(const eesd_kv4_tensor *t, int n, size_t bytes) {
+    return (uintptr_t)t->data % (n * bytes) == 0 && t->stride_b % n == 0 && t->stride_row % n == 0 && t->stride_head % n == 0;
+}
+}  // namespace
+
+extern "C" {
+
+int eesd_kv4_layout_of(const eesd_kv4 *c, eesd_kv4_layout *out) {
+    if (!c || !out || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535) return EESD_ERR_BADARG;
+    if (c->head_dim != 64 && c->head_dim != 128) return EESD_ERR_UNSUPPORTED;
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return EESD_ERR_UNSUPPORTED;
+    if ((c->group != 32 && c->group != 64 && c->group != 128) || c->group > c->head_dim) return EESD_ERR_UNSUPPORTED;
+    const size_t D = (size_t)c->head_dim, G = D / (size_t)c->group;
+    out->v_codes = 8 * D;
+    out->scales = 16 * D;
+    out->k_zeros = out->scales + 64 * G;
+    out->v_zeros = out->k_zeros + 16 * G;
+    out->tile_bytes = out->v_zeros + 16 * G;
+    out->page_bytes = out->tile_bytes * (size_t)(c->page_tokens / 16) * (size_t)c->n_kv_heads;
+    out->total_bytes = out->page_bytes * (size_t)c->n_pages;
+    return EESD_OK;
+}
+
+int eesd_kv4_append(void *cuda_stream, const eesd_kv4 *c, void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *k,
+                    const eesd_kv4_tensor *v) {
+    kv4::AppendArgs a = {};
+    eesd_kv4_layout l;
+    int st = kv4_open(c, pool, pool_bytes, r, &a.c, &l);
+    if (st) return st;
+    if (!r->at || (dtype != EESD_F32 && dtype != EESD_BF16)) return EESD_ERR_BADARG;
+    if ((st = kv4_rows_check(k, dtype)) || (st = kv4_rows_check(v, dtype))) return st;
+    unsigned int blocks;
+    if (!kv4_grid(r, c->n_kv_heads, &a.r, &blocks)) return EESD_ERR_UNSUPPORTED;
+    a.k = k->data;
+    a.v = v->data;
+    a.ks[0] = k->stride_b, a.ks[1] = k->stride_row, a.ks[2] = k->stride_head;
+    a.vs[0] = v->stride_b, a.vs[1] = v->stride_row, a.vs[2] = v->stride_head;
+    a.rope = r->rope;
+    a.positions = r->positions;
+    a.n_rope = r->n_rope;
+    const size_t es = dtype == EESD_F32 ? 4 : 2;
+    a.vec = whole(k, c->head_dim / 32, es) && whole(v, c->head_dim / 32, es);
+    const int G = c->head_dim / c->group;
+    launch_k(dtype == EESD_F32 ? kv4::pick_append<float>(c->head_dim, G) : kv4::pick_append<__nv_bfloat16>(c->head_dim, G), dim3(blocks), dim3(kv4::kThreads), 0,
+             (cudaStream_t)cuda_stream, pdl_enabled(), a);
+    return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
+}
+
+int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, const int32_t *n_ctx, int out_dtype, void *k,
+                  void *v) {
+    kv4::ReadArgs a = {};
+    eesd_kv4_layout l;
+    const int st = kv4_open(c, pool, pool_bytes, r, &a.c, &l);
+    if (st) return st;
+    if ((!k && !v) || ((uintptr_t)k & 15) || ((uintptr_t)v & 15) || ((uintptr_t)n_ctx & 3) || (out_dtype != EESD_F32 && out_dtype != EESD_BF16)) return EESD_ERR_BADARG;
+    unsigned int blocks;
+    if (!kv4_grid(r, c->n_kv_heads, &a.r, &blocks)) return EESD_ERR_UNSUPPORTED;
+    a.n_ctx = n_ctx;
+    a.k = k;
+    a.v = v;
+    const int G = c->head_dim / c->group;
+    launch_k(out_dtype == EESD_F32 ? kv4::pick_read<float>(c->head_dim, G) : kv4::pick_read<__nv_bfloat16>(c->head_dim, G), dim3(blocks), dim3(kv4::kThreads), 0,
+             (cudaStream_t)cuda_stream, pdl_enabled(), a);
+    return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
+}
+
+}  // extern "C"
