@@ -441,7 +441,7 @@ def test_refusals():
             pytest.fail(f"call {i} went through")
     for f in (lambda: eesd.KV4Cache(4, 2, 96), lambda: eesd.KV4Cache(4, 2, 64, page_tokens=8), lambda: eesd.KV4Cache(4, 2, 64, group=128), lambda: eesd.KV4Cache(0, 2, 64),
               lambda: eesd.attend_rows(q, c, table, L, scale=0.0), lambda: eesd.attend_rows(q, c, table, L, scale=math.nan),
-              lambda: eesd.attend_rows(torch.zeros(2, 1, 4, 64, device="cuda"), c, torch.zeros(2, 999, dtype=torch.int32, device="cuda"), L,
+              lambda: eesd.attend_rows(torch.zeros(2, 1, 4, 64, device="cuda"), c, torch.zeros(2, 99999, dtype=torch.int32, device="cuda"), L,
                                        scratch=torch.zeros(16, dtype=torch.uint8, device="cuda")),
               lambda: c.read(torch.zeros(1025, 1, dtype=torch.int32, device="cuda"), 1)):
         with pytest.raises(eesd.EesdError):

@@ -81,10 +81,10 @@ def test_entry_refusals():
 def test_scratch():
     L, d = eesd.lib(), desc(400, 2, 128, 16, 64)
     p, n = C.addressof(d), size(d).total_bytes
-    long = rows(stride=200, pages=200)
+    long = rows(stride=99999, pages=99999)
     need = L.eesd_kv4_attend_scratch_bytes(p, long, 4, 0)
     assert need > 0 and need % 16 == 0
-    for bad in (dict(H=3), dict(dt=7), dict(r=rows(stride=200, pages=200, rows=17)), dict(r=None)):
+    for bad in (dict(H=3), dict(dt=7), dict(r=rows(stride=99999, pages=99999, rows=17)), dict(r=None)):
         assert L.eesd_kv4_attend_scratch_bytes(p, bad.get("r", long), bad.get("H", 4), bad.get("dt", 0)) == 0
     f = lambda s, sn: L.eesd_kv4_attend(None, p, AT, n, long, 0, tensor(), 4, 0.125, None, AT, s, sn)
     assert f(None, need) == BADARG and f(AT + 8, need) == BADARG and f(AT, need - 1) == NOMEM
