@@ -607,9 +607,9 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  * from n on are 0.  Row m's new key is not among what it sees by itself: a tree's mask sets the row's own bit.
  * q in dtype, out contiguous [B][rows][n_heads][head_dim] in dtype, overlapping no input.  scratch: device, 16-byte aligned, eesd_kv4_attend_scratch_bytes
  * bytes (0: it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.
- * Arithmetic: sums, maxima and exponentials are fp32.  A query is taken as two fp16 terms (dtype EESD_BF16: one) under a power of two of its row and head:
- * off by at most 2^-22 (2^-11) of itself, and where it is below 2^-17 (2^-28) of the largest there by at most 2^-39 of that.  So is a softmax numerator
- * times its value's scale, with 2^-33 of the row's largest. */
+ * Arithmetic: sums, maxima and exponentials are fp32.  A row and head's queries are taken as whole numbers of 24 bits (dtype EESD_BF16: 16) under a power of
+ * two: off by at most 2^-22 (2^-14) of the largest; their products with codes are exact.  A softmax numerator times its value's scale is taken as two fp16 terms
+ * (EESD_BF16: one): off by at most 2^-22 (2^-11) of itself, or 2^-29 of the row's largest.  A row of queries that holds a NaN or an infinity gives NaN. */
 size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads, int dtype);
 int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *q,
                     int n_heads, float scale, const int32_t *visible, void *out, void *scratch, size_t scratch_bytes);

@@ -15,6 +15,7 @@
 //   runs      the tiles of all segments stand in a row and are dealt out evenly, whatever the sequences' lengths; a second kernel joins what was cut
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
+#include <limits.h>
 
 #include <atomic>
 #include <type_traits>
@@ -27,12 +28,23 @@ namespace kv4 {
 
 namespace cg = cooperative_groups;
 
-constexpr int kWarps = 8, kAttnThreads = kWarps * 32;
-constexpr int kStages = 4;   // tiles of a warp's ring
-constexpr int kUnit = kWarps;
+#ifndef TT1
+#define TT1 2
+#endif
+#ifndef NB2
+#define NB2 2
+#endif
+#ifndef NW2
+#define NW2 6
+#endif
+#ifndef TT2
+#define TT2 1
+#endif
+__host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : NW2; }
+__host__ __device__ constexpr int unit_of(int nt) { return 2 * warps_of(nt); }   // runs: tiles between the places where a segment may be cut
 constexpr int kMaxGrid = 296;
-constexpr int grid_of(int nt) { return nt == 1 ? kMaxGrid : kMaxGrid / 2; }   // blocks that fit the machine's 148 multiprocessors at once
-constexpr int kRise = 4;     // a running maximum is let fall behind by this much (powers of two)
+__host__ __device__ constexpr int grid_of(int nt) { return nt == 1 ? kMaxGrid : kMaxGrid / 2 * NB2; }   // blocks that fit the machine's 148 multiprocessors at once
+constexpr int kRise = 8;     // a running maximum is let fall behind by this much (powers of two)
 constexpr float kLowest = -3.402823466e38f;
 
 struct AttnArgs {
@@ -58,8 +70,8 @@ __device__ __forceinline__ int tiles_of(const AttnArgs &a, int b) {
 }
 
 // ---------------------------------------------------------------------------------- runs
-// A cut inside a segment lies at a multiple of kUnit tiles (one a warp), and at an end where fewer than that would be left.
-__device__ __forceinline__ int64_t cut_at(int64_t off, int64_t n) {
+// A cut inside a segment lies at a multiple of kUnit tiles, and at an end where fewer than that would be left.
+template <int kUnit> __device__ __forceinline__ int64_t cut_at(int64_t off, int64_t n) {
     if (off <= 0) return 0;
     if (off >= n) return n;
     const int64_t c = (off + kUnit / 2) / kUnit * kUnit;
@@ -100,17 +112,26 @@ __device__ __forceinline__ Place find(const AttnArgs &a, const Plan &p, int64_t 
     Place r;
     r.b = lo;
     r.n = (int)(p.before[lo + 1] - p.before[lo]);
-    const int64_t in = pos - p.before[lo] * per;
-    r.seg = (int)(in / r.n);
-    r.off = (int)(in - (int64_t)r.seg * r.n);
+    const uint64_t in = (uint64_t)(pos - p.before[lo] * per);
+    r.seg = in >> 32 ? (int)(in / (uint32_t)r.n) : (int)((uint32_t)in / (uint32_t)r.n);
+    r.off = (int)(in - (uint64_t)r.seg * r.n);
     return r;
 }
-// where block i's run begins
-__device__ __forceinline__ int64_t run_start(const AttnArgs &a, const Plan &p, int64_t i, int64_t grid) {
-    const int64_t total = p.before[a.B] * a.c.Hkv * a.blocks, raw = total * i / grid;
+// the tiles that the blocks before block i of GRID take, and where its run begins
+template <int GRID, int UNIT> __device__ __forceinline__ int64_t run_start(const AttnArgs &a, const Plan &p, int i, Place &f) {
+    const int64_t total = p.before[a.B] * a.c.Hkv * a.blocks, raw = (int64_t)((uint64_t)(total * i) / GRID);
     if (raw >= total) return total;
-    const Place f = find(a, p, raw);
-    return raw - f.off + cut_at(f.off, f.n);
+    f = find(a, p, raw);
+    const int64_t cut = cut_at<UNIT>(f.off, f.n), at = raw - f.off + cut;
+    f.off = (int)cut;
+    if (f.off == f.n) {   // (the next segment's first)
+        f.off = 0;
+        if (++f.seg == a.c.Hkv * a.blocks) {
+            f.seg = 0, f.b++;
+            if (f.b < a.B) f.n = (int)(p.before[f.b + 1] - p.before[f.b]);
+        }
+    }
+    return at;
 }
 
 // ---------------------------------------------------------------------------------- pieces
@@ -139,6 +160,12 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// bytes 0 .. 15 by digits -128 .. 127
+__device__ __forceinline__ void imma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 // c - z of two codes, exactly: the low nibbles of x's bytes 0 and 2 set into the mantissa of 1024, or the high ones into that of 64, less what the zero
 // point makes of it.  (The two bases in registers: with mask and base both known the compiler would take two operations for one.)
 struct Pair { uint32_t low, high; };
@@ -152,11 +179,8 @@ __device__ __forceinline__ uint32_t high(uint32_t x, const Pair &base, const Pai
     asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;\n\tadd.rn.f16x2 %0, %0, %3;" : "=&r"(r) : "r"(x), "r"(base.high), "r"(zero.high));
     return r;
 }
-// -(1024 + z) and -(64 + z) of two zero points: byte 0 of z twice, or bytes 0 and 1 (below 16)
-template <bool SAME> __device__ __forceinline__ Pair zeros(uint32_t z) {
-    constexpr uint32_t pick = SAME ? 0x4040u : 0x4140u;
-    return Pair{__byte_perm(z, 0xe4u, pick), __byte_perm(z << 4, 0xd4u, pick)};
-}
+// -(1024 + z) and -(64 + z) of two zero points, bytes 0 and 1 of z (below 16)
+__device__ __forceinline__ Pair zeros(uint32_t z) { return Pair{__byte_perm(z, 0xe4u, 0x4140), __byte_perm(z << 4, 0xd4u, 0x4140)}; }
 __device__ __forceinline__ void copy16(uint32_t dst, const unsigned char *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -182,88 +206,100 @@ template <int D, typename T> __device__ __forceinline__ void store_out(const Att
     store4(out, r == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x * r, y.y * r, y.z * r, y.w * r));
 }
 
-template <int D, int G, int NT> struct Shared {
-    static constexpr int C = 8 * NT;
+template <int D, int G, int NT, int TT> struct Shared {
+    static constexpr int C = 8 * NT, kWarps = warps_of(NT), STAGES = TT == 1 ? 4 : 2;   // STAGES: steps of a warp's ring
     union {
-        unsigned char ring[kWarps][kStages][Tile<D, G>::BYTES];
+        unsigned char ring[kWarps][STAGES][TT * Tile<D, G>::BYTES];
         float o[kWarps][C][D + 4];   // the warps' outputs
     };
-    struct {
-        uint32_t hi[NT][D / 32][32][4], lo[NT][D / 32][32][4];   // in operand order
-    } q;
+    uint32_t q[NT][D / 32][32][4];    // digits 0 and 1 of the queries, in operand order
+    uint32_t q2[NT][D / 32][32][2];   // digit 2 (fp32 queries)
+    int2 qsum[C][D / 32];             // of a group (at first: of 32 dimensions): the sum of digits 0 and 1 together, and of digit 2
     float2 ml[kWarps][C];   // the warps' maxima and sums
     float most[C][2];       // largest finite query of a column (of its halves)
+    int bad[C][2];          // whether one is not finite
     float alpha[C];         // what a unit of its scores is worth
     float2 ml_all[C];       // the block's
     float y[C][D];
+    Place begin;            // runs: where the block begins, and how many tiles it takes
+    int64_t count[2];
     Plan plan;              // (runs alone; last)
 };
 
-template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAttnThreads, NT == 1 ? 2 : 1) attend_kernel(const AttnArgs a) {
+template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __launch_bounds__(32 * warps_of(NT), NT == 1 ? 2 : NB2) attend_kernel(const AttnArgs a) {
     using L = Tile<D, G>;
-    constexpr int J = D / 32, W = D / 64, C = 8 * NT, HALF = D / 2;
+    constexpr int J = D / 32, W = D / 64, C = 8 * NT, HALF = D / 2, kStages = Shared<D, G, NT, TT>::STAGES;
+    constexpr int kWarps = warps_of(NT), kAttnThreads = 32 * kWarps;
     using T = std::conditional_t<F32, float, __nv_bfloat16>;
     extern __shared__ __align__(16) unsigned char raw[];
-    Shared<D, G, NT> &sh = *reinterpret_cast<Shared<D, G, NT> *>(raw);
+    using S = Shared<D, G, NT, TT>;
+    S &sh = *reinterpret_cast<S *>(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     Pair base;
     asm volatile("mov.b32 %0, 0x64006400;" : "=r"(base.low));
     asm volatile("mov.b32 %0, 0x54005400;" : "=r"(base.high));
-    pdl_trigger();
     pdl_wait();
-    int64_t pos = 0, end = 1;
-    if (!a.share) {
+    pdl_trigger();   // (after the wait: the joining kernel reads the lengths before its own)
+    Place f;
+    int64_t left = 1;   // runs: tiles to do
+    if constexpr (RUNS) {
         make_plan(a, sh.plan);
-        pos = run_start(a, sh.plan, blockIdx.x, gridDim.x);
-        end = run_start(a, sh.plan, blockIdx.x + 1, gridDim.x);
+        if (tid < 2) sh.count[tid] = run_start<grid_of(NT), unit_of(NT)>(a, sh.plan, blockIdx.x + tid, f);
+        if (tid == 0) sh.begin = f;
+        __syncthreads();
+        f = sh.begin;
+        left = sh.count[1] - sh.count[0];
+    } else {
+        const int seg = blockIdx.x / a.share, per = a.c.Hkv * a.blocks;
+        f.b = seg / per;
+        f.seg = seg % per;
+        f.off = 0;
+        f.n = tiles_of(a, f.b);
     }
-    while (pos < end) {
-        Place f;
-        int tile1, first, step = kWarps;
-        if (a.share) {
-            const int seg = blockIdx.x / a.share, per = a.c.Hkv * a.blocks;
-            f.b = seg / per;
-            f.seg = seg % per;
-            f.off = 0;
-            f.n = tile1 = tiles_of(a, f.b);
-            first = blockIdx.x % a.share * kWarps + warp;
-            step *= a.share;
-        } else {
-            f = find(a, sh.plan, pos);
-            tile1 = (int)min((int64_t)f.n, f.off + end - pos);
-            first = f.off + warp;
-        }
+    while (left > 0) {
+        const int tile1 = RUNS ? (int)min((int64_t)f.n, f.off + left) : f.n;
+        const int first = f.off + (RUNS ? warp : blockIdx.x % a.share * kWarps + warp) * TT, step = TT * kWarps * (RUNS ? 1 : a.share);
         const int b = f.b, h = f.seg / a.blocks, pair0 = f.seg % a.blocks * C;
         const int n = rows_of(a, b), old = (int)max((int64_t)a.n_ctx[b] - n, (int64_t)-64);   // positions before the new rows
 
-        // ---- the ring: stage i % kStages holds the warp's tile first + i * step
+        // ---- the ring: stage i % kStages holds the warp's TT tiles from first + i * step on
         const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp][0]);
         const int32_t *table = a.c.table + b * a.c.table_stride;
-        uint32_t there = 0;   // bit s: stage s holds a tile
-        auto page_of = [&](int tile) { return tile < tile1 ? table[tile >> a.c.shift] : -1; };
-        auto fetch = [&](int stage, int tile, int page) {
-            there &= ~(1u << stage);
-            if ((unsigned)page < (unsigned)a.c.n_pages) {
-                const unsigned char *src = a.c.pool + ((((size_t)page * a.c.Hkv + h) << a.c.shift) + (tile & ((1 << a.c.shift) - 1))) * L::BYTES + lane * 16;
-                const uint32_t dst = ring + stage * L::BYTES + lane * 16;
+        uint32_t there = 0;   // bit TT s + i: tile i of stage s exists
+        struct Pages { int v[TT]; };
+        auto pages_of = [&](int tile) {
+            Pages p;
 #pragma unroll
-                for (int i = 0; i < L::BYTES / 512; i++) copy16(dst + i * 512, src + i * 512);
-                if (lane < L::BYTES % 512 / 16) copy16(dst + L::BYTES / 512 * 512, src + L::BYTES / 512 * 512);
-                there |= 1u << stage;
+            for (int i = 0; i < TT; i++) p.v[i] = tile + i < tile1 ? table[(tile + i) >> a.c.shift] : -1;
+            return p;
+        };
+        auto fetch = [&](int stage, int tile, const Pages &pages) {
+#pragma unroll
+            for (int i = 0; i < TT; i++) {
+                there &= ~(1u << (TT * stage + i));
+                if ((unsigned)pages.v[i] < (unsigned)a.c.n_pages) {
+                    const unsigned char *src =
+                        a.c.pool + ((((size_t)pages.v[i] * a.c.Hkv + h) << a.c.shift) + ((tile + i) & ((1 << a.c.shift) - 1))) * L::BYTES + lane * 16;
+                    const uint32_t dst = ring + (stage * TT + i) * L::BYTES + lane * 16;
+#pragma unroll
+                    for (int j = 0; j < L::BYTES / 512; j++) copy16(dst + j * 512, src + j * 512);
+                    if (lane < L::BYTES % 512 / 16) copy16(dst + L::BYTES / 512 * 512, src + L::BYTES / 512 * 512);
+                    there |= 1u << (TT * stage + i);
+                }
             }
             end_copies();
         };
-        int next_page;
+        Pages next_pages;
         {
-            int pages[kStages];
+            Pages pages[kStages];
 #pragma unroll
-            for (int i = 0; i < kStages; i++) pages[i] = page_of(first + i * step);
+            for (int i = 0; i < kStages; i++) pages[i] = pages_of(first + i * step);
 #pragma unroll
             for (int i = 0; i < kStages - 1; i++) fetch(i, first + i * step, pages[i]);
-            next_page = pages[kStages - 1];
+            next_pages = pages[kStages - 1];
         }
 
-        // ---- queries: turned, scaled by a power of two that takes the largest below 2^15, split into fp16 terms
+        // ---- queries: turned, and as whole numbers of 16 (fp32: 24) bits under a power of two of their column, in digits of 8 bits
         constexpr int QI = (C * HALF + kAttnThreads - 1) / kAttnThreads;
         static_assert(C * HALF % 32 == 0 && HALF % 32 == 0, "a warp's values belong to one column");
         float2 qv[QI];
@@ -272,6 +308,7 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
             const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF, rho = pair0 + c, m = rho / a.heads;
             qv[i] = make_float2(0.f, 0.f);
             float most = 0.f;
+            bool bad = false;
             if (c < C && m < n) {
                 const T *src = (const T *)a.q + b * a.qs[0] + m * a.qs[1] + (int64_t)(h * a.heads + rho % a.heads) * a.qs[2] + 2 * e;
                 qv[i] = make_float2(to_f(src[0]), to_f(src[1]));
@@ -279,37 +316,58 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
                     const int at = a.positions ? a.positions[(int64_t)b * a.rows + m] : old + m;
                     qv[i] = turn(qv[i].x, qv[i].y, reinterpret_cast<const float2 *>(a.rope)[(int64_t)min(max(at, 0), a.n_rope - 1) * HALF + e]);
                 }
-                const float u = fabsf(qv[i].x), v = fabsf(qv[i].y);   // (what is not finite does not count)
-                if (u <= -kLowest) most = fmaxf(most, u);
-                if (v <= -kLowest) most = fmaxf(most, v);
+                const float u = fabsf(qv[i].x), v = fabsf(qv[i].y);
+                bad = !(u <= -kLowest) || !(v <= -kLowest);
+                if (bad) qv[i] = make_float2(0.f, 0.f);   // (the column is NaN)
+                else most = fmaxf(u, v);
             }
             most = warp_max(most);
-            if (c < C && lane == 0) sh.most[c][e / 32] = most;
+            bad = __any_sync(0xffffffffu, bad);
+            if (c < C && lane == 0) sh.most[c][e / 32] = most, sh.bad[c][e / 32] = bad;
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < QI; i++) {
             const int idx = tid + i * kAttnThreads, c = idx / HALF, d = idx % HALF * 2;
             if (c < C) {
+                constexpr int kBits = F32 ? 22 : 14;
                 const float most = HALF == 64 ? fmaxf(sh.most[c][0], sh.most[c][1]) : sh.most[c][0];
-                const int ex = max((int)(__float_as_uint(most) >> 23) - 127, -110);   // floor(log2), not below -110
-                const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-                if (d == 0) sh.alpha[c] = a.scale2 * __uint_as_float((uint32_t)(127 + ex - 14) << 23);
-                // operand order: word p of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + p and + 4 of it
-                const int j = d / 32, tt = d % 32 / 8, p = d % 4, half = d % 8 / 4;
-                const float x = qv[i].x * up, y = qv[i].y * up;
-                const __half hx = __float2half_rn(x), hy = __float2half_rn(y);
-                __half *hi = reinterpret_cast<__half *>(sh.q.hi[c / 8][j][c % 8 * 4 + tt]) + half;
-                hi[2 * p] = hx;
-                hi[2 * p + 2] = hy;
+                int ex = max((int)(__float_as_uint(most) >> 23) - 127, -100);   // floor(log2), not below -100
+                if (most * power(kBits - ex) > (F32 ? 127.f * 65536.f : 127.f * 256.f)) ex++;   // (the first digit's range)
+                const int x = __float2int_rn(qv[i].x * power(kBits - ex)), y = __float2int_rn(qv[i].y * power(kBits - ex));
+                if (d == 0) sh.alpha[c] = sh.bad[c][0] || (HALF == 64 && sh.bad[c][1]) ? __uint_as_float(0x7fc00000u) : a.scale2 * power(ex - kBits);
+                // word 0 of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + 0, 2, 4, 6, word 1 the others
+                const int j = d / 32, slot = c % 8 * 4 + d % 32 / 8, byte = d % 8 / 2;
+                const int xl = (int8_t)x, yl = (int8_t)y, xh = (x - xl) >> 8, yh = (y - yl) >> 8;   // the last digit, and the others
+                int8_t *q = reinterpret_cast<int8_t *>(sh.q[c / 8][j][slot]) + byte;
+                const int xm = F32 ? (int8_t)xh : xl, ym = F32 ? (int8_t)yh : yl;
+                q[0] = (int8_t)(F32 ? (xh - xm) >> 8 : xh), q[4] = (int8_t)(F32 ? (yh - ym) >> 8 : yh);
+                q[8] = (int8_t)xm, q[12] = (int8_t)ym;
                 if (F32) {
-                    __half *lo = reinterpret_cast<__half *>(sh.q.lo[c / 8][j][c % 8 * 4 + tt]) + half;
-                    lo[2 * p] = __float2half_rn(x - __half2float(hx));
-                    lo[2 * p + 2] = __float2half_rn(y - __half2float(hy));
+                    int8_t *q2 = reinterpret_cast<int8_t *>(sh.q2[c / 8][j][slot]) + byte;
+                    q2[0] = (int8_t)xl, q2[4] = (int8_t)yl;
                 }
+                int first = F32 ? xh + yh : x + y, second = xl + yl;
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1) {
+                    first += __shfl_xor_sync(0xffffffffu, first, o);
+                    second += __shfl_xor_sync(0xffffffffu, second, o);
+                }
+                if (lane % 16 == 0) sh.qsum[c][j] = make_int2(first, second);
             }
         }
         __syncthreads();
+        if (G < J) {   // 32 dimensions -> a group
+            int2 v = make_int2(0, 0);
+            if (tid < C * G)
+                for (int j = 0; j < J / G; j++) {
+                    const int2 part = sh.qsum[tid / G][tid % G * (J / G) + j];
+                    v.x += part.x, v.y += part.y;
+                }
+            __syncthreads();
+            if (tid < C * G) sh.qsum[tid / G][tid % G] = v;
+            __syncthreads();
+        }
 
         // ---- what the lane's columns (2 t, 2 t + 1 of each eight) see
         int limit[NT][2];
@@ -324,11 +382,16 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
             }
 
         float o[D / 16][NT][4], mx[NT][2], sum[NT][2], alpha[NT][2];
-        // A numerator enters the product as e * scale * unit, with a power of two for each column that puts the largest so far near 2^8: e <=
-        // 2^kRise then keeps them below fp16's range, and what is dropped is below 2^-33 of the largest.  units: the largest of the lane's
+        // A numerator enters the product as e * scale * unit, with a power of two for each column that puts the largest so far near 2^4: e <=
+        // 2^kRise then keeps them below fp16's range, and what is dropped is below 2^-29 of the largest.  units: the largest of the lane's
         float unit[NT][2], weight[NT][2], units = 0x1p120f;
+        float oz[F32 ? 1 : G][NT][4];   // bf16: sums of numerators times zero points (all rows alike)
 #pragma unroll
         for (int i = 0; i < NT; i++) {
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int gi = 0; gi < (F32 ? 1 : G); gi++) oz[gi][i][k] = 0.f;
 #pragma unroll
             for (int k = 0; k < 2; k++) mx[i][k] = kLowest, sum[i][k] = 0.f, unit[i][k] = units, weight[i][k] = 0.f, alpha[i][k] = sh.alpha[i * 8 + 2 * t + k];
 #pragma unroll
@@ -341,113 +404,143 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
         for (int tile = first; tile < tile1; tile += step, stage = (stage + 1) % kStages) {
             wait_copies<kStages - 2>();
             __syncwarp();   // (every lane's copies; and the stage before this one has been read)
-            fetch((stage + kStages - 1) % kStages, tile + (kStages - 1) * step, next_page);
-            next_page = page_of(tile + kStages * step);
-            if (!(there >> stage & 1)) continue;
+            fetch((stage + kStages - 1) % kStages, tile + (kStages - 1) * step, next_pages);
+            next_pages = pages_of(tile + kStages * step);
+            const uint32_t here = there >> (TT * stage) & ((1u << TT) - 1);
+            if (!here) continue;
             const unsigned char *src = sh.ring[warp][stage];
             // ---- scores
-            float x[NT][4], vs[G][2];
+            float x[TT][NT][4], vs[TT][G][2];
+            uint32_t kw[TT][2][J];
 #pragma unroll
-            for (int i = 0; i < NT; i++)
-#pragma unroll
-                for (int k = 0; k < 4; k++) x[i][k] = 0.f;
-            uint32_t kw[2][J];
-#pragma unroll
-            for (int r = 0; r < 2; r++) {
-                if constexpr (J == 4) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (g + 8 * r) * (D / 2) + t * 16);
-                    kw[r][0] = v.x, kw[r][1] = v.y, kw[r][2] = v.z, kw[r][3] = v.w;
-                } else {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(src + (g + 8 * r) * (D / 2) + t * 8);
-                    kw[r][0] = v.x, kw[r][1] = v.y;
-                }
-            }
-#pragma unroll
-            for (int gi = 0; gi < G; gi++) {
-                float ks[2];
-                Pair z[2];
+            for (int u = 0; u < TT; u++)
 #pragma unroll
                 for (int r = 0; r < 2; r++) {
-                    const uint32_t word = reinterpret_cast<const uint32_t *>(src + L::SCALES)[gi * 16 + g + 8 * r];
-                    ks[r] = __uint_as_float(word << 16);
-                    vs[gi][r] = __uint_as_float(word & 0xffff0000u);
-                    z[r] = zeros<true>(src[L::KZ + gi * 16 + g + 8 * r]);
+                    const unsigned char *at = src + u * L::BYTES + (g + 8 * r) * (D / 2) + t * (D / 8);
+                    if constexpr (J == 4) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(at);
+                        kw[u][r][0] = v.x, kw[u][r][1] = v.y, kw[u][r][2] = v.z, kw[u][r][3] = v.w;
+                    } else {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(at);
+                        kw[u][r][0] = v.x, kw[u][r][1] = v.y;
+                    }
                 }
-                float acc[NT][4];
 #pragma unroll
-                for (int i = 0; i < NT; i++)
+            for (int gi = 0; gi < G; gi++) {
+                int acc[TT][NT][F32 ? 3 : 2][4];
 #pragma unroll
-                    for (int k = 0; k < 4; k++) acc[i][k] = 0.f;
+                for (int u = 0; u < TT; u++)
+#pragma unroll
+                    for (int i = 0; i < NT; i++)
+#pragma unroll
+                        for (int p = 0; p < (F32 ? 3 : 2); p++)
+#pragma unroll
+                            for (int k = 0; k < 4; k++) acc[u][i][p][k] = 0;
 #pragma unroll
                 for (int j = gi * J / G; j < (gi + 1) * J / G; j++) {
-                    uint32_t e[2][4];   // [row][dimensions p, p + 4 of the word]
 #pragma unroll
-                    for (int r = 0; r < 2; r++) {
-                        e[r][0] = low(kw[r][j], base, z[r]);
-                        e[r][1] = high(kw[r][j], base, z[r]);
-                        e[r][2] = low(kw[r][j] >> 8, base, z[r]);
-                        e[r][3] = high(kw[r][j] >> 8, base, z[r]);
-                    }
-                    const uint32_t a0[4] = {e[0][0], e[1][0], e[0][1], e[1][1]}, a1[4] = {e[0][2], e[1][2], e[0][3], e[1][3]};
+                    for (int u = 0; u < TT; u++) {
+                        const uint32_t w0 = kw[u][0][j], w1 = kw[u][1][j], w[4] = {w0 & 0x0f0f0f0fu, w1 & 0x0f0f0f0fu, w0 >> 4 & 0x0f0f0f0fu, w1 >> 4 & 0x0f0f0f0fu};
 #pragma unroll
-                    for (int i = 0; i < NT; i++) {
-                        const uint4 q = *reinterpret_cast<const uint4 *>(sh.q.hi[i][j][lane]);
-                        mma(acc[i], a0, q.x, q.y);
-                        mma(acc[i], a1, q.z, q.w);
-                        if (F32) {
-                            const uint4 l = *reinterpret_cast<const uint4 *>(sh.q.lo[i][j][lane]);
-                            mma(acc[i], a0, l.x, l.y);
-                            mma(acc[i], a1, l.z, l.w);
+                        for (int i = 0; i < NT; i++) {
+                            const uint4 q = *reinterpret_cast<const uint4 *>(sh.q[i][j][lane]);
+                            imma(acc[u][i][0], w, q.x, q.y);
+                            imma(acc[u][i][1], w, q.z, q.w);
+                            if constexpr (F32) {
+                                const uint2 q2 = *reinterpret_cast<const uint2 *>(sh.q2[i][j][lane]);
+                                imma(acc[u][i][2], w, q2.x, q2.y);
+                            }
                         }
                     }
                 }
+                int2 qs[NT][2];
 #pragma unroll
                 for (int i = 0; i < NT; i++)
 #pragma unroll
-                    for (int k = 0; k < 4; k++) x[i][k] = gi ? fmaf(acc[i][k], ks[k >> 1], x[i][k]) : acc[i][k] * ks[k >> 1];
+                    for (int k = 0; k < 2; k++) qs[i][k] = sh.qsum[i * 8 + 2 * t + k][gi];
+#pragma unroll
+                for (int u = 0; u < TT; u++) {
+                    float ks[2];
+                    int z[2];
+#pragma unroll
+                    for (int r = 0; r < 2; r++) {
+                        const uint32_t word = reinterpret_cast<const uint32_t *>(src + u * L::BYTES + L::SCALES)[gi * 16 + g + 8 * r];
+                        ks[r] = __uint_as_float(word << 16);
+                        vs[u][gi][r] = __uint_as_float(word & 0xffff0000u);
+                        z[r] = src[u * L::BYTES + L::KZ + gi * 16 + g + 8 * r];
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; i++)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            // sums of q c less the zero point's part: whole numbers until here
+                            const int first = acc[u][i][0][k] * 256 + acc[u][i][1][k] - z[k >> 1] * qs[i][k & 1].x;
+                            float v = (float)first;
+                            if constexpr (F32) v = fmaf(v, 256.f, (float)(acc[u][i][2][k] - z[k >> 1] * qs[i][k & 1].y));
+                            x[u][i][k] = gi ? fmaf(v, ks[k >> 1], x[u][i][k]) : v * ks[k >> 1];
+                        }
+                }
             }
 #pragma unroll
-            for (int i = 0; i < NT; i++)
+            for (int u = 0; u < TT; u++)
 #pragma unroll
-                for (int k = 0; k < 4; k++) x[i][k] *= alpha[i][k & 1];
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) x[u][i][k] *= alpha[i][k & 1];
             // ---- masks
-            uint32_t hidden = 0;   // bit 4 i + k
-            const bool masked = old - tile * 16 < 16;
+            uint32_t hidden = 0;   // bit 4 (u NT + i) + k
+            const bool masked = old - tile * 16 < 16 * TT || here != (1u << TT) - 1;
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < NT; i++)
+                for (int u = 0; u < TT; u++)
 #pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const int p = tile * 16 + g + 8 * (k >> 1);
-                        const uint32_t j = (uint32_t)p - (uint32_t)old;   // (past the old ones: which of the new)
-                        const bool seen = p < limit[i][k & 1] || (j < 16u && bits[i][k & 1] >> j & 1);
-                        if (!seen) hidden |= 1u << (4 * i + k), x[i][k] = -INFINITY;
-                    }
+                    for (int i = 0; i < NT; i++)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            const int p = (tile + u) * 16 + g + 8 * (k >> 1);
+                            const uint32_t j = (uint32_t)p - (uint32_t)old;   // (past the old ones: which of the new)
+                            const bool seen = (here >> u & 1) && (p < limit[i][k & 1] || (j < 16u && bits[i][k & 1] >> j & 1));
+                            if (!seen) hidden |= 1u << (4 * (u * NT + i) + k), x[u][i][k] = -INFINITY;
+                        }
             }
             // ---- a new maximum, or a new unit, where some score (or scale) is far above the last: seldom
-            float vmost = 0.f;
+            float v[TT][2], vmost = 0.f;   // the tokens' largest scales
 #pragma unroll
-            for (int gi = 0; gi < G; gi++) vmost = fmaxf(vmost, fmaxf(vs[gi][0], vs[gi][1]));
+            for (int u = 0; u < TT; u++)
+#pragma unroll
+                for (int r = 0; r < 2; r++) {
+                    v[u][r] = vs[u][0][r];
+#pragma unroll
+                    for (int gi = 1; gi < G; gi++) v[u][r] = fmaxf(v[u][r], vs[u][gi][r]);
+                    vmost = fmaxf(vmost, v[u][r]);
+                }
             bool rise = masked || vmost * units > 65000.f / (1 << kRise);
 #pragma unroll
             for (int i = 0; i < NT; i++)
 #pragma unroll
-                for (int k = 0; k < 4; k++) rise |= x[i][k] > mx[i][k & 1] + (float)kRise;
-            if (__any_sync(0xffffffffu, rise)) {
-                float v[2] = {vs[0][0], vs[0][1]};   // the tokens' largest scales
+                for (int k = 0; k < 2; k++) {
+                    float top = fmaxf(x[0][i][k], x[0][i][k + 2]);
 #pragma unroll
-                for (int gi = 1; gi < G; gi++) v[0] = fmaxf(v[0], vs[gi][0]), v[1] = fmaxf(v[1], vs[gi][1]);
+                    for (int u = 1; u < TT; u++) top = fmaxf(top, fmaxf(x[u][i][k], x[u][i][k + 2]));
+                    rise |= top > mx[i][k] + (float)kRise;
+                }
+            if (__any_sync(0xffffffffu, rise)) {
                 units = 0.f;
 #pragma unroll
                 for (int i = 0; i < NT; i++)
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
-                        float top = fmaxf(x[i][k], x[i][k + 2]);
+                        float top = mx[i][k], most = 0.f;
+#pragma unroll
+                        for (int u = 0; u < TT; u++) top = fmaxf(top, fmaxf(x[u][i][k], x[u][i][k + 2]));
 #pragma unroll
                         for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-                        top = fmaxf(top, mx[i][k]);
                         // (what a column does not see changes neither its maximum nor its unit)
-                        float most = fmaxf(hidden >> (4 * i + k) & 1 ? 0.f : ex2(x[i][k] - top) * v[0], hidden >> (4 * i + k + 2) & 1 ? 0.f : ex2(x[i][k + 2] - top) * v[1]);
+#pragma unroll
+                        for (int u = 0; u < TT; u++)
+#pragma unroll
+                            for (int r = 0; r < 2; r++)
+                                if (!(hidden >> (4 * (u * NT + i) + k + 2 * r) & 1)) most = fmaxf(most, ex2(x[u][i][k + 2 * r] - top) * v[u][r]);
 #pragma unroll
                         for (int s = 4; s < 32; s <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
                         float shift = mx[i][k] - top;
@@ -456,71 +549,96 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
                         sum[i][k] *= f1;
                         weight[i][k] = fmaxf(weight[i][k] * f1, most);
                         if (weight[i][k] > 0.f && weight[i][k] <= -kLowest) {
-                            const int next = 8 + 127 - max((int)(__float_as_uint(weight[i][k]) >> 23), 15), last = (int)(__float_as_uint(unit[i][k]) >> 23) - 127;
+                            const int next = 4 + 127 - max((int)(__float_as_uint(weight[i][k]) >> 23), 11), last = (int)(__float_as_uint(unit[i][k]) >> 23) - 127;
                             shift += (float)(next - last);
                             unit[i][k] = power(next);
                         }
                         units = fmaxf(units, unit[i][k]);
-                        const float f = ex2(shift);
+                        const float f0 = ex2(shift);
 #pragma unroll
-                        for (int r = 0; r < D / 16; r++) o[r][i][k] *= f, o[r][i][k + 2] *= f;
+                        for (int r = 0; r < D / 16; r++) o[r][i][k] *= f0, o[r][i][k + 2] *= f0;
+#pragma unroll
+                        for (int gi = 0; gi < (F32 ? 1 : G); gi++) oz[gi][i][k] *= f0, oz[gi][i][k + 2] *= f0;
                     }
             }
             // ---- numerators
 #pragma unroll
-            for (int i = 0; i < NT; i++)
+            for (int u = 0; u < TT; u++)
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    x[i][k] = ex2(x[i][k] - mx[i][k & 1]);
-                    sum[i][k & 1] += x[i][k];
-                }
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        x[u][i][k] = ex2(x[u][i][k] - mx[i][k & 1]);
+                        sum[i][k & 1] += x[u][i][k];
+                    }
             // ---- outputs
-            uint32_t vw[W][4];
 #pragma unroll
-            for (int w = 0; w < W; w++) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(src + L::V + w * 512 + lane * 16);
-                vw[w][0] = v.x, vw[w][1] = v.y, vw[w][2] = v.z, vw[w][3] = v.w;
-            }
+            for (int u = 0; u < TT; u++) {
+                const unsigned char *at = src + u * L::BYTES;
+                uint32_t vw[W][4];
 #pragma unroll
-            for (int gi = 0; gi < G; gi++) {
-                uint32_t ph[NT][2], pl[NT][2];
-#pragma unroll
-                for (int i = 0; i < NT; i++) {
-                    float y[4];
-#pragma unroll
-                    for (int k = 0; k < 4; k++) y[k] = x[i][k] * (vs[gi][k >> 1] * unit[i][k & 1]);
-                    if (masked) {   // (0 times a scale that is not finite)
-#pragma unroll
-                        for (int k = 0; k < 4; k++)
-                            if (hidden >> (4 * i + k) & 1) y[k] = 0.f;
-                    }
-                    ph[i][0] = pack(y[0], y[1]);
-                    ph[i][1] = pack(y[2], y[3]);
-                    if (F32) {
-                        pl[i][0] = transpose(pack_rest(y[0], y[1], ph[i][0]));
-                        pl[i][1] = transpose(pack_rest(y[2], y[3], ph[i][1]));
-                    }
-                    ph[i][0] = transpose(ph[i][0]);
-                    ph[i][1] = transpose(ph[i][1]);
+                for (int w = 0; w < W; w++) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(at + L::V + w * 512 + lane * 16);
+                    vw[w][0] = q.x, vw[w][1] = q.y, vw[w][2] = q.z, vw[w][3] = q.w;
                 }
-                Pair z[2];   // of tokens 2 t, 2 t + 1 and those 8 after them
 #pragma unroll
-                for (int r = 0; r < 2; r++) z[r] = zeros<false>(*reinterpret_cast<const uint16_t *>(src + L::VZ + gi * 16 + 8 * r + 2 * t));
-#pragma unroll
-                for (int r16 = gi * (D / 16) / G; r16 < (gi + 1) * (D / 16) / G; r16++) {
-                    const int w = r16 / 4, q = r16 % 4;   // nibbles 2 q, 2 q + 1 of the words
-                    uint32_t av[4];
-#pragma unroll
-                    for (int r = 0; r < 2; r++) {
-                        uint32_t y = __byte_perm(vw[w][2 * r], vw[w][2 * r + 1], q < 2 ? 0x5410 : 0x7632);
-                        if (q & 1) y >>= 8;
-                        av[2 * r] = low(y, base, z[r]);
-                        av[2 * r + 1] = high(y, base, z[r]);
-                    }
+                for (int gi = 0; gi < G; gi++) {
+                    uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
                     for (int i = 0; i < NT; i++) {
-                        mma(o[r16][i], av, ph[i][0], ph[i][1]);
-                        if (F32) mma(o[r16][i], av, pl[i][0], pl[i][1]);
+                        float y[4];
+#pragma unroll
+                        for (int k = 0; k < 4; k++) y[k] = x[u][i][k] * (vs[u][gi][k >> 1] * unit[i][k & 1]);
+                        if (masked) {   // (0 times a scale that is not finite)
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+                                if (hidden >> (4 * (u * NT + i) + k) & 1) y[k] = 0.f;
+                        }
+                        ph[i][0] = pack(y[0], y[1]);
+                        ph[i][1] = pack(y[2], y[3]);
+                        if (F32) {
+                            pl[i][0] = transpose(pack_rest(y[0], y[1], ph[i][0]));
+                            pl[i][1] = transpose(pack_rest(y[2], y[3], ph[i][1]));
+                        }
+                        ph[i][0] = transpose(ph[i][0]);
+                        ph[i][1] = transpose(ph[i][1]);
+                    }
+                    // zero points of tokens 2 t, 2 t + 1 and those 8 after them.  fp32: codes less their zero points, so that nothing large cancels.  bf16:
+                    // codes as they are (a nibble in fp16's lowest bits is c 2^-24), and the zero points as rows of their own, whose sums are taken
+                    // off at the end
+                    Pair z[2];
+                    uint32_t az[4];
+#pragma unroll
+                    for (int r = 0; r < 2; r++) {
+                        const uint32_t z2 = *reinterpret_cast<const uint16_t *>(at + L::VZ + gi * 16 + 8 * r + 2 * t);
+                        if (F32) z[r] = zeros(z2);
+                        else az[2 * r] = az[2 * r + 1] = __byte_perm(z2, 0, 0x4140) & 0x000f000fu;
+                    }
+                    if constexpr (!F32) {
+#pragma unroll
+                        for (int i = 0; i < NT; i++) mma(oz[gi][i], az, ph[i][0], ph[i][1]);
+                    }
+#pragma unroll
+                    for (int r16 = gi * (D / 16) / G; r16 < (gi + 1) * (D / 16) / G; r16++) {
+                        const int w = r16 / 4, q = r16 % 4;   // nibbles 2 q, 2 q + 1 of the words
+                        uint32_t av[4];
+#pragma unroll
+                        for (int r = 0; r < 2; r++) {
+                            uint32_t y = __byte_perm(vw[w][2 * r], vw[w][2 * r + 1], q < 2 ? 0x5410 : 0x7632);
+                            if (q & 1) y >>= 8;
+                            if (F32) {
+                                av[2 * r] = low(y, base, z[r]);
+                                av[2 * r + 1] = high(y, base, z[r]);
+                            } else {
+                                av[2 * r] = y & 0x000f000fu;
+                                av[2 * r + 1] = y & 0x00f000f0u;   // (16 c 2^-24)
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < NT; i++) {
+                            mma(o[r16][i], av, ph[i][0], ph[i][1]);
+                            if (F32) mma(o[r16][i], av, pl[i][0], pl[i][1]);
+                        }
                     }
                 }
             }
@@ -541,12 +659,20 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
             for (int k = 0; k < 2; k++) {
                 const int c = i * 8 + 2 * t + k;
                 const float worth = 1.f / unit[i][k];
+                if constexpr (!F32) {
+#pragma unroll
+                    for (int r = 0; r < D / 16; r++) {
+                        const float z = oz[r * G / (D / 16)][i][k] * 0x1p24f;
+                        o[r][i][k] = fmaf(o[r][i][k], 0x1p24f, -z);
+                        o[r][i][k + 2] = fmaf(o[r][i][k + 2], 0x1p20f, -z);
+                    }
+                }
                 if (g == 0) sh.ml[warp][c] = make_float2(mx[i][k], sum[i][k]);
 #pragma unroll
                 for (int r = 0; r < D / 16; r++) sh.o[warp][c][16 * r + g] = o[r][i][k] * worth, sh.o[warp][c][16 * r + 8 + g] = o[r][i][k + 2] * worth;
             }
         __syncthreads();
-        const bool all = a.share ? a.share == 1 : f.off == 0 && tile1 == f.n;
+        const bool all = RUNS ? f.off == 0 && tile1 == f.n : a.share == 1;
         float *part = a.part + (size_t)(2 * blockIdx.x + (f.off == 0)) * C * (D + 4);
         for (int idx = tid; idx < C * (D / 4); idx += kAttnThreads) {
             const int c = idx / (D / 4), d = idx % (D / 4) * 4, rho = pair0 + c;
@@ -564,7 +690,7 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
             }
             if (all) {
                 store_out<D, T>(a, b, h, rho, d, n, y, total);
-            } else if (a.share) {
+            } else if (!RUNS) {
                 *reinterpret_cast<float4 *>(&sh.y[c][d]) = y;
                 if (d == 0) sh.ml_all[c] = make_float2(top, total);
             } else {
@@ -572,7 +698,7 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
                 if (d == 0) *reinterpret_cast<float2 *>(part + c * (D + 4) + D) = make_float2(top, total);
             }
         }
-        if (a.share > 1) {
+        if (!RUNS && a.share > 1) {
             cg::cluster_group cluster = cg::this_cluster();
             cluster.sync();
             for (int idx = blockIdx.x % a.share * kAttnThreads + tid; idx < C * (D / 4); idx += a.share * kAttnThreads) {
@@ -591,44 +717,54 @@ template <int D, int G, int NT, bool F32> __global__ void __launch_bounds__(kAtt
             }
             cluster.sync();   // (the others read this block's memory)
         }
-        if (a.share) return;
+        if (!RUNS) return;
         __syncthreads();
-        pos += tile1 - f.off;
+        left -= tile1 - f.off;
+        f.off = 0;
+        if (++f.seg == a.c.Hkv * a.blocks) {
+            f.seg = 0, f.b++;
+            if (left > 0) f.n = (int)(sh.plan.before[f.b + 1] - sh.plan.before[f.b]);
+        }
     }
 }
 
 // One block: a column of a segment that several blocks shared; their parts are added in the order of the tiles.
-template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThreads) join_kernel(const AttnArgs a, int grid) {
-    constexpr int C = 8 * NT, LANES = D / 4, GROUPS = kAttnThreads / LANES;
+template <int D, int NT, bool F32> __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a) {
+    constexpr int kAttnThreads = 256, kWarps = 8, kUnit = unit_of(NT);
+    constexpr int C = 8 * NT, LANES = D / 4, GROUPS = kAttnThreads / LANES, grid = grid_of(NT);
     using T = std::conditional_t<F32, float, __nv_bfloat16>;
     __shared__ Plan plan;
     __shared__ float2 ml[kMaxGrid + 1];
+    __shared__ int slot[kMaxGrid + 1];
     __shared__ float4 ys[GROUPS][LANES];
     __shared__ float tops[kWarps], sums[kWarps];
-    pdl_trigger();
-    pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.c.Hkv * a.blocks, b = blockIdx.x / per, seg = blockIdx.x % per, c = blockIdx.y, rho = seg % a.blocks * C + c;
-    if (rho >= a.rows * a.heads) return;
+    if (rho >= a.rows * a.heads) {   // (every block waits: what comes after this kernel may count on the one before it)
+        pdl_wait();
+        return;
+    }
     make_plan(a, plan);
     const int64_t len = plan.before[b + 1] - plan.before[b], start = plan.before[b] * per + seg * len, total = plan.before[a.B] * per;
-    if (len < 2 * kUnit) return;   // (never cut)
-    auto cut = [&](int64_t i) { return cut_at(total * i / grid - start, len); };
+    auto cut = [&](int64_t i) { return cut_at<kUnit>((int64_t)((uint64_t)(total * i) / grid) - start, len); };
     // runs i0 .. i0 + count - 1 may hold a part of it
     const int i0 = (int)(start * grid / total), count = (int)min((int64_t)grid - 1, (start + len - 1) * grid / total + 1) - i0 + 1;
     int parts = 0;
-    float top = kLowest;
     for (int k0 = 0; k0 < count; k0 += kAttnThreads) {
         const int k = k0 + tid;
         const int64_t from = k < count ? cut(i0 + k) : 0, to = k < count ? cut(i0 + k + 1) : 0;
         parts += __syncthreads_count(from < to);
-        if (k < count) {
-            ml[k].x = kLowest, ml[k].y = 0.f;
-            if (from < to) ml[k] = *reinterpret_cast<const float2 *>(a.part + ((size_t)(2 * (i0 + k) + (from == 0)) * C + c) * (D + 4) + D);
-            top = fmaxf(top, ml[k].x);
-        }
+        if (k < count) slot[k] = from < to ? 2 * (i0 + k) + (from == 0) : -1;
     }
+    pdl_wait();
+    pdl_trigger();
     if (parts < 2) return;
+    __syncthreads();
+    float top = kLowest;
+    for (int k = tid; k < count; k += kAttnThreads) {
+        ml[k] = slot[k] < 0 ? make_float2(kLowest, 0.f) : __ldcg(reinterpret_cast<const float2 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + D));
+        top = fmaxf(top, ml[k].x);
+    }
     top = warp_max(top);
     if (lane == 0) tops[warp] = top;
     __syncthreads();
@@ -638,8 +774,7 @@ template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThread
     const int d = tid % LANES * 4;
 #pragma unroll 8
     for (int k = tid / LANES; k < count; k += GROUPS) {
-        const int64_t from = cut(i0 + k);
-        if (from < cut(i0 + k + 1)) add4(y, ex2(ml[k].x - top), __ldcg(reinterpret_cast<const float4 *>(a.part + ((size_t)(2 * (i0 + k) + (from == 0)) * C + c) * (D + 4) + d)));
+        if (slot[k] >= 0) add4(y, ex2(ml[k].x - top), __ldcg(reinterpret_cast<const float4 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + d)));
     }
     ys[tid / LANES][tid % LANES] = y;
     float sum = 0.f;
@@ -666,29 +801,32 @@ Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     w.nt = columns <= 8 ? 1 : 2;
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * ((columns + 8 * w.nt - 1) / (8 * w.nt));
     w.share = 1;
-    while (w.share < 8 && segments * w.share * 2 <= grid_of(w.nt) && w.share * kWarps < tiles) w.share *= 2;
+    while (w.share < 8 && segments * w.share * 2 <= grid_of(w.nt) && w.share * warps_of(w.nt) < tiles) w.share *= 2;
     if (segments * tiles > 64LL * grid_of(w.nt) || tiles > 64LL * w.share * 4) w.share = 0;
     return w;
 }
 
-template <int D, int G, int NT, bool F32> cudaError_t launch(cudaStream_t s, const AttnArgs &a, int64_t segments) {
-    constexpr int kSmem = sizeof(Shared<D, G, NT>);
-    auto kernel = attend_kernel<D, G, NT, F32>;
-    {
-        static std::atomic<uint64_t> done{0};
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
+template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(cudaStream_t s, const AttnArgs &a, int64_t segments) {
+    constexpr int kSmem = sizeof(Shared<D, G, NT, TT>) - (RUNS ? 0 : sizeof(Plan));
+    auto kernel = attend_kernel<D, G, NT, TT, RUNS, F32>;
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev > 63 || !(done.load(std::memory_order_acquire) >> dev & 1)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
-        if (dev > 63 || !(done.load(std::memory_order_acquire) >> dev & 1)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-            if (e != cudaSuccess) return e;
-            if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
-        }
+        if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
+    }
+    if (RUNS) {
+        launch_k(kernel, dim3(grid_of(NT)), dim3(32 * warps_of(NT)), kSmem, s, pdl_enabled(), a);
+        launch_k(join_kernel<D, NT, F32>, dim3((unsigned int)segments, 8 * NT), dim3(256), 0, s, pdl_enabled(), a);
+        return cudaGetLastError();
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.share ? (unsigned int)(segments * a.share) : grid_of(NT));
-    cfg.blockDim = dim3(kAttnThreads);
-    cfg.dynamicSmemBytes = a.share ? kSmem - sizeof(Plan) : kSmem;
+    cfg.gridDim = dim3((unsigned int)(segments * a.share));
+    cfg.blockDim = dim3(32 * warps_of(NT));
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int na = 0;
@@ -706,14 +844,14 @@ template <int D, int G, int NT, bool F32> cudaError_t launch(cudaStream_t s, con
     }
     cfg.attrs = attr;
     cfg.numAttrs = na;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
-    if (e != cudaSuccess) return e;
-    if (!a.share) launch_k(join_kernel<D, NT, F32>, dim3((unsigned int)segments, 8 * NT), dim3(kAttnThreads), 0, s, pdl_enabled(), a, grid_of(NT));
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+template <int D, int G, bool F32> cudaError_t launch_kind(cudaStream_t s, const AttnArgs &a, int nt, int64_t segments) {
+    if (nt == 1) return a.share ? launch<D, G, 1, 1, false, F32>(s, a, segments) : launch<D, G, 1, TT1, true, F32>(s, a, segments);
+    return a.share ? launch<D, G, 2, 1, false, F32>(s, a, segments) : launch<D, G, 2, TT2, true, F32>(s, a, segments);
 }
 template <int D, int G> cudaError_t launch_type(cudaStream_t s, const AttnArgs &a, bool f32, int nt, int64_t segments) {
-    if (nt == 1) return f32 ? launch<D, G, 1, true>(s, a, segments) : launch<D, G, 1, false>(s, a, segments);
-    return f32 ? launch<D, G, 2, true>(s, a, segments) : launch<D, G, 2, false>(s, a, segments);
+    return f32 ? launch_kind<D, G, true>(s, a, nt, segments) : launch_kind<D, G, false>(s, a, nt, segments);
 }
 
 }  // namespace kv4

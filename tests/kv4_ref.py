@@ -92,11 +92,11 @@ def values(codes, scales, zeros, group):
 
 def attend(q, k, v, n_ctx, n_rows, scale, visible=None):
     """q [B, R, H, D] (turned), k, v [B, n, Hkv, D] float64 on any device, -> out and what tolerances are made of: A = sum p |v| [B, R, H, D], and of
-    each row and head [B, R, H] the largest sum |q k| scale and the largest p |v|"""
+    each row and head [B, R, H] the largest sum |q k| scale, the largest p |v|, the largest (max |q|) sum |k| scale, and sum p max |v|"""
     B, R, H, D = q.shape
     share = H // k.shape[2]
     out, A = (torch.zeros(B, R, H, D, dtype=torch.float64, device=k.device) for _ in range(2))
-    S, most = (torch.zeros(B, R, H, dtype=torch.float64, device=k.device) for _ in range(2))
+    S, most, Q, M = (torch.zeros(B, R, H, dtype=torch.float64, device=k.device) for _ in range(4))
     for b in range(B):
         n = R if n_rows is None else min(max(int(n_rows[b]), 0), R)
         L = int(n_ctx[b])
@@ -117,17 +117,20 @@ def attend(q, k, v, n_ctx, n_rows, scale, visible=None):
             w = torch.softmax(x, -1)
             out[b, m], A[b, m] = torch.einsum("hp,phd->hd", w, vv), torch.einsum("hp,phd->hd", w, vv.abs())
             S[b, m] = scale * torch.einsum("hd,phd->hp", qq.abs(), kk.abs()).amax(-1)
-            most[b, m] = (w.t()[..., None] * vv.abs()).amax((0, 2))
-    return out, A, (S, most)
+            Q[b, m] = scale * qq.abs().amax(-1) * kk.abs().sum(-1).amax(0)
+            most[b, m], M[b, m] = (w.t()[..., None] * vv.abs()).amax((0, 2)), (w.t() * vv.abs().amax(-1)).sum(0)
+    return out, A, (S, most, Q, M)
 
 
-def bound(out, A, of_rows, n, D, dtype, turned):
-    """How far attend_rows may be: scores off by (2 D / 16 + 16) roundings of sums (matrix unit: one step of 2^-23 of the running sum each) and 2^-21 for
-    the queries' two fp16 terms (bf16 queries: one term, exact unless turned: 2^-11), exponentials by 2^-22, numerators by 2^-21 (bf16: 2^-11), and each by
-    2^-32 of the largest product with a value (a group's largest value is at least 7.5 scales, a code at most 15); sums over n
-    positions take two steps per 16 of them, and 64 for joining; the result is rounded to its type."""
-    S, most = of_rows
+def bound(out, A, of_rows, n, D, dtype):
+    """How far attend_rows may be.  Scores: whole numbers up to the scales; queries are off by half a step of 2^-22 (bf16: 2^-14) of their row's largest at most (the largest
+    is at least half of 127 * 65536, or 127 * 256, steps), and up to 4 groups' sums, two conversions and products are rounded to fp32: 16 * 2^-24.  Exponentials by
+    2^-22, numerators by 2^-21 (bf16: 2^-11) and each by 2^-28 of the largest product with a value (a group's largest value is at least 7.5 scales, a
+    code at most 15).  Sums over n positions take two steps per 16 of them, and 64 for joining (bf16: of codes less 8, at most 1.1 of the largest value each);
+    the result is rounded to its type."""
+    S, most, Q, M = of_rows
     f32 = dtype == torch.float32
-    dx = S * ((2 * D / 16 + 16) * 2.0 ** -23 + (2.0 ** -21 if f32 else 2.0 ** -11 if turned else 2.0 ** -22))
-    rel = 2 * dx + 2.0 ** -22 + (2.0 ** -21 if f32 else 2.0 ** -11) + (n / 8 + 64) * 2.0 ** -23
-    return A * rel[..., None] * (1 + 1e-3) + n * 2.0 ** -32 * most[..., None] + (2.0 ** -24 if f32 else 2.0 ** -8) * out.abs() + 1e-37
+    dx = S * 2.0 ** -20 + Q * 2.0 ** (-22 if f32 else -14)
+    steps = (n / 8 + 64) * 2.0 ** -23
+    rel = 2 * dx + 2.0 ** -22 + (2.0 ** -21 if f32 else 2.0 ** -11) + steps
+    return A * rel[..., None] * (1 + 1e-3) + (n * 2.0 ** -28 * most + (0 if f32 else steps * 1.1 * M))[..., None] + (2.0 ** -24 if f32 else 2.0 ** -8) * out.abs() + 1e-37

@@ -162,7 +162,7 @@ def test_pages_that_do_not_exist():
         # the same with the page's positions left out
         keep = list(range(16)) + list(range(32, 47))
         want, A, S = ref.attend(q.double(), gk[:, keep].double(), gv[:, keep].double(), [31], None, D ** -0.5)
-        assert ((out.double() - want).abs() <= ref.bound(want, A, S, 48, D, torch.float32, False)).all()
+        assert ((out.double() - want).abs() <= ref.bound(want, A, S, 48, D, torch.float32)).all()
         assert eesd.attend_rows(q, c, ints([[bad, bad, bad]]), ints([47])).eq(0).all()
 
 
@@ -206,10 +206,12 @@ def test_read_bounds():
             assert torch.equal(x, want)
 
 
-def check_attend(c, table, q, n_ctx, n_rows=None, visible=None, rope=None, positions=None, scale=None):
+def check_attend(c, table, q, n_ctx, n_rows=None, visible=None, rope=None, positions=None, scale=None, room=0):
+    """room: entries that the call's page table has to spare (what a call may hold decides how it is shared out)"""
     B, R, H, D = q.shape
     n = table.shape[1] * c.page_tokens
     k, v = c.read(table, n)
+    table = torch.nn.functional.pad(table, (0, room), value=-1)
     out = eesd.attend_rows(q, c, table, ints(n_ctx), n_rows=None if n_rows is None else ints(n_rows), scale=scale, visible=visible, rope=rope, positions=positions)
     assert out.dtype == q.dtype and out.shape == q.shape
     qq = q.float()
@@ -218,7 +220,7 @@ def check_attend(c, table, q, n_ctx, n_rows=None, visible=None, rope=None, posit
         where = np.array([[n_ctx[b] - own[b] + m for m in range(R)] for b in range(B)]) if positions is None else positions.cpu().numpy()
         qq = torch.from_numpy(ref.turn(qq.cpu().numpy(), rope, where)).cuda()
     want, A, S = ref.attend(qq, k.double(), v.double(), n_ctx, n_rows, scale or D ** -0.5, visible)
-    tol = ref.bound(want, A, S, n, D, q.dtype, rope is not None)
+    tol = ref.bound(want, A, S, n, D, q.dtype)
     off = (out.double() - want).abs()
     assert (off <= tol).all(), (float((off / tol.clamp(min=1e-300)).nan_to_num().max()), float(off.max()))
     again = eesd.attend_rows(q, c, table, ints(n_ctx), n_rows=None if n_rows is None else ints(n_rows), scale=scale, visible=visible, rope=rope, positions=positions)
@@ -237,7 +239,8 @@ def test_attend(B, R, H, Hkv, page, n, D, group, a):
     c.append(k, v, table, ints([0] * B), rope=rope)
     q = torch.randn(B, R, H, D, generator=gen(n + 1), device="cuda").to(DT[a])
     n_ctx = [max(1, n - 11 * b) for b in range(B)]
-    check_attend(c, table, q, n_ctx, rope=rope)
+    for room in (0, 30000):
+        check_attend(c, table, q, n_ctx, rope=rope, room=room)
 
 
 @pytest.mark.parametrize("a", ["f32", "bf16"])
