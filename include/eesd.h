@@ -610,9 +610,18 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  * Arithmetic: sums, maxima and exponentials are fp32.  A row and head's queries are taken as whole numbers of 24 bits (dtype EESD_BF16: 16) under a power of
  * two: off by at most 2^-22 (2^-14) of the largest; their products with codes are exact.  A softmax numerator times its value's scale is taken as two fp16 terms
  * (EESD_BF16: one): off by at most 2^-22 (2^-11) of itself, or 2^-29 of the row's largest.  A row of queries that holds a NaN or an infinity gives NaN. */
-size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads, int dtype);
-int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *q,
-                    int n_heads, float scale, const int32_t *visible, void *out, void *scratch, size_t scratch_bytes);
+typedef struct eesd_kv4_attention {
+    eesd_kv4_rows rows;
+    eesd_kv4_tensor q;
+    const int32_t *visible;    /* [B][rows]; NULL: a chain                                            */
+    void *out;
+    void *scratch;
+    size_t scratch_bytes;
+    int32_t dtype, n_heads;
+    float scale;               /* > 0                                                                 */
+} eesd_kv4_attention;
+size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads);
+int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_attention *call);
 
 #ifdef __cplusplus
 }

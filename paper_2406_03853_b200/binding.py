@@ -179,8 +179,8 @@ def lib():
         L.eesd_kv4_append.argtypes = [vp, vp, vp, sz, vp, C.c_int, vp, vp]
         L.eesd_kv4_read.argtypes = [vp, vp, vp, sz, vp, vp, C.c_int, vp, vp]
         L.eesd_kv4_attend_scratch_bytes.restype = sz
-        L.eesd_kv4_attend_scratch_bytes.argtypes = [vp, vp, C.c_int, C.c_int]
-        L.eesd_kv4_attend.argtypes = [vp, vp, vp, sz, vp, C.c_int, vp, C.c_int, C.c_float, vp, vp, vp, sz]
+        L.eesd_kv4_attend_scratch_bytes.argtypes = [vp, vp, C.c_int]
+        L.eesd_kv4_attend.argtypes = [vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -881,14 +881,9 @@ def process_logits(logits: torch.Tensor, rules: LogitRules, out: Optional[torch.
 
 
 # ---- key / value cache in 4 bits
-_kv4_rows = struct.Struct("PqiiiiPPPP").pack      # eesd_kv4_rows
-_kv4_tensor = struct.Struct("Pqqq").pack          # eesd_kv4_tensor
-
-
-def _kv4_vector(t, name: str, B: int, index: int) -> int:
-    if not isinstance(t, torch.Tensor) or t.dtype is not _I32 or not t.is_cuda or t.get_device() != index or t.shape != (B,) or not t.is_contiguous():
-        raise ValueError(f"{name}: wanted a contiguous tensor of torch.int32 [{B}] on device {index}")
-    return t.data_ptr()
+_kv4_rows = struct.Struct("PqiiiiPPPP").pack                       # eesd_kv4_rows
+_kv4_tensor = struct.Struct("Pqqq").pack                           # eesd_kv4_tensor
+_kv4_attention = struct.Struct("PqiiiiPPPPPqqqPPPNiif4x").pack     # eesd_kv4_attention
 
 
 class KV4Cache:
@@ -911,44 +906,57 @@ class KV4Cache:
         if buffer.dim() != 1 or not buffer.is_contiguous() or buffer.numel() < self.layout.total_bytes:
             raise ValueError(f"buffer: wanted {self.layout.total_bytes} contiguous bytes")
         self.buffer, self._ptr, self._bytes = buffer, buffer.data_ptr(), buffer.numel()
+        self._scratch = {}   # (B, rows, heads, pages) -> bytes of scratch memory that attend_rows takes
 
     @property
     def device(self) -> torch.device:
         return self.buffer.device
 
-    def _rows(self, page_table, B: int, rows: int, at, at_name: str, n_rows, rope, positions) -> bytes:
-        """eesd_kv4_rows of a call, its tensors checked"""
-        index = self._index
-        if not isinstance(page_table, torch.Tensor) or page_table.dtype is not _I32 or not page_table.is_cuda or page_table.get_device() != index:
-            raise ValueError(f"page_table: wanted a tensor of torch.int32 on device {index}")
-        if page_table.dim() != 2 or page_table.shape[0] != B or page_table.shape[1] < 1 or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
-            raise ValueError(f"page_table: wanted [{B}, pages] with the pages of a sequence next to each other")
-        pages = page_table.shape[1]
-        stride = page_table.stride(0) if B > 1 else pages
-        if stride < pages:
-            raise ValueError("page_table: the tables of two sequences overlap")
+    def _ints(self, t, name: str, shape) -> int:
+        """The address of a contiguous int32 tensor of that shape on the cache's device."""
+        if not isinstance(t, torch.Tensor) or t.dtype is not _I32 or t.shape != shape or not t.is_cuda or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"{name}: wanted a contiguous tensor of torch.int32 {list(shape)} on device {self._index}")
+        return t.data_ptr()
+
+    def _rows(self, page_table, B: int, rows: int, at, at_name: str, n_rows, rope, positions):
+        """The fields of a call's eesd_kv4_rows, its tensors checked."""
+        if not isinstance(page_table, torch.Tensor) or page_table.dtype is not _I32 or not page_table.is_cuda or page_table.get_device() != self._index:
+            raise ValueError(f"page_table: wanted a tensor of torch.int32 on device {self._index}")
+        shape = page_table.shape
+        if len(shape) != 2 or shape[0] != B or shape[1] < 1:
+            raise ValueError(f"page_table: wanted [{B}, pages]")
+        pages = stride = shape[1]
+        if not page_table.is_contiguous():
+            s = page_table.stride()
+            if (s[1] != 1 and pages > 1) or (B > 1 and s[0] < pages):
+                raise ValueError("page_table: the pages of a sequence lie next to each other, and no two tables overlap")
+            if B > 1:
+                stride = s[0]
         n_rope = rope_ptr = pos_ptr = 0
         if rope is not None:
-            _check_tensor(rope, "rope", (_F32,), index)
-            if rope.dim() != 3 or rope.shape[0] < 1 or rope.shape[1] != self.head_dim // 2 or rope.shape[2] != 2 or not rope.is_contiguous():
+            if not isinstance(rope, torch.Tensor) or rope.dtype is not _F32 or not rope.is_cuda or rope.get_device() != self._index:
+                raise ValueError(f"rope: wanted a tensor of torch.float32 on device {self._index}")
+            shape = rope.shape
+            if len(shape) != 3 or shape[0] < 1 or shape[1] != self.head_dim >> 1 or shape[2] != 2 or not rope.is_contiguous():
                 raise ValueError(f"rope: wanted contiguous [positions, {self.head_dim // 2}, 2]")
-            n_rope, rope_ptr = rope.shape[0], rope.data_ptr()
+            n_rope, rope_ptr = shape[0], rope.data_ptr()
         if positions is not None:
-            _check_tensor(positions, "positions", (_I32,), index)
-            if positions.shape != (B, rows) or not positions.is_contiguous():
-                raise ValueError(f"positions: wanted contiguous [{B}, {rows}]")
-            pos_ptr = positions.data_ptr()
-        return _kv4_rows(page_table.data_ptr(), stride, pages, B, rows, n_rope, 0 if at is None else _kv4_vector(at, at_name, B, index),
-                         0 if n_rows is None else _kv4_vector(n_rows, "n_rows", B, index), rope_ptr, pos_ptr)
+            pos_ptr = self._ints(positions, "positions", (B, rows))
+        return (page_table.data_ptr(), stride, pages, B, rows, n_rope, 0 if at is None else self._ints(at, at_name, (B,)),
+                0 if n_rows is None else self._ints(n_rows, "n_rows", (B,)), rope_ptr, pos_ptr)
 
-    def _tensor(self, t, name: str, dtypes, heads: Optional[int] = None) -> bytes:
-        """eesd_kv4_tensor of [B, rows, heads, head_dim]"""
-        _check_tensor(t, name, dtypes, self._index)
+    def _tensor(self, t, name: str, heads: int = 0):
+        """The fields of an eesd_kv4_tensor: [B, rows, heads, head_dim] fp32 or bf16, and its shape."""
+        if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or not t.is_cuda or t.get_device() != self._index:
+            raise ValueError(f"{name}: wanted a tensor of torch.float32 or torch.bfloat16 on device {self._index}")
         shape = t.shape
-        if len(shape) != 4 or shape[3] != self.head_dim or t.stride(3) != 1 or not shape[0] or not shape[1] or not shape[2] or (heads and shape[2] != heads):
-            raise ValueError(f"{name}: wanted [B, rows, {heads or 'heads'}, {self.head_dim}] with a head's values next to each other")
-        s = t.stride()
-        return _kv4_tensor(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+        if len(shape) != 4 or shape[3] != self.head_dim or not t.numel() or (heads and shape[2] != heads):
+            raise ValueError(f"{name}: wanted [B, rows, {heads or 'heads'}, {self.head_dim}]")
+        s0, s1, s2, s3 = t.stride()
+        if s3 != 1:
+            raise ValueError(f"{name}: a head's values lie next to each other")
+        B, rows, H, _ = shape
+        return (t.data_ptr(), s0 if B > 1 else 0, s1 if rows > 1 else 0, s2 if H > 1 else 0), B, rows, H
 
     def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, start: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
                rope: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None) -> None:
@@ -956,13 +964,15 @@ class KV4Cache:
         positions start[b] + m.  start, n_rows [B] int32: the first row's position, and how many of the rows a sequence has (left out: all), read on
         the device.  rope [positions, head_dim / 2, 2] fp32: (cos, sin) by which the keys are turned first, at the rows' places or at
         positions [B, rows] int32.  No two rows of a call may have the same place."""
-        kt, vt = self._tensor(k, "k", _DTYPES, self.n_kv_heads), self._tensor(v, "v", (k.dtype,), self.n_kv_heads)
-        if v.shape != k.shape:
-            raise ValueError("k and v: wanted the same shape")
+        kt, B, rows, _ = self._tensor(k, "k", self.n_kv_heads)
+        vt, *shape = self._tensor(v, "v", self.n_kv_heads)
+        if v.dtype is not k.dtype or shape[0] != B or shape[1] != rows:
+            raise ValueError("k and v: wanted the same shape and type")
         if start is None:
             raise ValueError("start: wanted a tensor")
-        r = self._rows(page_table, k.shape[0], k.shape[1], start, "start", n_rows, rope, positions)
-        _call(lib().eesd_kv4_append, "eesd_kv4_append", self._index, self._desc_ptr, self._ptr, self._bytes, r, _DTYPES[k.dtype], kt, vt)
+        r = self._rows(page_table, B, rows, start, "start", n_rows, rope, positions)
+        _call(lib().eesd_kv4_append, "eesd_kv4_append", self._index, self._desc_ptr, self._ptr, self._bytes, _kv4_rows(*r), _DTYPES[k.dtype], _kv4_tensor(*kt),
+              _kv4_tensor(*vt))
 
     def read(self, page_table: torch.Tensor, count: int, start: Optional[torch.Tensor] = None, n_ctx: Optional[torch.Tensor] = None,
              dtype: torch.dtype = torch.float32):
@@ -976,11 +986,12 @@ class KV4Cache:
         if count < 1:
             raise ValueError("count: at least one position")
         r = self._rows(page_table, B, count, start, "start", None, None, None)
-        n = None if n_ctx is None else _kv4_vector(n_ctx, "n_ctx", B, self._index)
-        k = self.buffer.new_empty((B, count, self.n_kv_heads, self.head_dim), dtype=dtype)
-        v = torch.empty_like(k)
-        _call(lib().eesd_kv4_read, "eesd_kv4_read", self._index, self._desc_ptr, self._ptr, self._bytes, r, n, _DTYPES[dtype], k.data_ptr(), v.data_ptr())
-        return k, v
+        n = None if n_ctx is None else self._ints(n_ctx, "n_ctx", (B,))
+        both = self.buffer.new_empty((2, B, count, self.n_kv_heads, self.head_dim), dtype=dtype)
+        at = both.data_ptr()
+        _call(lib().eesd_kv4_read, "eesd_kv4_read", self._index, self._desc_ptr, self._ptr, self._bytes, _kv4_rows(*r), n, _DTYPES[dtype], at,
+              at + (both.nbytes >> 1))
+        return both.unbind()
 
 
 def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ctx: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
@@ -993,41 +1004,35 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
     page_table are read on the device.  out, scratch: contiguous, made for the call when left out; calls that may overlap need their own."""
     if not isinstance(cache, KV4Cache):
         raise ValueError("cache: wanted a KV4Cache")
-    index, D = cache._index, cache.head_dim
-    qt = cache._tensor(q, "q", _DTYPES)
-    B, rows, H, _ = q.shape
+    qt, B, rows, H = cache._tensor(q, "q")
     if rows > MAX_ROWS:
         raise ValueError(f"q: 1 to {MAX_ROWS} rows, not {rows}")
     if H % cache.n_kv_heads:
         raise ValueError(f"q: {H} heads do not share {cache.n_kv_heads}")
     if n_ctx is None:
         raise ValueError("n_ctx: wanted a tensor")
+    index = cache._index
     r = cache._rows(page_table, B, rows, n_ctx, "n_ctx", n_rows, rope, positions)
-    vis = None
-    if visible is not None:
-        _check_tensor(visible, "visible", (_I32,), index)
-        if visible.shape != (B, rows) or not visible.is_contiguous():
-            raise ValueError(f"visible: wanted contiguous [{B}, {rows}]")
-        vis = visible.data_ptr()
-    if scale is None:
-        scale = D ** -0.5
-    dt = _DTYPES[q.dtype]
-    L, ptr = lib(), None
+    vis = 0 if visible is None else cache._ints(visible, "visible", (B, rows))
+    L, ptr = lib(), 0
     if scratch is not None:
         _check_tensor(scratch, "scratch", (_U8,), index)
         if not scratch.is_contiguous():
             raise ValueError("scratch: wanted contiguous")
         ptr, size = scratch.data_ptr(), scratch.numel()
     else:
-        size = L.eesd_kv4_attend_scratch_bytes(cache._desc_ptr, r, H, dt)
+        size = cache._scratch.get((B, rows, H, r[2]))
+        if size is None:
+            size = cache._scratch[B, rows, H, r[2]] = L.eesd_kv4_attend_scratch_bytes(cache._desc_ptr, _kv4_rows(*r), H)
         if size:
-            scratch = q.new_empty(size, dtype=_U8)
+            scratch = cache.buffer.new_empty(size)
             ptr = scratch.data_ptr()
     if out is None:
-        out = q.new_empty((B, rows, H, D))
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     else:
         _check_tensor(out, "out", (q.dtype,), index)
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out: wanted contiguous, of q's shape")
-    _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, r, dt, qt, H, scale, vis, out.data_ptr(), ptr, size)
+    call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, cache.head_dim ** -0.5 if scale is None else scale)
+    _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, call)
     return out

@@ -28,22 +28,10 @@ namespace kv4 {
 
 namespace cg = cooperative_groups;
 
-#ifndef TT1
-#define TT1 2
-#endif
-#ifndef NB2
-#define NB2 2
-#endif
-#ifndef NW2
-#define NW2 6
-#endif
-#ifndef TT2
-#define TT2 1
-#endif
-__host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : NW2; }
-__host__ __device__ constexpr int unit_of(int nt) { return 2 * warps_of(nt); }   // runs: tiles between the places where a segment may be cut
+constexpr int kWarps = 8, kAttnThreads = kWarps * 32;
+constexpr int kUnit = 2 * kWarps;   // runs: tiles between the places where a segment may be cut
 constexpr int kMaxGrid = 296;
-__host__ __device__ constexpr int grid_of(int nt) { return nt == 1 ? kMaxGrid : kMaxGrid / 2 * NB2; }   // blocks that fit the machine's 148 multiprocessors at once
+__host__ __device__ constexpr int grid_of(int nt) { return nt == 1 ? kMaxGrid : kMaxGrid / 2; }   // blocks that fit the machine's 148 multiprocessors at once
 constexpr int kRise = 8;     // a running maximum is let fall behind by this much (powers of two)
 constexpr float kLowest = -3.402823466e38f;
 
@@ -59,7 +47,9 @@ struct AttnArgs {
     int B, rows, heads;  // heads: query heads of a key head
     int blocks;          // column blocks of a key head
     int share;           // blocks of a cluster (runs: 0)
-    float *part;         // runs: [2 * grid][columns][D + 4]: outputs, maximum, sum
+    int4 *head;          // runs: of each block, the sequence and segment that it began and left to the next ones (-1: none), and what it did of the one
+                         // that it found begun: 0 nothing, 1 some, 2 its end
+    float *part;         // runs: [2 * grid][columns][D + 4]: outputs, maximum, sum; of what a block found begun, and of what it left
 };
 
 __device__ __forceinline__ int rows_of(const AttnArgs &a, int b) { return a.n_rows ? min(max(a.n_rows[b], 0), a.rows) : a.rows; }
@@ -71,67 +61,76 @@ __device__ __forceinline__ int tiles_of(const AttnArgs &a, int b) {
 
 // ---------------------------------------------------------------------------------- runs
 // A cut inside a segment lies at a multiple of kUnit tiles, and at an end where fewer than that would be left.
-template <int kUnit> __device__ __forceinline__ int64_t cut_at(int64_t off, int64_t n) {
+__device__ __forceinline__ int64_t cut_at(int64_t off, int64_t n) {
     if (off <= 0) return 0;
     if (off >= n) return n;
     const int64_t c = (off + kUnit / 2) / kUnit * kUnit;
     return c + kUnit > n ? n : c;
 }
-struct Plan {
-    int64_t before[EESD_KV4_MAX_BATCH + 1];   // tiles of the sequences before (of one key head and column block)
-};
-__device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p) {
-    if (threadIdx.x < 32) {
-        int64_t sum = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 32) {
-            const int b = b0 + threadIdx.x;
-            int64_t v = b < a.B ? tiles_of(a, b) : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
-                if ((int)threadIdx.x >= o) v += u;
-            }
-            if (b < a.B) p.before[b + 1] = sum + v;
-            sum += __shfl_sync(0xffffffffu, v, 31);
-        }
-        if (threadIdx.x == 0) p.before[0] = 0;
-    }
-    __syncthreads();
-}
 struct Place {
     int b, seg;    // sequence; key head * blocks + column block
     int off, n;    // tile in the segment, of n
 };
-__device__ __forceinline__ Place find(const AttnArgs &a, const Plan &p, int64_t pos) {
-    const int64_t per = (int64_t)a.c.Hkv * a.blocks;
-    int lo = 0, hi = a.B;   // before[lo] * per <= pos < before[hi] * per
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.before[mid] * per <= pos) lo = mid; else hi = mid;
-    }
-    Place r;
-    r.b = lo;
-    r.n = (int)(p.before[lo + 1] - p.before[lo]);
-    const uint64_t in = (uint64_t)(pos - p.before[lo] * per);
-    r.seg = in >> 32 ? (int)(in / (uint32_t)r.n) : (int)((uint32_t)in / (uint32_t)r.n);
-    r.off = (int)(in - (uint64_t)r.seg * r.n);
-    return r;
-}
-// the tiles that the blocks before block i of GRID take, and where its run begins
-template <int GRID, int UNIT> __device__ __forceinline__ int64_t run_start(const AttnArgs &a, const Plan &p, int i, Place &f) {
-    const int64_t total = p.before[a.B] * a.c.Hkv * a.blocks, raw = (int64_t)((uint64_t)(total * i) / GRID);
-    if (raw >= total) return total;
-    f = find(a, p, raw);
-    const int64_t cut = cut_at<UNIT>(f.off, f.n), at = raw - f.off + cut;
-    f.off = (int)cut;
-    if (f.off == f.n) {   // (the next segment's first)
-        f.off = 0;
-        if (++f.seg == a.c.Hkv * a.blocks) {
-            f.seg = 0, f.b++;
-            if (f.b < a.B) f.n = (int)(p.before[f.b + 1] - p.before[f.b]);
+struct Plan {
+    int tiles[EESD_KV4_MAX_BATCH];   // of a segment of each sequence
+    Place begin;                     // where the block's run begins
+    int64_t count;                   // how many tiles it takes
+};
+// The run of block `block` of `grid`, worked out by the first warp.
+__device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block, int grid) {
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        const int64_t per = (int64_t)a.c.Hkv * a.blocks;
+        int64_t total = 0;
+        for (int b = lane; b < a.B; b += 32) total += p.tiles[b] = tiles_of(a, b);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        total *= per;
+        __syncwarp();
+        // lane 0 .. 31: the sequences 32 i + lane; the one whose tiles hold a run's end says where
+        Place f = {a.B, 0, 0, 1};
+        int64_t at[2];
+#pragma unroll
+        for (int end = 0; end < 2; end++) {
+            const int64_t raw = total * (block + end) / grid;
+            int64_t before = 0;   // tiles of one head and column block up to the chunk
+            at[end] = total;
+            for (int b0 = 0; b0 < a.B; b0 += 32) {
+                const int n = b0 + lane < a.B ? p.tiles[b0 + lane] : 0;
+                int64_t sum = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t u = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += u;
+                }
+                const int64_t in = raw - (before + sum - n) * per;   // tiles past the start of the lane's sequence
+                const bool here = n > 0 && in >= 0 && in < n * per;
+                int64_t start = 0;
+                if (here) {
+                    int seg = (uint64_t)in >> 32 ? (int)(in / n) : (int)((uint32_t)in / (uint32_t)n);
+                    const int off = (int)(in - (int64_t)seg * n);
+                    int cut = (int)cut_at(off, n);
+                    start = raw - off + cut;
+                    int b = b0 + lane;
+                    if (cut == n) {   // (the next segment's first)
+                        cut = 0;
+                        if (++seg == per) seg = 0, b++;
+                    }
+                    f = Place{b, seg, cut, b < a.B ? p.tiles[b] : 1};
+                }
+                const uint32_t who = __ballot_sync(0xffffffffu, here);
+                if (who) {
+                    const int from = __ffs(who) - 1;
+                    at[end] = __shfl_sync(0xffffffffu, start, from);
+                    if (end == 0 && lane == from) p.begin = f;
+                    break;
+                }
+                before += __shfl_sync(0xffffffffu, sum, 31);
+            }
         }
+        if (lane == 0) p.count = at[1] - at[0];
     }
-    return at;
+    __syncthreads();
 }
 
 // ---------------------------------------------------------------------------------- pieces
@@ -207,7 +206,7 @@ template <int D, typename T> __device__ __forceinline__ void store_out(const Att
 }
 
 template <int D, int G, int NT, int TT> struct Shared {
-    static constexpr int C = 8 * NT, kWarps = warps_of(NT), STAGES = TT == 1 ? 4 : 2;   // STAGES: steps of a warp's ring
+    static constexpr int C = 8 * NT, STAGES = TT == 1 ? 4 : 2;   // STAGES: steps of a warp's ring
     union {
         unsigned char ring[kWarps][STAGES][TT * Tile<D, G>::BYTES];
         float o[kWarps][C][D + 4];   // the warps' outputs
@@ -221,15 +220,12 @@ template <int D, int G, int NT, int TT> struct Shared {
     float alpha[C];         // what a unit of its scores is worth
     float2 ml_all[C];       // the block's
     float y[C][D];
-    Place begin;            // runs: where the block begins, and how many tiles it takes
-    int64_t count[2];
     Plan plan;              // (runs alone; last)
 };
 
-template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __launch_bounds__(32 * warps_of(NT), NT == 1 ? 2 : NB2) attend_kernel(const AttnArgs a) {
+template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __launch_bounds__(kAttnThreads, NT == 1 ? 2 : 1) attend_kernel(const AttnArgs a) {
     using L = Tile<D, G>;
     constexpr int J = D / 32, W = D / 64, C = 8 * NT, HALF = D / 2, kStages = Shared<D, G, NT, TT>::STAGES;
-    constexpr int kWarps = warps_of(NT), kAttnThreads = 32 * kWarps;
     using T = std::conditional_t<F32, float, __nv_bfloat16>;
     extern __shared__ __align__(16) unsigned char raw[];
     using S = Shared<D, G, NT, TT>;
@@ -238,17 +234,15 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
     Pair base;
     asm volatile("mov.b32 %0, 0x64006400;" : "=r"(base.low));
     asm volatile("mov.b32 %0, 0x54005400;" : "=r"(base.high));
+    pdl_trigger();
     pdl_wait();
-    pdl_trigger();   // (after the wait: the joining kernel reads the lengths before its own)
     Place f;
     int64_t left = 1;   // runs: tiles to do
     if constexpr (RUNS) {
-        make_plan(a, sh.plan);
-        if (tid < 2) sh.count[tid] = run_start<grid_of(NT), unit_of(NT)>(a, sh.plan, blockIdx.x + tid, f);
-        if (tid == 0) sh.begin = f;
-        __syncthreads();
-        f = sh.begin;
-        left = sh.count[1] - sh.count[0];
+        make_plan(a, sh.plan, blockIdx.x, grid_of(NT));
+        f = sh.plan.begin;
+        left = sh.plan.count;
+        if (tid == 0) a.head[blockIdx.x] = make_int4(-1, 0, 0, 0);
     } else {
         const int seg = blockIdx.x / a.share, per = a.c.Hkv * a.blocks;
         f.b = seg / per;
@@ -718,51 +712,53 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             cluster.sync();   // (the others read this block's memory)
         }
         if (!RUNS) return;
+        if (tid == 0 && !all) {
+            if (f.off) a.head[blockIdx.x].z = tile1 == f.n ? 2 : 1;
+            else a.head[blockIdx.x].x = b, a.head[blockIdx.x].y = f.seg;
+        }
         __syncthreads();
         left -= tile1 - f.off;
         f.off = 0;
         if (++f.seg == a.c.Hkv * a.blocks) {
             f.seg = 0, f.b++;
-            if (left > 0) f.n = (int)(sh.plan.before[f.b + 1] - sh.plan.before[f.b]);
+            if (left > 0) f.n = sh.plan.tiles[f.b];
         }
     }
 }
 
-// One block: a column of a segment that several blocks shared; their parts are added in the order of the tiles.
-template <int D, int NT, bool F32> __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a) {
-    constexpr int kAttnThreads = 256, kWarps = 8, kUnit = unit_of(NT);
-    constexpr int C = 8 * NT, LANES = D / 4, GROUPS = kAttnThreads / LANES, grid = grid_of(NT);
+// One block: a column of the segment that block blockIdx.x of the runs began and left; the parts are added in the order of the tiles.
+template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThreads) join_kernel(const AttnArgs a) {
+    constexpr int C = 8 * NT, LANES = D / 4, GROUPS = kAttnThreads / LANES, GRID = grid_of(NT);
     using T = std::conditional_t<F32, float, __nv_bfloat16>;
-    __shared__ Plan plan;
-    __shared__ float2 ml[kMaxGrid + 1];
-    __shared__ int slot[kMaxGrid + 1];
+    __shared__ int slot[GRID + 1];
+    __shared__ int parts_of;
+    __shared__ float2 ml[GRID + 1];
     __shared__ float4 ys[GROUPS][LANES];
     __shared__ float tops[kWarps], sums[kWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = a.c.Hkv * a.blocks, b = blockIdx.x / per, seg = blockIdx.x % per, c = blockIdx.y, rho = seg % a.blocks * C + c;
-    if (rho >= a.rows * a.heads) {   // (every block waits: what comes after this kernel may count on the one before it)
-        pdl_wait();
-        return;
-    }
-    make_plan(a, plan);
-    const int64_t len = plan.before[b + 1] - plan.before[b], start = plan.before[b] * per + seg * len, total = plan.before[a.B] * per;
-    auto cut = [&](int64_t i) { return cut_at<kUnit>((int64_t)((uint64_t)(total * i) / grid) - start, len); };
-    // runs i0 .. i0 + count - 1 may hold a part of it
-    const int i0 = (int)(start * grid / total), count = (int)min((int64_t)grid - 1, (start + len - 1) * grid / total + 1) - i0 + 1;
-    int parts = 0;
-    for (int k0 = 0; k0 < count; k0 += kAttnThreads) {
-        const int k = k0 + tid;
-        const int64_t from = k < count ? cut(i0 + k) : 0, to = k < count ? cut(i0 + k + 1) : 0;
-        parts += __syncthreads_count(from < to);
-        if (k < count) slot[k] = from < to ? 2 * (i0 + k) + (from == 0) : -1;
-    }
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.y;
     pdl_wait();
     pdl_trigger();
-    if (parts < 2) return;
+    const int4 head = a.head[blockIdx.x];
+    const int b = head.x, seg = head.y, rho = seg % a.blocks * C + c;
+    if (b < 0 || rho >= a.rows * a.heads) return;
+    if (warp == 0) {
+        int parts = 1;
+        if (lane == 0) slot[0] = 2 * blockIdx.x + 1;
+        for (int i0 = blockIdx.x + 1; i0 < GRID; i0 += 32) {
+            const int does = i0 + lane < GRID ? a.head[i0 + lane].z : 0;
+            const uint32_t ends = __ballot_sync(0xffffffffu, does == 2), upto = ends ? (ends & -ends) * 2 - 1 : 0xffffffffu;
+            const uint32_t some = __ballot_sync(0xffffffffu, does != 0) & upto;
+            if (some >> lane & 1) slot[parts + __popc(some & ((1u << lane) - 1))] = 2 * (i0 + lane);
+            parts += __popc(some);
+            if (ends) break;
+        }
+        if (lane == 0) parts_of = parts;
+    }
     __syncthreads();
+    const int parts = parts_of;
     float top = kLowest;
-    for (int k = tid; k < count; k += kAttnThreads) {
-        ml[k] = slot[k] < 0 ? make_float2(kLowest, 0.f) : __ldcg(reinterpret_cast<const float2 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + D));
+    for (int k = tid; k < parts; k += kAttnThreads) {
+        ml[k] = *reinterpret_cast<const float2 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + D);
         top = fmaxf(top, ml[k].x);
     }
     top = warp_max(top);
@@ -773,12 +769,11 @@ template <int D, int NT, bool F32> __global__ void __launch_bounds__(256) join_k
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     const int d = tid % LANES * 4;
 #pragma unroll 8
-    for (int k = tid / LANES; k < count; k += GROUPS) {
-        if (slot[k] >= 0) add4(y, ex2(ml[k].x - top), __ldcg(reinterpret_cast<const float4 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + d)));
-    }
+    for (int k = tid / LANES; k < parts; k += GROUPS)
+        add4(y, ex2(ml[k].x - top), *reinterpret_cast<const float4 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + d));
     ys[tid / LANES][tid % LANES] = y;
     float sum = 0.f;
-    for (int k = tid; k < count; k += kAttnThreads) sum = fmaf(ex2(ml[k].x - top), ml[k].y, sum);
+    for (int k = tid; k < parts; k += kAttnThreads) sum = fmaf(ex2(ml[k].x - top), ml[k].y, sum);
     sum = warp_sum(sum);
     if (lane == 0) sums[warp] = sum;
     __syncthreads();
@@ -801,10 +796,12 @@ Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     w.nt = columns <= 8 ? 1 : 2;
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * ((columns + 8 * w.nt - 1) / (8 * w.nt));
     w.share = 1;
-    while (w.share < 8 && segments * w.share * 2 <= grid_of(w.nt) && w.share * warps_of(w.nt) < tiles) w.share *= 2;
+    while (w.share < 8 && segments * w.share * 2 <= grid_of(w.nt) && w.share * kWarps < tiles) w.share *= 2;
     if (segments * tiles > 64LL * grid_of(w.nt) || tiles > 64LL * w.share * 4) w.share = 0;
     return w;
 }
+
+size_t scratch_of(const eesd_kv4 *c, const Way &w) { return w.share ? 0 : (size_t)grid_of(w.nt) * (16 + 2 * 8 * w.nt * (c->head_dim + 4) * 4); }
 
 template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(cudaStream_t s, const AttnArgs &a, int64_t segments) {
     constexpr int kSmem = sizeof(Shared<D, G, NT, TT>) - (RUNS ? 0 : sizeof(Plan));
@@ -819,13 +816,13 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(
         if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
     }
     if (RUNS) {
-        launch_k(kernel, dim3(grid_of(NT)), dim3(32 * warps_of(NT)), kSmem, s, pdl_enabled(), a);
-        launch_k(join_kernel<D, NT, F32>, dim3((unsigned int)segments, 8 * NT), dim3(256), 0, s, pdl_enabled(), a);
+        launch_k(kernel, dim3(grid_of(NT)), dim3(kAttnThreads), kSmem, s, pdl_enabled(), a);
+        launch_k(join_kernel<D, NT, F32>, dim3(grid_of(NT), 8 * NT), dim3(kAttnThreads), 0, s, pdl_enabled(), a);
         return cudaGetLastError();
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned int)(segments * a.share));
-    cfg.blockDim = dim3(32 * warps_of(NT));
+    cfg.blockDim = dim3(kAttnThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -847,8 +844,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 template <int D, int G, bool F32> cudaError_t launch_kind(cudaStream_t s, const AttnArgs &a, int nt, int64_t segments) {
-    if (nt == 1) return a.share ? launch<D, G, 1, 1, false, F32>(s, a, segments) : launch<D, G, 1, TT1, true, F32>(s, a, segments);
-    return a.share ? launch<D, G, 2, 1, false, F32>(s, a, segments) : launch<D, G, 2, TT2, true, F32>(s, a, segments);
+    if (nt == 1) return a.share ? launch<D, G, 1, 1, false, F32>(s, a, segments) : launch<D, G, 1, 2, true, F32>(s, a, segments);
+    return a.share ? launch<D, G, 2, 1, false, F32>(s, a, segments) : launch<D, G, 2, 2, true, F32>(s, a, segments);
 }
 template <int D, int G> cudaError_t launch_type(cudaStream_t s, const AttnArgs &a, bool f32, int nt, int64_t segments) {
     return f32 ? launch_kind<D, G, true>(s, a, nt, segments) : launch_kind<D, G, false>(s, a, nt, segments);
@@ -861,44 +858,46 @@ using namespace eesd;
 
 extern "C" {
 
-size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads, int dtype) {
+size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     eesd_kv4_layout l;
-    if (eesd_kv4_layout_of(c, &l) || !r || r->max_pages < 1 || r->rows < 1 || r->rows > EESD_MAX_ROWS) return 0;
-    if (n_heads < 1 || n_heads % c->n_kv_heads || (dtype != EESD_F32 && dtype != EESD_BF16) || r->B < 1) return 0;
-    const kv4::Way w = kv4::way_of(c, r, n_heads);
-    return w.share ? 0 : (size_t)2 * kv4::grid_of(w.nt) * 8 * w.nt * (c->head_dim + 4) * 4;
+    if (eesd_kv4_layout_of(c, &l) || !r || r->B < 1 || r->max_pages < 1 || r->rows < 1 || r->rows > EESD_MAX_ROWS) return 0;
+    if (n_heads < 1 || n_heads % c->n_kv_heads) return 0;
+    return kv4::scratch_of(c, kv4::way_of(c, r, n_heads));
 }
 
-int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, int dtype, const eesd_kv4_tensor *q,
-                    int n_heads, float scale, const int32_t *visible, void *out, void *scratch, size_t scratch_bytes) {
+int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_attention *call) {
+    if (!call) return EESD_ERR_BADARG;
+    const eesd_kv4_rows *r = &call->rows;
+    const int dtype = call->dtype, n_heads = call->n_heads;
     kv4::AttnArgs a = {};
     eesd_kv4_layout l;
     int st = kv4_open(c, pool, pool_bytes, r, &a.c, &l);
     if (st) return st;
     if (!r->at || (dtype != EESD_F32 && dtype != EESD_BF16) || r->rows > EESD_MAX_ROWS || n_heads < 1 || n_heads % c->n_kv_heads) return EESD_ERR_BADARG;
-    if ((st = kv4_rows_check(q, dtype))) return st;
-    if (!out || ((uintptr_t)out & 15) || ((uintptr_t)visible & 3) || !(scale > 0.f) || !(scale <= 3.402823466e38f)) return EESD_ERR_BADARG;
-    if (const size_t need = eesd_kv4_attend_scratch_bytes(c, r, n_heads, dtype)) {
-        if (!scratch || ((uintptr_t)scratch & 15)) return EESD_ERR_BADARG;
-        if (scratch_bytes < need) return EESD_ERR_NOMEM;
+    if ((st = kv4_rows_check(&call->q, dtype))) return st;
+    if (!call->out || ((uintptr_t)call->out & 15) || ((uintptr_t)call->visible & 3) || !(call->scale > 0.f) || !(call->scale <= 3.402823466e38f)) return EESD_ERR_BADARG;
+    const kv4::Way w = kv4::way_of(c, r, n_heads);
+    if (const size_t need = kv4::scratch_of(c, w)) {
+        if (!call->scratch || ((uintptr_t)call->scratch & 15)) return EESD_ERR_BADARG;
+        if (call->scratch_bytes < need) return EESD_ERR_NOMEM;
     }
     a.n_ctx = r->at;
     a.n_rows = r->n_rows;
     a.positions = r->positions;
-    a.visible = visible;
+    a.visible = call->visible;
     a.rope = r->rope;
     a.n_rope = r->n_rope;
-    a.q = q->data;
-    a.qs[0] = q->stride_b, a.qs[1] = q->stride_row, a.qs[2] = q->stride_head;
-    a.out = out;
-    a.scale2 = scale * 1.4426950408889634f;
+    a.q = call->q.data;
+    a.qs[0] = call->q.stride_b, a.qs[1] = call->q.stride_row, a.qs[2] = call->q.stride_head;
+    a.out = call->out;
+    a.scale2 = call->scale * 1.4426950408889634f;
     a.B = r->B;
     a.rows = r->rows;
     a.heads = n_heads / c->n_kv_heads;
-    const kv4::Way w = kv4::way_of(c, r, n_heads);
     a.blocks = (int)(((int64_t)a.heads * r->rows + 8 * w.nt - 1) / (8 * w.nt));
     a.share = w.share;
-    a.part = (float *)scratch;
+    a.head = (int4 *)call->scratch;
+    a.part = (float *)(a.head + kv4::grid_of(w.nt));
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * a.blocks;
     if (segments * (w.share ? w.share : 1) > 0x7fffffffLL) return EESD_ERR_UNSUPPORTED;
     const bool f32 = dtype == EESD_F32;

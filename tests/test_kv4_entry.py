@@ -1,5 +1,6 @@
 """The C entries of the 4-bit key / value cache refuse what they cannot do before anything reaches a device."""
 import ctypes as C
+import struct
 
 import pytest
 
@@ -20,6 +21,10 @@ def rows(table=AT, stride=4, pages=4, B=2, rows=3, n_rope=0, at=AT, n_rows=0, ro
 
 def tensor(data=AT, sb=384, sr=128, sh=64):
     return b._kv4_tensor(data, sb, sr, sh)
+
+
+def attention(r, dt, q, H, scale, vis, out, s, sn):
+    return None if r is None else r + q + struct.pack("PPPNiif4x", vis, out, s, sn, dt, H, scale)
 
 
 def size(d):
@@ -50,12 +55,12 @@ def calls():
     L, d = eesd.lib(), desc()
     n = size(d).total_bytes
     p = C.addressof(d)
-    need = L.eesd_kv4_attend_scratch_bytes(p, rows(), 4, 0)
+    need = L.eesd_kv4_attend_scratch_bytes(p, rows(), 4)
     assert need == 0
     append = lambda d=p, pool=AT, n=n, r=rows(), dt=0, k=tensor(), v=tensor(): L.eesd_kv4_append(None, d, pool, n, r, dt, k, v)
     read = lambda d=p, pool=AT, n=n, r=rows(), ctx=None, dt=0, k=AT, v=AT: L.eesd_kv4_read(None, d, pool, n, r, ctx, dt, k, v)
-    attend = lambda d=p, pool=AT, n=n, r=rows(), dt=0, q=tensor(), H=4, scale=0.125, vis=None, out=AT, s=None, sn=0: L.eesd_kv4_attend(
-        None, d, pool, n, r, dt, q, H, scale, vis, out, s, sn)
+    attend = lambda d=p, pool=AT, n=n, r=rows(), dt=0, q=tensor(), H=4, scale=0.125, vis=0, out=AT, s=0, sn=0: L.eesd_kv4_attend(
+        None, d, pool, n, attention(r, dt, q, H, scale, vis, out, s, sn))
     return append, read, attend, n, d
 
 
@@ -73,8 +78,8 @@ def test_entry_refusals():
     assert append(r=rows(rows=2 ** 31 - 1, B=1024)) == UNSUPPORTED and read(r=rows(rows=2 ** 31 - 1, B=1024)) == UNSUPPORTED
     for kw in (dict(k=None, v=None), dict(k=AT + 4), dict(v=AT + 8), dict(ctx=AT + 2)):
         assert read(**kw) == BADARG, kw
-    for kw in (dict(q=None), dict(q=tensor(data=0)), dict(q=tensor(sr=-1)), dict(r=rows(rows=17)), dict(H=0), dict(H=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
-               dict(scale=float("inf")), dict(vis=AT + 1), dict(out=None), dict(r=rows(at=0))):
+    for kw in (dict(q=tensor(data=0)), dict(q=tensor(sr=-1)), dict(r=rows(rows=17)), dict(H=0), dict(H=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+               dict(scale=float("inf")), dict(vis=AT + 1), dict(out=0), dict(out=AT + 8), dict(r=rows(at=0))):
         assert attend(**kw) == BADARG, kw
 
 
@@ -82,9 +87,9 @@ def test_scratch():
     L, d = eesd.lib(), desc(400, 2, 128, 16, 64)
     p, n = C.addressof(d), size(d).total_bytes
     long = rows(stride=99999, pages=99999)
-    need = L.eesd_kv4_attend_scratch_bytes(p, long, 4, 0)
+    need = L.eesd_kv4_attend_scratch_bytes(p, long, 4)
     assert need > 0 and need % 16 == 0
-    for bad in (dict(H=3), dict(dt=7), dict(r=rows(stride=99999, pages=99999, rows=17)), dict(r=None)):
-        assert L.eesd_kv4_attend_scratch_bytes(p, bad.get("r", long), bad.get("H", 4), bad.get("dt", 0)) == 0
-    f = lambda s, sn: L.eesd_kv4_attend(None, p, AT, n, long, 0, tensor(), 4, 0.125, None, AT, s, sn)
-    assert f(None, need) == BADARG and f(AT + 8, need) == BADARG and f(AT, need - 1) == NOMEM
+    for bad in (dict(H=3), dict(H=0), dict(r=rows(stride=99999, pages=99999, rows=17)), dict(r=None)):
+        assert L.eesd_kv4_attend_scratch_bytes(p, bad.get("r", long), bad.get("H", 4)) == 0
+    f = lambda s, sn: L.eesd_kv4_attend(None, p, AT, n, attention(long, 0, tensor(), 4, 0.125, 0, AT, s, sn))
+    assert f(0, need) == BADARG and f(AT + 8, need) == BADARG and f(AT, need - 1) == NOMEM
