@@ -53,10 +53,9 @@ struct AttnArgs {
 };
 
 __device__ __forceinline__ int rows_of(const AttnArgs &a, int b) { return a.n_rows ? min(max(a.n_rows[b], 0), a.rows) : a.rows; }
-// tiles that hold what some row of the sequence may see, at least 1
-__device__ __forceinline__ int tiles_of(const AttnArgs &a, int b) {
-    if (a.n_rows && a.n_rows[b] <= 0) return 1;
-    return (int)max((int64_t)1, min((int64_t)a.c.max_pages << a.c.shift, ((int64_t)a.n_ctx[b] + 15) / 16));
+// tiles that hold what some of n rows of a sequence of ctx tokens may see, at least 1
+__device__ __forceinline__ int tiles_of(const AttnArgs &a, int ctx, int n) {
+    return n ? (int)max((int64_t)1, min((int64_t)a.c.max_pages << a.c.shift, ((int64_t)ctx + 15) / 16)) : 1;
 }
 
 // ---------------------------------------------------------------------------------- runs
@@ -72,9 +71,11 @@ struct Place {
     int off, n;    // tile in the segment, of n
 };
 struct Plan {
-    int tiles[EESD_KV4_MAX_BATCH];   // of a segment of each sequence
-    Place begin;                     // where the block's run begins
-    int64_t count;                   // how many tiles it takes
+    int ctx[EESD_KV4_MAX_BATCH];   // tokens and rows of each sequence
+    uint8_t rows[EESD_KV4_MAX_BATCH];
+    Place begin;                   // where the block's run begins
+    int64_t count;                 // how many tiles it takes
+    __device__ __forceinline__ int tiles(const AttnArgs &a, int b) const { return tiles_of(a, ctx[b], rows[b]); }
 };
 // The run of block `block` of `grid`, worked out by the first warp.
 __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block, int grid) {
@@ -82,7 +83,11 @@ __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block,
         const int lane = threadIdx.x;
         const int64_t per = (int64_t)a.c.Hkv * a.blocks;
         int64_t total = 0;
-        for (int b = lane; b < a.B; b += 32) total += p.tiles[b] = tiles_of(a, b);
+        for (int b = lane; b < a.B; b += 32) {
+            p.ctx[b] = a.n_ctx[b];
+            p.rows[b] = (uint8_t)rows_of(a, b);
+            total += p.tiles(a, b);
+        }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         total *= per;
@@ -96,7 +101,7 @@ __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block,
             int64_t before = 0;   // tiles of one head and column block up to the chunk
             at[end] = total;
             for (int b0 = 0; b0 < a.B; b0 += 32) {
-                const int n = b0 + lane < a.B ? p.tiles[b0 + lane] : 0;
+                const int n = b0 + lane < a.B ? p.tiles(a, b0 + lane) : 0;
                 int64_t sum = n;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -116,7 +121,7 @@ __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block,
                         cut = 0;
                         if (++seg == per) seg = 0, b++;
                     }
-                    f = Place{b, seg, cut, b < a.B ? p.tiles[b] : 1};
+                    f = Place{b, seg, cut, b < a.B ? p.tiles(a, b) : 1};
                 }
                 const uint32_t who = __ballot_sync(0xffffffffu, here);
                 if (who) {
@@ -248,25 +253,57 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         f.b = seg / per;
         f.seg = seg % per;
         f.off = 0;
-        f.n = tiles_of(a, f.b);
+        f.n = tiles_of(a, a.n_ctx[f.b], rows_of(a, f.b));
     }
+    // What a segment begins with: its rows, the pages of the first tiles, its queries and their angles.  Asked for before the last segment's parts meet.
+    constexpr int QI = (C * HALF + kAttnThreads - 1) / kAttnThreads;
+    static_assert(C * HALF % kAttnThreads == 0 && HALF % 32 == 0, "a warp's values belong to one column");
+    const int step = TT * kWarps * (RUNS ? 1 : a.share);
+    struct Pages { int v[TT]; };
+    struct Start {
+        int b, h, pair0, n, old, tile1, first;
+        Pages pages[kStages];
+        float2 q[QI], turn[QI];
+    };
+    auto pages_of = [&](const int32_t *table, int tile, int tile1) {
+        Pages p;
+#pragma unroll
+        for (int i = 0; i < TT; i++) p.v[i] = tile + i < tile1 ? table[(tile + i) >> a.c.shift] : -1;
+        return p;
+    };
+    auto read_ahead = [&](Start &s) {
+        s.b = f.b, s.h = f.seg / a.blocks, s.pair0 = f.seg % a.blocks * C;
+        s.tile1 = RUNS ? (int)min((int64_t)f.n, f.off + left) : f.n;
+        s.first = f.off + (RUNS ? warp : blockIdx.x % a.share * kWarps + warp) * TT;
+        s.n = RUNS ? sh.plan.rows[f.b] : rows_of(a, f.b);
+        s.old = (int)max((int64_t)(RUNS ? sh.plan.ctx[f.b] : a.n_ctx[f.b]) - s.n, (int64_t)-64);   // positions before the new rows
+        const int32_t *table = a.c.table + s.b * a.c.table_stride;
+#pragma unroll
+        for (int i = 0; i < kStages; i++) s.pages[i] = pages_of(table, s.first + i * step, s.tile1);
+#pragma unroll
+        for (int i = 0; i < QI; i++) {
+            const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF, rho = s.pair0 + c, m = rho / a.heads;
+            s.q[i] = make_float2(0.f, 0.f);
+            s.turn[i] = make_float2(1.f, 0.f);
+            if (m < s.n) {
+                const T *src = (const T *)a.q + s.b * a.qs[0] + m * a.qs[1] + (int64_t)(s.h * a.heads + rho % a.heads) * a.qs[2] + 2 * e;
+                s.q[i] = make_float2(to_f(src[0]), to_f(src[1]));
+                if (a.rope) {
+                    const int at = a.positions ? a.positions[(int64_t)s.b * a.rows + m] : s.old + m;
+                    s.turn[i] = reinterpret_cast<const float2 *>(a.rope)[(int64_t)min(max(at, 0), a.n_rope - 1) * HALF + e];
+                }
+            }
+        }
+    };
+    Start now;
+    if (left > 0) read_ahead(now);
     while (left > 0) {
-        const int tile1 = RUNS ? (int)min((int64_t)f.n, f.off + left) : f.n;
-        const int first = f.off + (RUNS ? warp : blockIdx.x % a.share * kWarps + warp) * TT, step = TT * kWarps * (RUNS ? 1 : a.share);
-        const int b = f.b, h = f.seg / a.blocks, pair0 = f.seg % a.blocks * C;
-        const int n = rows_of(a, b), old = (int)max((int64_t)a.n_ctx[b] - n, (int64_t)-64);   // positions before the new rows
+        const int b = now.b, h = now.h, pair0 = now.pair0, n = now.n, old = now.old, tile1 = now.tile1, first = now.first;
 
         // ---- the ring: stage i % kStages holds the warp's TT tiles from first + i * step on
         const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp][0]);
         const int32_t *table = a.c.table + b * a.c.table_stride;
         uint32_t there = 0;   // bit TT s + i: tile i of stage s exists
-        struct Pages { int v[TT]; };
-        auto pages_of = [&](int tile) {
-            Pages p;
-#pragma unroll
-            for (int i = 0; i < TT; i++) p.v[i] = tile + i < tile1 ? table[(tile + i) >> a.c.shift] : -1;
-            return p;
-        };
         auto fetch = [&](int stage, int tile, const Pages &pages) {
 #pragma unroll
             for (int i = 0; i < TT; i++) {
@@ -283,41 +320,25 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             }
             end_copies();
         };
-        Pages next_pages;
-        {
-            Pages pages[kStages];
 #pragma unroll
-            for (int i = 0; i < kStages; i++) pages[i] = pages_of(first + i * step);
-#pragma unroll
-            for (int i = 0; i < kStages - 1; i++) fetch(i, first + i * step, pages[i]);
-            next_pages = pages[kStages - 1];
-        }
+        for (int i = 0; i < kStages - 1; i++) fetch(i, first + i * step, now.pages[i]);
+        Pages next_pages = now.pages[kStages - 1];
 
         // ---- queries: turned, and as whole numbers of 16 (fp32: 24) bits under a power of two of their column, in digits of 8 bits
-        constexpr int QI = (C * HALF + kAttnThreads - 1) / kAttnThreads;
-        static_assert(C * HALF % 32 == 0 && HALF % 32 == 0, "a warp's values belong to one column");
         float2 qv[QI];
 #pragma unroll
         for (int i = 0; i < QI; i++) {
-            const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF, rho = pair0 + c, m = rho / a.heads;
-            qv[i] = make_float2(0.f, 0.f);
+            const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF;
+            // (1, 0) turns nothing, but for what is not finite
+            qv[i] = a.rope ? turn(now.q[i].x, now.q[i].y, now.turn[i]) : now.q[i];
+            const float u = fabsf(qv[i].x), v = fabsf(qv[i].y);
+            bool bad = !(u <= -kLowest) || !(v <= -kLowest);
             float most = 0.f;
-            bool bad = false;
-            if (c < C && m < n) {
-                const T *src = (const T *)a.q + b * a.qs[0] + m * a.qs[1] + (int64_t)(h * a.heads + rho % a.heads) * a.qs[2] + 2 * e;
-                qv[i] = make_float2(to_f(src[0]), to_f(src[1]));
-                if (a.rope) {
-                    const int at = a.positions ? a.positions[(int64_t)b * a.rows + m] : old + m;
-                    qv[i] = turn(qv[i].x, qv[i].y, reinterpret_cast<const float2 *>(a.rope)[(int64_t)min(max(at, 0), a.n_rope - 1) * HALF + e]);
-                }
-                const float u = fabsf(qv[i].x), v = fabsf(qv[i].y);
-                bad = !(u <= -kLowest) || !(v <= -kLowest);
-                if (bad) qv[i] = make_float2(0.f, 0.f);   // (the column is NaN)
-                else most = fmaxf(u, v);
-            }
+            if (bad) qv[i] = make_float2(0.f, 0.f);   // (the column is NaN)
+            else most = fmaxf(u, v);
             most = warp_max(most);
             bad = __any_sync(0xffffffffu, bad);
-            if (c < C && lane == 0) sh.most[c][e / 32] = most, sh.bad[c][e / 32] = bad;
+            if (lane == 0) sh.most[c][e / 32] = most, sh.bad[c][e / 32] = bad;
         }
         __syncthreads();
 #pragma unroll
@@ -399,7 +420,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             wait_copies<kStages - 2>();
             __syncwarp();   // (every lane's copies; and the stage before this one has been read)
             fetch((stage + kStages - 1) % kStages, tile + (kStages - 1) * step, next_pages);
-            next_pages = pages_of(tile + kStages * step);
+            next_pages = pages_of(table, tile + kStages * step, tile1);
             const uint32_t here = there >> (TT * stage) & ((1u << TT) - 1);
             if (!here) continue;
             const unsigned char *src = sh.ring[warp][stage];
@@ -638,6 +659,14 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             }
         }
         wait_copies<0>();
+        const bool all = RUNS ? f.off == 0 && tile1 == f.n : a.share == 1;
+        const int off = f.off, seg = f.seg;
+        if (RUNS) {
+            if (tid == 0 && !all) {
+                if (off) a.head[blockIdx.x].z = tile1 == f.n ? 2 : 1;
+                else a.head[blockIdx.x].x = b, a.head[blockIdx.x].y = seg;
+            }
+        }
 
         // ---- the warps' results meet
 #pragma unroll
@@ -665,9 +694,17 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
 #pragma unroll
                 for (int r = 0; r < D / 16; r++) sh.o[warp][c][16 * r + g] = o[r][i][k] * worth, sh.o[warp][c][16 * r + 8 + g] = o[r][i][k + 2] * worth;
             }
+        if (RUNS) {
+            left -= tile1 - off;
+            f.off = 0;
+            if (++f.seg == a.c.Hkv * a.blocks) f.seg = 0, f.b++;
+            if (left > 0) {
+                f.n = sh.plan.tiles(a, f.b);
+                read_ahead(now);   // (while the parts meet)
+            }
+        }
         __syncthreads();
-        const bool all = RUNS ? f.off == 0 && tile1 == f.n : a.share == 1;
-        float *part = a.part + (size_t)(2 * blockIdx.x + (f.off == 0)) * C * (D + 4);
+        float *part = a.part + (size_t)(2 * blockIdx.x + (off == 0)) * C * (D + 4);
         for (int idx = tid; idx < C * (D / 4); idx += kAttnThreads) {
             const int c = idx / (D / 4), d = idx % (D / 4) * 4, rho = pair0 + c;
             if (rho >= a.rows * a.heads) break;
@@ -712,40 +749,30 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             cluster.sync();   // (the others read this block's memory)
         }
         if (!RUNS) return;
-        if (tid == 0 && !all) {
-            if (f.off) a.head[blockIdx.x].z = tile1 == f.n ? 2 : 1;
-            else a.head[blockIdx.x].x = b, a.head[blockIdx.x].y = f.seg;
-        }
         __syncthreads();
-        left -= tile1 - f.off;
-        f.off = 0;
-        if (++f.seg == a.c.Hkv * a.blocks) {
-            f.seg = 0, f.b++;
-            if (left > 0) f.n = sh.plan.tiles[f.b];
-        }
     }
 }
 
-// One block: a column of the segment that block blockIdx.x of the runs began and left; the parts are added in the order of the tiles.
+// One block: the segment that block blockIdx.x of the runs began and left; the parts are added in the order of the tiles.  A thread has four dimensions of a
+// column; with a grid of as many blocks high as there are columns, a block has one column and its threads share the parts (few segments of
+// many parts).
 template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThreads) join_kernel(const AttnArgs a) {
     constexpr int C = 8 * NT, LANES = D / 4, GROUPS = kAttnThreads / LANES, GRID = grid_of(NT);
     using T = std::conditional_t<F32, float, __nv_bfloat16>;
     __shared__ int slot[GRID + 1];
     __shared__ int parts_of;
-    __shared__ float2 ml[GRID + 1];
     __shared__ float4 ys[GROUPS][LANES];
-    __shared__ float tops[kWarps], sums[kWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.y;
+    __shared__ float2 mls[GROUPS];
+    const int tid = threadIdx.x, lane = tid & 31;
     pdl_wait();
     pdl_trigger();
     const int4 head = a.head[blockIdx.x];
-    const int b = head.x, seg = head.y, rho = seg % a.blocks * C + c;
-    if (b < 0 || rho >= a.rows * a.heads) return;
-    if (warp == 0) {
+    if (tid < 32) {
         int parts = 1;
         if (lane == 0) slot[0] = 2 * blockIdx.x + 1;
         for (int i0 = blockIdx.x + 1; i0 < GRID; i0 += 32) {
             const int does = i0 + lane < GRID ? a.head[i0 + lane].z : 0;
+            if (head.x < 0) break;
             const uint32_t ends = __ballot_sync(0xffffffffu, does == 2), upto = ends ? (ends & -ends) * 2 - 1 : 0xffffffffu;
             const uint32_t some = __ballot_sync(0xffffffffu, does != 0) & upto;
             if (some >> lane & 1) slot[parts + __popc(some & ((1u << lane) - 1))] = 2 * (i0 + lane);
@@ -754,35 +781,36 @@ template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThread
         }
         if (lane == 0) parts_of = parts;
     }
+    if (head.x < 0) return;
     __syncthreads();
-    const int parts = parts_of;
-    float top = kLowest;
-    for (int k = tid; k < parts; k += kAttnThreads) {
-        ml[k] = *reinterpret_cast<const float2 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + D);
-        top = fmaxf(top, ml[k].x);
-    }
-    top = warp_max(top);
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWarps; w++) top = fmaxf(top, tops[w]);
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int d = tid % LANES * 4;
-#pragma unroll 8
-    for (int k = tid / LANES; k < parts; k += GROUPS)
-        add4(y, ex2(ml[k].x - top), *reinterpret_cast<const float4 *>(a.part + ((size_t)slot[k] * C + c) * (D + 4) + d));
-    ys[tid / LANES][tid % LANES] = y;
-    float sum = 0.f;
-    for (int k = tid; k < parts; k += kAttnThreads) sum = fmaf(ex2(ml[k].x - top), ml[k].y, sum);
-    sum = warp_sum(sum);
-    if (lane == 0) sums[warp] = sum;
-    __syncthreads();
-    if (tid < LANES) {
-        sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; w++) sum += sums[w];
-#pragma unroll
-        for (int k = 1; k < GROUPS; k++) add4(y, 1.f, ys[k][tid]);
+    const int parts = parts_of, b = head.x, seg = head.y, pair0 = seg % a.blocks * C;
+    const bool apart = gridDim.y > 1;
+    const int from = apart ? tid / LANES : 0, by = apart ? GROUPS : 1;
+    for (int idx = apart ? blockIdx.y * LANES + tid % LANES : tid; idx < C * LANES; idx += apart ? C * LANES : kAttnThreads) {
+        const int c = idx / LANES, d = idx % LANES * 4, rho = pair0 + c;
+        if (rho >= a.rows * a.heads) break;
+        float top = kLowest, sum = 0.f;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float2 ml, float4 part) {
+            const float last = top;
+            top = fmaxf(top, ml.x);
+            const float keep = ex2(last - top), f = ex2(ml.x - top);
+            sum = fmaf(f, ml.y, sum * keep);
+            y = make_float4(y.x * keep, y.y * keep, y.z * keep, y.w * keep);
+            add4(y, f, part);
+        };
+#pragma unroll 4
+        for (int k = from; k < parts; k += by) {
+            const float *p = a.part + ((size_t)slot[k] * C + c) * (D + 4);
+            add(*reinterpret_cast<const float2 *>(p + D), *reinterpret_cast<const float4 *>(p + d));
+        }
+        if (apart) {
+            ys[tid / LANES][tid % LANES] = y;
+            if (tid % LANES == 0) mls[tid / LANES] = make_float2(top, sum);
+            __syncthreads();
+            if (tid >= LANES) break;
+            for (int k = 1; k < GROUPS; k++) add(mls[k], ys[k][tid]);
+        }
         store_out<D, T>(a, b, seg / a.blocks, rho, d, rows_of(a, b), y, sum);
     }
 }
@@ -817,7 +845,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(
     }
     if (RUNS) {
         launch_k(kernel, dim3(grid_of(NT)), dim3(kAttnThreads), kSmem, s, pdl_enabled(), a);
-        launch_k(join_kernel<D, NT, F32>, dim3(grid_of(NT), 8 * NT), dim3(kAttnThreads), 0, s, pdl_enabled(), a);
+        launch_k(join_kernel<D, NT, F32>, dim3(grid_of(NT), segments * 16 < grid_of(NT) ? 8 * NT : 1), dim3(kAttnThreads), 0, s, pdl_enabled(), a);
         return cudaGetLastError();
     }
     cudaLaunchConfig_t cfg = {};
