@@ -55,12 +55,15 @@ struct AppendArgs {
     bool vec;
 };
 
-// One block: a tile of 16 tokens of one head, as far as the call's rows fill it; one warp a token's keys or values, N = D / 32 neighbours a
-// lane.  The codes meet in shared memory and go out as the tile's bytes, whole where the tile is.
+// One block: a tile of 16 tokens of one head, as far as the call's rows fill it; one warp the keys and values of two tokens (four tasks), N = D / 32
+// neighbours a lane.  The tasks' extremes are found together, the tasks halved among the lanes at each exchange, so that a group's scale is worked
+// out once, beside the others'.  Codes by the reciprocal, settled by the remainder (as in w4.cu).  They meet in shared memory and go out as the
+// tile's bytes, whole where the tile is.
 template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
     constexpr int N = D / 32, GL = 32 / G;   // GL: lanes of a group
     using L = Tile<D, G>;
     __shared__ __align__(16) unsigned char tile[L::BYTES];
+    __shared__ float4 table[kThreads / 32][4][G];   // {s, 1 / s, 1.5 * 2^23 + z, whether 1 / s will do} of each task and group
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -75,68 +78,121 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
     if (ti < 0 || lo >= hi) return;
     unsigned char *dst = tile_at(a.c, b, h, ti, L::BYTES);
     if (!dst) return;
-    for (int task = warp; task < 2 * (hi - lo); task += kThreads / 32) {
-        const bool is_v = task & 1;
-        const int tok = lo + (task >> 1), m = (int)(tok - first);
-        float w[N];
-        if (is_v) load<N>((const T *)a.v + b * a.vs[0] + m * a.vs[1] + h * a.vs[2] + lane * N, a.vec, w);
-        else load<N>((const T *)a.k + b * a.ks[0] + m * a.ks[1] + h * a.ks[2] + lane * N, a.vec, w);
-        if (!is_v && a.rope) {
-            const int64_t pos = a.positions ? (int64_t)a.positions[(int64_t)b * a.r.rows + m] : ti * 16 + tok;
-            const int64_t row = min(max(pos, (int64_t)0), (int64_t)(a.n_rope - 1));
-            const float2 *cs = reinterpret_cast<const float2 *>(a.rope) + row * (D / 2) + lane * (N / 2);
+    constexpr float M = 12582912.f;   // 1.5 * 2^23
+    constexpr uint32_t MB = 0x4b400000u;
+    const int tok0 = lo + 2 * warp, left = hi - tok0;   // the warp's tokens: min(left, 2)
+    if (left > 0) {
+        float w[4][N];   // tasks: keys, keys, values, values
 #pragma unroll
-            for (int i = 0; i < N / 2; i++) {
-                const float2 y = turn(w[2 * i], w[2 * i + 1], cs[i]);
-                w[2 * i] = y.x, w[2 * i + 1] = y.y;
+        for (int i = 0; i < 4; i++) {
+            const int m = (int)(tok0 + (i & 1 && left > 1) - first);   // (a token that is not there: the first again)
+            const int64_t *st = i < 2 ? a.ks : a.vs;
+            load<N>((const T *)(i < 2 ? a.k : a.v) + b * st[0] + m * st[1] + h * st[2] + lane * N, a.vec, w[i]);
+        }
+        if (a.rope) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const int tok = tok0 + (i && left > 1);
+                const int64_t pos = a.positions ? (int64_t)a.positions[(int64_t)b * a.r.rows + (tok - first)] : ti * 16 + tok;
+                const int64_t row = min(max(pos, (int64_t)0), (int64_t)(a.n_rope - 1));
+                const float2 *cs = reinterpret_cast<const float2 *>(a.rope) + row * (D / 2) + lane * (N / 2);
+#pragma unroll
+                for (int j = 0; j < N / 2; j++) {
+                    const float2 y = turn(w[i][2 * j], w[i][2 * j + 1], cs[j]);
+                    w[i][2 * j] = y.x, w[i][2 * j + 1] = y.y;
+                }
             }
         }
-        float most = 0.f, least = 0.f;
+        // extremes: e[task] the largest, e[4 + task] the least turned over; afterwards the lane has that of task (lane >> 1 & 1) * 2 + (lane >> 2 & 1), the largest
+        // where its bit 0 is not set
+        float e[8];
 #pragma unroll
-        for (int i = 0; i < N; i++) most = max_nan(most, w[i]), least = min_nan(least, w[i]);
+        for (int i = 0; i < 4; i++) {
+            e[i] = e[4 + i] = 0.f;
 #pragma unroll
-        for (int o = 1; o < GL; o <<= 1) {
-            most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-            least = min_nan(least, __shfl_xor_sync(0xffffffffu, least, o));
+            for (int j = 0; j < N; j++) e[i] = max_nan(e[i], w[i][j]), e[4 + i] = max_nan(e[4 + i], -w[i][j]);
         }
-        float s = round_range(most, least, EESD_BF16);
-        if (!(most <= 3.402823466e38f) || !(least >= -3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
-        const bool plain = s > 0.f;   // (neither 0 nor NaN)
-        const float z = plain ? fminf(nearest_quotient(-least, s), 15.f) : 0.f;
-        uint32_t c[N];
 #pragma unroll
-        for (int i = 0; i < N; i++) c[i] = plain ? (uint32_t)fminf(fmaxf(nearest_quotient(w[i], s) + z, 0.f), 15.f) : 0u;
-        if (lane % GL == 0) {
-            const int gi = lane / GL;
-            reinterpret_cast<uint16_t *>(tile + L::SCALES)[(gi * 16 + tok) * 2 + is_v] = __bfloat16_as_ushort(__float2bfloat16_rn(s));
-            tile[(is_v ? L::VZ : L::KZ) + gi * 16 + tok] = (unsigned char)z;
+        for (int s = 0; s < 3; s++) {
+            const bool up = lane >> s & 1;
+#pragma unroll
+            for (int i = 0; i < 4 >> s; i++) {
+                const float send = up ? e[i] : e[i + (4 >> s)], keep = up ? e[i + (4 >> s)] : e[i];
+                e[i] = max_nan(keep, __shfl_xor_sync(0xffffffffu, send, 1 << s));
+            }
         }
-        if (!is_v) {
-            const int d = lane * N, at = tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4 + d % 8 / 2;
-            if constexpr (N == 4) *reinterpret_cast<uint16_t *>(tile + at) = (uint16_t)(c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12);
-            else tile[at] = (unsigned char)(c[0] | c[1] << 4);
-        } else {
-            // a word takes one nibble of each of 8 lanes: N words, halved among the lanes at each exchange
-            const int d = lane * N, shift = 4 * (d % 64 / 8), t = tok % 8 / 2, he = tok / 8 * 2 + tok % 2;
-            int word;
-            uint32_t v;
-            if constexpr (N == 4) {
-                const bool up1 = lane & 2, up2 = lane & 4;
-                const uint32_t s0 = up1 ? c[0] : c[2], s1 = up1 ? c[1] : c[3];
-                uint32_t k0 = (up1 ? c[2] : c[0]) << shift, k1 = (up1 ? c[3] : c[1]) << shift;
-                k0 |= __shfl_xor_sync(0xffffffffu, s0 << shift, 2);
-                k1 |= __shfl_xor_sync(0xffffffffu, s1 << shift, 2);
-                v = (up2 ? k1 : k0) | __shfl_xor_sync(0xffffffffu, up2 ? k0 : k1, 4);
-                v |= __shfl_xor_sync(0xffffffffu, v, 8);
-                word = up1 * 2 + up2;
+#pragma unroll
+        for (int o = 8; o < GL; o <<= 1) e[0] = max_nan(e[0], __shfl_xor_sync(0xffffffffu, e[0], o));
+        {
+            const float other = __shfl_xor_sync(0xffffffffu, e[0], 1);
+            const float most = lane & 1 ? other : e[0], least = lane & 1 ? e[0] : other;   // (least: turned over)
+            float s = round_range(most, -least, EESD_BF16);
+            if (!(most <= 3.402823466e38f) || !(least <= 3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
+            const bool plain = s > 0.f, fine = s >= 0x1p-100f;   // plain: neither 0 nor NaN
+            const float z = plain ? fminf(nearest_quotient(least, s), 15.f) : 0.f;
+            const int task = (lane >> 1 & 1) * 2 + (lane >> 2 & 1), gi = lane / GL;
+            if (lane % GL < 8 && !(lane & 1)) {
+                table[warp][task][gi] = make_float4(plain ? s : 1.f, fine ? __frcp_rn(s) : 0.f, M + z, plain && !fine ? 0.f : 1.f);
+                const int tok = tok0 + (task & 1), is_v = task >> 1;
+                if ((task & 1) < left) {
+                    reinterpret_cast<uint16_t *>(tile + L::SCALES)[(gi * 16 + tok) * 2 + is_v] = __bfloat16_as_ushort(__float2bfloat16_rn(s));
+                    tile[(is_v ? L::VZ : L::KZ) + gi * 16 + tok] = (unsigned char)z;
+                }
+            }
+        }
+        __syncwarp();
+        const int d = lane * N, shift = 4 * (d % 64 / 8);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float4 t = table[warp][i][lane / GL];
+            float y[N];
+            bool off = t.w == 0.f;
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                y[j] = __fmaf_rn(w[i][j], t.y, t.z);   // 1.5 * 2^23 + the code
+                const float rem = __fmaf_rn(t.z - y[j], t.x, w[i][j]);
+                off |= fabsf(rem) * 2.f >= t.x;
+            }
+            if (off) {   // a quotient at (or beside) a half, or a scale whose reciprocal will not do
+#pragma unroll
+                for (int j = 0; j < N; j++) y[j] = t.z + nearest_quotient(w[i][j], t.x);
+            }
+            uint32_t c[N];   // MB + the code (what is not finite: 0)
+#pragma unroll
+            for (int j = 0; j < N; j++) c[j] = __float_as_uint(fminf(fmaxf(y[j], M), M + 15.f));
+            const int tok = tok0 + (i & 1);
+            if (i < 2) {
+                const int at = tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4 + d % 8 / 2;
+                if constexpr (N == 4) {
+                    const uint32_t v = c[0] + c[1] * 16u + c[2] * 256u + c[3] * 4096u - MB * 4369u;
+                    if ((i & 1) < left) *reinterpret_cast<uint16_t *>(tile + at) = (uint16_t)v;
+                } else {
+                    if ((i & 1) < left) tile[at] = (unsigned char)(c[0] + c[1] * 16u - MB * 17u);
+                }
             } else {
-                const bool up = lane & 4;
-                v = ((up ? c[1] : c[0]) << shift) | __shfl_xor_sync(0xffffffffu, (up ? c[0] : c[1]) << shift, 4);
-                v |= __shfl_xor_sync(0xffffffffu, v, 8);
-                v |= __shfl_xor_sync(0xffffffffu, v, 16);
-                word = up;
+                // a word takes one nibble of each of 8 lanes: N words, halved among the lanes at each exchange
+                const int t2 = tok % 8 / 2, he = tok / 8 * 2 + tok % 2;
+                int word;
+                uint32_t v;
+#pragma unroll
+                for (int j = 0; j < N; j++) c[j] = (c[j] - MB) << shift;
+                if constexpr (N == 4) {
+                    const bool up1 = lane & 2, up2 = lane & 4;
+                    uint32_t k0 = up1 ? c[2] : c[0], k1 = up1 ? c[3] : c[1];
+                    k0 |= __shfl_xor_sync(0xffffffffu, up1 ? c[0] : c[2], 2);
+                    k1 |= __shfl_xor_sync(0xffffffffu, up1 ? c[1] : c[3], 2);
+                    v = (up2 ? k1 : k0) | __shfl_xor_sync(0xffffffffu, up2 ? k0 : k1, 4);
+                    v |= __shfl_xor_sync(0xffffffffu, v, 8);
+                    word = up1 * 2 + up2;
+                } else {
+                    const bool up = lane & 4;
+                    v = (up ? c[1] : c[0]) | __shfl_xor_sync(0xffffffffu, up ? c[0] : c[1], 4);
+                    v |= __shfl_xor_sync(0xffffffffu, v, 8);
+                    v |= __shfl_xor_sync(0xffffffffu, v, 16);
+                    word = up;
+                }
+                if ((N == 4 ? !(lane & 8) : !(lane & 24)) && (i & 1) < left) reinterpret_cast<uint32_t *>(tile + L::V)[((d / 64 * 8 + d % 8 + word) * 4 + t2) * 4 + he] = v;
             }
-            if (N == 4 ? !(lane & 8) : !(lane & 24)) reinterpret_cast<uint32_t *>(tile + L::V)[((d / 64 * 8 + d % 8 + word) * 4 + t) * 4 + he] = v;
         }
     }
     __syncthreads();
@@ -160,7 +216,22 @@ struct ReadArgs {
     void *k, *v;
 };
 
-// One block: a tile, brought into shared memory; one warp a token's keys or values, N = D / 32 neighbours a lane.
+template <int N, typename T> __device__ __forceinline__ void store(T *out, const float (&w)[N]) {
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (N == 4) __stcs(reinterpret_cast<float4 *>(out), make_float4(w[0], w[1], w[2], w[3]));
+        else __stcs(reinterpret_cast<float2 *>(out), make_float2(w[0], w[1]));
+    } else {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(w[0], w[1]);
+        if constexpr (N == 4) {
+            const __nv_bfloat162 q = __floats2bfloat162_rn(w[2], w[3]);
+            __stcs(reinterpret_cast<uint2 *>(out), make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q)));
+        } else {
+            __stcs(reinterpret_cast<uint32_t *>(out), *reinterpret_cast<const uint32_t *>(&p));
+        }
+    }
+}
+
+// One block: a tile, brought into shared memory; one warp two tokens' keys and values, N = D / 32 neighbours a lane.
 template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a) {
     constexpr int N = D / 32, GL = 32 / G;
     using L = Tile<D, G>;
@@ -180,43 +251,36 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
     if (src)
         for (int i = threadIdx.x; i < L::BYTES / 16; i += kThreads) reinterpret_cast<uint4 *>(tile)[i] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
     __syncthreads();
+    const int end = src ? (int)min((int64_t)16, left) : 0;   // tokens that are there
     const int gi = lane / GL, d = lane * N;
-    for (int task = warp; task < 2 * (hi - lo); task += kThreads / 32) {
-        const bool is_v = task & 1;
-        const int tok = lo + (task >> 1);
-        T *out = (T *)(is_v ? a.v : a.k);
-        if (!out) continue;
-        float w[N];
-        if (src && tok < left) {
-            const uint32_t word = reinterpret_cast<const uint32_t *>(tile + L::SCALES)[gi * 16 + tok];
-            const float s = __uint_as_float(is_v ? word & 0xffff0000u : word << 16);
-            const int z = tile[(is_v ? L::VZ : L::KZ) + gi * 16 + tok];
-            if (!is_v) {
+    const size_t row = (size_t)a.c.Hkv * D;
+    const size_t at = ((size_t)((int64_t)b * a.r.rows - first) * a.c.Hkv + h) * D + d;   // of token 0
+    // 2^23 + c (the code's nibble set into the mantissa) - (2^23 + z), times s
+    auto value = [](uint32_t word, int shift, float z, float s) { return __fmul_rn(__uint_as_float((word >> shift & 15u) | 0x4b000000u) - z, s); };
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int tok = warp + 8 * i;
+        if (tok < lo || tok >= hi) continue;
+        const uint32_t scales = reinterpret_cast<const uint32_t *>(tile + L::SCALES)[gi * 16 + tok];
+        float k[N], v[N];
+#pragma unroll
+        for (int j = 0; j < N; j++) k[j] = v[j] = 0.f;
+        if (tok < end) {
+            if (a.k) {
                 const uint32_t c = reinterpret_cast<const uint32_t *>(tile)[(tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4) / 4] >> 4 * (d % 8);
+                const float s = __uint_as_float(scales << 16), z = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]);
 #pragma unroll
-                for (int i = 0; i < N; i++) w[i] = __fmul_rn((float)((int)(c >> 4 * i & 15) - z), s);
-            } else {
-                const uint32_t *at = reinterpret_cast<const uint32_t *>(tile + L::V) + ((d / 64 * 8 + d % 8) * 4 + tok % 8 / 2) * 4 + tok / 8 * 2 + tok % 2;
-#pragma unroll
-                for (int i = 0; i < N; i++) w[i] = __fmul_rn((float)((int)(at[i * 16] >> 4 * (d % 64 / 8) & 15) - z), s);
+                for (int j = 0; j < N; j++) k[j] = value(c, 4 * j, z, s);
             }
-        } else {
+            if (a.v) {
+                const uint32_t *c = reinterpret_cast<const uint32_t *>(tile + L::V) + ((d / 64 * 8 + d % 8) * 4 + tok % 8 / 2) * 4 + tok / 8 * 2 + tok % 2;
+                const float s = __uint_as_float(scales & 0xffff0000u), z = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
 #pragma unroll
-            for (int i = 0; i < N; i++) w[i] = 0.f;
-        }
-        out += (((size_t)b * a.r.rows + (size_t)(tok - first)) * a.c.Hkv + h) * D + d;
-        if constexpr (sizeof(T) == 4) {
-            if constexpr (N == 4) __stcs(reinterpret_cast<float4 *>(out), make_float4(w[0], w[1], w[2], w[3]));
-            else __stcs(reinterpret_cast<float2 *>(out), make_float2(w[0], w[1]));
-        } else {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(w[0], w[1]);
-            if constexpr (N == 4) {
-                const __nv_bfloat162 q = __floats2bfloat162_rn(w[2], w[3]);
-                __stcs(reinterpret_cast<uint2 *>(out), make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q)));
-            } else {
-                __stcs(reinterpret_cast<uint32_t *>(out), *reinterpret_cast<const uint32_t *>(&p));
+                for (int j = 0; j < N; j++) v[j] = value(c[j * 16], 4 * (d % 64 / 8), z, s);
             }
         }
+        if (a.k) store<N>((T *)a.k + at + tok * row, k);
+        if (a.v) store<N>((T *)a.v + at + tok * row, v);
     }
 }
 
