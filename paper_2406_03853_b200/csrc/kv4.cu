@@ -63,7 +63,7 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
     constexpr int N = D / 32, GL = 32 / G;   // GL: lanes of a group
     using L = Tile<D, G>;
     __shared__ __align__(16) unsigned char tile[L::BYTES];
-    __shared__ float4 table[kThreads / 32][4][G];   // {s, 1 / s, 1.5 * 2^23 + z, whether 1 / s will do} of each task and group
+    __shared__ float4 table[kThreads / 32][4][G];   // {s, 1 / s, 1.5 * 2^23 + z, what twice a remainder is looked at from} of each task and group
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -132,7 +132,7 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
             const float z = plain ? fminf(nearest_quotient(least, s), 15.f) : 0.f;
             const int task = (lane >> 1 & 1) * 2 + (lane >> 2 & 1), gi = lane / GL;
             if (lane % GL < 8 && !(lane & 1)) {
-                table[warp][task][gi] = make_float4(plain ? s : 1.f, fine ? __frcp_rn(s) : 0.f, M + z, plain && !fine ? 0.f : 1.f);
+                table[warp][task][gi] = make_float4(plain ? s : 1.f, fine ? __frcp_rn(s) : 0.f, M + z, fine ? s : plain ? 0.f : 3.402823466e38f);
                 const int tok = tok0 + (task & 1), is_v = task >> 1;
                 if ((task & 1) < left) {
                     reinterpret_cast<uint16_t *>(tile + L::SCALES)[(gi * 16 + tok) * 2 + is_v] = __bfloat16_as_ushort(__float2bfloat16_rn(s));
@@ -145,17 +145,21 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const float4 t = table[warp][i][lane / GL];
-            float y[N];
-            bool off = t.w == 0.f;
+            float y[N], twice[N], most = 0.f;   // twice: the remainder
 #pragma unroll
             for (int j = 0; j < N; j++) {
                 y[j] = __fmaf_rn(w[i][j], t.y, t.z);   // 1.5 * 2^23 + the code
-                const float rem = __fmaf_rn(t.z - y[j], t.x, w[i][j]);
-                off |= fabsf(rem) * 2.f >= t.x;
+                twice[j] = __fmaf_rn(t.z - y[j], t.x, w[i][j]) * 2.f;
+                most = fmaxf(most, fabsf(twice[j]));
             }
-            if (off) {   // a quotient at (or beside) a half, or a scale whose reciprocal will not do
+            if (most >= t.w) {   // a quotient at (or beside) a half: to the nearer, or the even one; or a scale whose reciprocal will not do (t.w 0)
 #pragma unroll
-                for (int j = 0; j < N; j++) y[j] = t.z + nearest_quotient(w[i][j], t.x);
+                for (int j = 0; j < N; j++) {
+                    const bool odd = (__float_as_int(y[j]) ^ __float_as_int(t.z)) & 1;
+                    if (twice[j] > t.x || (twice[j] == t.x && odd)) y[j] += 1.f;
+                    else if (-twice[j] > t.x || (-twice[j] == t.x && odd)) y[j] -= 1.f;
+                    if (t.w == 0.f) y[j] = t.z + nearest_quotient(w[i][j], t.x);
+                }
             }
             uint32_t c[N];   // MB + the code (what is not finite: 0)
 #pragma unroll
@@ -231,56 +235,61 @@ template <int N, typename T> __device__ __forceinline__ void store(T *out, const
     }
 }
 
-// One block: a tile, brought into shared memory; one warp two tokens' keys and values, N = D / 32 neighbours a lane.
-template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a) {
+// One block: kTiles neighbouring tiles of a head, brought into shared memory; a warp two tokens' keys and values of each, N = D / 32 neighbours a lane.
+template <int D, int G, int kTiles, typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a) {
     constexpr int N = D / 32, GL = 32 / G;
     using L = Tile<D, G>;
-    __shared__ __align__(16) unsigned char tile[L::BYTES];
+    __shared__ __align__(16) unsigned char tiles[kTiles][L::BYTES];
+    __shared__ int ends[kTiles];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned int blk = blockIdx.x;
     const int h = blk % a.c.Hkv;
     blk /= a.c.Hkv;
-    const int x = blk % a.r.tiles, b = blk / a.r.tiles;
-    const int64_t start = a.r.at ? a.r.at[b] : 0, ti = (start >> 4) + x, first = start - ti * 16, past = first + a.r.rows;
-    const int lo = first > 0 ? (int)first : 0, hi = past < 16 ? (int)past : 16;
+    const int groups = (a.r.tiles + kTiles - 1) / kTiles, x = blk % groups * kTiles, b = blk / groups;
+    const int64_t start = a.r.at ? a.r.at[b] : 0, ti = (start >> 4) + x, first = start - ti * 16, past = first + a.r.rows;   // (of the block's first tile)
+    const int lo = first > 0 ? (int)first : 0, hi = past < 16 * kTiles ? (int)past : 16 * kTiles;
     if (lo >= hi) return;
-    const int64_t left = a.n_ctx ? (int64_t)a.n_ctx[b] - ti * 16 : 16;
-    const unsigned char *src = ti < 0 || left <= lo ? nullptr : tile_at(a.c, b, h, ti, L::BYTES);
-    if (src)
-        for (int i = threadIdx.x; i < L::BYTES / 16; i += kThreads) reinterpret_cast<uint4 *>(tile)[i] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
+    // a warp brings a tile (kTiles <= 8); one tile is brought by all
+    const int64_t left = a.n_ctx ? (int64_t)a.n_ctx[b] - ti * 16 : 16 * kTiles;
+    if (kTiles == 1 || warp < kTiles) {
+        const int j = kTiles == 1 ? 0 : warp, by = kTiles == 1 ? kThreads : 32;
+        const unsigned char *src = ti + j < 0 || left <= max(lo, 16 * j) || 16 * j >= hi ? nullptr : tile_at(a.c, b, h, ti + j, L::BYTES);
+        if (src)
+#pragma unroll 5
+            for (int i = kTiles == 1 ? (int)threadIdx.x : lane; i < L::BYTES / 16; i += by) reinterpret_cast<uint4 *>(tiles[j])[i] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
+        if (kTiles == 1 ? threadIdx.x == 0 : lane == 0) ends[j] = src ? (int)min((int64_t)16, left - 16 * j) : 0;   // tokens that are there
+    }
     __syncthreads();
-    const int end = src ? (int)min((int64_t)16, left) : 0;   // tokens that are there
     const int gi = lane / GL, d = lane * N;
     const size_t row = (size_t)a.c.Hkv * D;
     const size_t at = ((size_t)((int64_t)b * a.r.rows - first) * a.c.Hkv + h) * D + d;   // of token 0
+    const int k_at = d % 32 / 8 * (D / 8) + d / 32 * 4, k_shift = 4 * (d % 8), v_at = L::V + (d / 64 * 8 + d % 8) * 64, v_shift = 4 * (d % 64 / 8);
     // 2^23 + c (the code's nibble set into the mantissa) - (2^23 + z), times s
     auto value = [](uint32_t word, int shift, float z, float s) { return __fmul_rn(__uint_as_float((word >> shift & 15u) | 0x4b000000u) - z, s); };
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int tok = warp + 8 * i;
-        if (tok < lo || tok >= hi) continue;
-        const uint32_t scales = reinterpret_cast<const uint32_t *>(tile + L::SCALES)[gi * 16 + tok];
+#pragma unroll 2
+    for (int i = 0; i < 2 * kTiles; i++) {
+        const int j = i >> 1, tok = warp + 8 * (i & 1), place = 16 * j + tok;
+        if (place < lo || place >= hi) continue;
+        const unsigned char *tile = tiles[j];
         float k[N], v[N];
 #pragma unroll
-        for (int j = 0; j < N; j++) k[j] = v[j] = 0.f;
-        if (tok < end) {
-            if (a.k) {
-                const uint32_t c = reinterpret_cast<const uint32_t *>(tile)[(tok * (D / 2) + d % 32 / 8 * (D / 8) + d / 32 * 4) / 4] >> 4 * (d % 8);
-                const float s = __uint_as_float(scales << 16), z = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]);
+        for (int n = 0; n < N; n++) k[n] = v[n] = 0.f;
+        if (tok < ends[j]) {
+            const uint32_t scales = *reinterpret_cast<const uint32_t *>(tile + L::SCALES + (gi * 16 + tok) * 4);
+            const uint32_t c = *reinterpret_cast<const uint32_t *>(tile + tok * (D / 2) + k_at) >> k_shift;
+            const unsigned char *vc = tile + v_at + (tok % 8 / 2) * 16 + (tok / 8 * 2 + tok % 2) * 4;
+            const float sk = __uint_as_float(scales << 16), sv = __uint_as_float(scales & 0xffff0000u);
+            const float zk = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]), zv = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
 #pragma unroll
-                for (int j = 0; j < N; j++) k[j] = value(c, 4 * j, z, s);
-            }
-            if (a.v) {
-                const uint32_t *c = reinterpret_cast<const uint32_t *>(tile + L::V) + ((d / 64 * 8 + d % 8) * 4 + tok % 8 / 2) * 4 + tok / 8 * 2 + tok % 2;
-                const float s = __uint_as_float(scales & 0xffff0000u), z = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
+            for (int n = 0; n < N; n++) k[n] = value(c, 4 * n, zk, sk);
 #pragma unroll
-                for (int j = 0; j < N; j++) v[j] = value(c[j * 16], 4 * (d % 64 / 8), z, s);
-            }
+            for (int n = 0; n < N; n++) v[n] = value(*reinterpret_cast<const uint32_t *>(vc + n * 64), v_shift, zv, sv);
         }
-        if (a.k) store<N>((T *)a.k + at + tok * row, k);
-        if (a.v) store<N>((T *)a.v + at + tok * row, v);
+        const size_t to = at + place * row;
+        if (a.k) store<N>((T *)a.k + to, k);
+        if (a.v) store<N>((T *)a.v + to, v);
     }
 }
 
@@ -288,9 +297,9 @@ template <typename T> void (*pick_append(int D, int G))(AppendArgs) {
     if (D == 64) return G == 1 ? append_kernel<64, 1, T> : append_kernel<64, 2, T>;
     return G == 1 ? append_kernel<128, 1, T> : G == 2 ? append_kernel<128, 2, T> : append_kernel<128, 4, T>;
 }
-template <typename T> void (*pick_read(int D, int G))(ReadArgs) {
-    if (D == 64) return G == 1 ? read_kernel<64, 1, T> : read_kernel<64, 2, T>;
-    return G == 1 ? read_kernel<128, 1, T> : G == 2 ? read_kernel<128, 2, T> : read_kernel<128, 4, T>;
+template <int TILES, typename T> void (*pick_read(int D, int G))(ReadArgs) {
+    if (D == 64) return G == 1 ? read_kernel<64, 1, TILES, T> : read_kernel<64, 2, TILES, T>;
+    return G == 1 ? read_kernel<128, 1, TILES, T> : G == 2 ? read_kernel<128, 2, TILES, T> : read_kernel<128, 4, TILES, T>;
 }
 
 }  // namespace kv4
@@ -397,8 +406,12 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
     a.k = k;
     a.v = v;
     const int G = c->head_dim / c->group;
-    launch_k(out_dtype == EESD_F32 ? kv4::pick_read<float>(c->head_dim, G) : kv4::pick_read<__nv_bfloat16>(c->head_dim, G), dim3(blocks), dim3(kv4::kThreads), 0,
-             (cudaStream_t)cuda_stream, pdl_enabled(), a);
+    // four tiles a block once there are blocks enough for every multiprocessor's eight (what a block does before its first value: half of what one tile takes)
+    const bool four = blocks >= 4u * 8u * 148u;
+    if (four) blocks = (unsigned int)((a.r.tiles + 3) / 4 * (int64_t)c->n_kv_heads * r->B);
+    auto kernel = out_dtype == EESD_F32 ? (four ? kv4::pick_read<4, float>(c->head_dim, G) : kv4::pick_read<1, float>(c->head_dim, G))
+                                        : (four ? kv4::pick_read<4, __nv_bfloat16>(c->head_dim, G) : kv4::pick_read<1, __nv_bfloat16>(c->head_dim, G));
+    launch_k(kernel, dim3(blocks), dim3(kv4::kThreads), 0, (cudaStream_t)cuda_stream, pdl_enabled(), a);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }
 
