@@ -18,6 +18,30 @@ struct Rows {
     int rows, tiles;   // tiles: those that a sequence's rows may touch
 };
 
+// bf16((hi + down) / 15) of hi, down >= 0, to nearest, ties to even: round_range without 64 bits.  The product with 1 / 15 gives the scale or its
+// neighbour; the exact sum (its rounding error beside it) against 15 times the borders, which are fp32 numbers, tells.  Sums whose borders
+// might not be are left to round_range.
+__device__ __forceinline__ float range_scale(float hi, float down) {
+    const float sum = __fadd_rn(hi, down);
+    if (!(sum >= 0x1p-90f && sum <= 0x1p120f)) return round_range(hi, -down, EESD_BF16);
+    const float part = __fsub_rn(sum, hi), lost = __fadd_rn(__fsub_rn(hi, __fsub_rn(sum, part)), __fsub_rn(down, part));
+    const uint32_t bits = __float_as_uint(__fmul_rn(sum, 1.f / 15.f)), near = bits + 0x7fffu + (bits >> 16 & 1) & 0xffff0000u;
+    auto side = [&](uint32_t border) {   // > 0: the sum lies above 15 times the border
+        const float d = __fsub_rn(sum, __fmul_rn(15.f, __uint_as_float(border)));
+        return d != 0.f ? d : lost;
+    };
+    const float above = side(near + 0x8000u), below = side(near - 0x8000u);
+    const bool odd = near & 0x10000u;
+    if (above > 0.f || (above == 0.f && odd)) return __uint_as_float(near + 0x10000u);
+    if (below < 0.f || (below == 0.f && odd)) return __uint_as_float(near - 0x10000u);
+    return __uint_as_float(near);
+}
+__device__ __forceinline__ float reciprocal(float x) {   // within 2 units in the last place
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // N neighbouring values of a row
 template <int N, typename T> __device__ __forceinline__ void load(const T *p, bool vec, float (&x)[N]) {
     if (vec) {
@@ -63,7 +87,7 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
     constexpr int N = D / 32, GL = 32 / G;   // GL: lanes of a group
     using L = Tile<D, G>;
     __shared__ __align__(16) unsigned char tile[L::BYTES];
-    __shared__ float4 table[kThreads / 32][4][G];   // {s, 1 / s, 1.5 * 2^23 + z, what twice a remainder is looked at from} of each task and group
+    __shared__ float4 table[kThreads / 32][4][G];   // {s, 1 / s, 1.5 * 2^23 + z, s / 2: the remainder that is looked at} of each task and group
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -126,13 +150,24 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
         {
             const float other = __shfl_xor_sync(0xffffffffu, e[0], 1);
             const float most = lane & 1 ? other : e[0], least = lane & 1 ? e[0] : other;   // (least: turned over)
-            float s = round_range(most, -least, EESD_BF16);
+            float s = range_scale(most, least);
             if (!(most <= 3.402823466e38f) || !(least <= 3.402823466e38f)) s = __uint_as_float(0x7fc00000u);
-            const bool plain = s > 0.f, fine = s >= 0x1p-100f;   // plain: neither 0 nor NaN
-            const float z = plain ? fminf(nearest_quotient(least, s), 15.f) : 0.f;
+            const bool plain = s > 0.f, fine = s >= 0x1p-90f;   // plain: neither 0 nor NaN
+            const float inv = fine ? reciprocal(s) : 0.f;
+            float z = 0.f;
+            if (fine) {
+                float q = __fmaf_rn(least, inv, M);
+                const float rem = __fmaf_rn(M - q, s, least);
+                const bool odd = __float_as_int(q) & 1;
+                if (rem > 0.5f * s || (rem == 0.5f * s && odd)) q += 1.f;
+                else if (-rem > 0.5f * s || (-rem == 0.5f * s && odd)) q -= 1.f;
+                z = fminf(q - M, 15.f);
+            } else if (plain) {
+                z = fminf(nearest_quotient(least, s), 15.f);
+            }
             const int task = (lane >> 1 & 1) * 2 + (lane >> 2 & 1), gi = lane / GL;
             if (lane % GL < 8 && !(lane & 1)) {
-                table[warp][task][gi] = make_float4(plain ? s : 1.f, fine ? __frcp_rn(s) : 0.f, M + z, fine ? s : plain ? 0.f : 3.402823466e38f);
+                table[warp][task][gi] = make_float4(plain ? s : 1.f, inv, M + z, fine ? 0.5f * s : plain ? 0.f : 3.402823466e38f);
                 const int tok = tok0 + (task & 1), is_v = task >> 1;
                 if ((task & 1) < left) {
                     reinterpret_cast<uint16_t *>(tile + L::SCALES)[(gi * 16 + tok) * 2 + is_v] = __bfloat16_as_ushort(__float2bfloat16_rn(s));
@@ -145,19 +180,19 @@ template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) 
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const float4 t = table[warp][i][lane / GL];
-            float y[N], twice[N], most = 0.f;   // twice: the remainder
+            float y[N], rem[N], most = 0.f;
 #pragma unroll
             for (int j = 0; j < N; j++) {
                 y[j] = __fmaf_rn(w[i][j], t.y, t.z);   // 1.5 * 2^23 + the code
-                twice[j] = __fmaf_rn(t.z - y[j], t.x, w[i][j]) * 2.f;
-                most = fmaxf(most, fabsf(twice[j]));
+                rem[j] = __fmaf_rn(t.z - y[j], t.x, w[i][j]);
+                most = fmaxf(most, fabsf(rem[j]));
             }
             if (most >= t.w) {   // a quotient at (or beside) a half: to the nearer, or the even one; or a scale whose reciprocal will not do (t.w 0)
 #pragma unroll
                 for (int j = 0; j < N; j++) {
                     const bool odd = (__float_as_int(y[j]) ^ __float_as_int(t.z)) & 1;
-                    if (twice[j] > t.x || (twice[j] == t.x && odd)) y[j] += 1.f;
-                    else if (-twice[j] > t.x || (-twice[j] == t.x && odd)) y[j] -= 1.f;
+                    if (rem[j] > t.w || (rem[j] == t.w && odd)) y[j] += 1.f;
+                    else if (-rem[j] > t.w || (-rem[j] == t.w && odd)) y[j] -= 1.f;
                     if (t.w == 0.f) y[j] = t.z + nearest_quotient(w[i][j], t.x);
                 }
             }
@@ -280,6 +315,23 @@ template <int D, int G, int kTiles, typename T> __global__ void __launch_bounds_
             const uint32_t scales = *reinterpret_cast<const uint32_t *>(tile + L::SCALES + (gi * 16 + tok) * 4);
             const uint32_t c = *reinterpret_cast<const uint32_t *>(tile + tok * (D / 2) + k_at) >> k_shift;
             const unsigned char *vc = tile + v_at + (tok % 8 / 2) * 16 + (tok / 8 * 2 + tok % 2) * 4;
+            if constexpr (sizeof(T) == 2 && N == 4) {
+                // two codes at a time: 128 + c (the nibble set into the mantissa of bf16's 128) - (128 + z), times s, rounded once
+                const uint32_t zk = tile[L::KZ + gi * 16 + tok] * 0x10001u | 0x43004300u, zv = tile[L::VZ + gi * 16 + tok] * 0x10001u | 0x43004300u;
+                const uint32_t sk = __byte_perm(scales, 0, 0x1010), sv = __byte_perm(scales, 0, 0x3232);
+                auto pair = [](uint32_t two, uint32_t z, uint32_t s) {
+                    uint32_t r = two & 0x000f000fu | 0x43004300u;
+                    asm("sub.rn.bf16x2 %0, %0, %1;\n\tmul.rn.bf16x2 %0, %0, %2;" : "+r"(r) : "r"(z), "r"(s));
+                    return r;
+                };
+                const uint32_t c4 = c & 0xffffu, *v4 = reinterpret_cast<const uint32_t *>(vc);
+                const size_t to = at + place * row;
+                if (a.k) __stcs(reinterpret_cast<uint2 *>((T *)a.k + to), make_uint2(pair(c4 | c4 << 12, zk, sk), pair(c4 >> 8 | c4 << 4, zk, sk)));
+                if (a.v)
+                    __stcs(reinterpret_cast<uint2 *>((T *)a.v + to),
+                           make_uint2(pair(__byte_perm(v4[0] >> v_shift, v4[16] >> v_shift, 0x5410), zv, sv), pair(__byte_perm(v4[32] >> v_shift, v4[48] >> v_shift, 0x5410), zv, sv)));
+                continue;
+            }
             const float sk = __uint_as_float(scales << 16), sv = __uint_as_float(scales & 0xffff0000u);
             const float zk = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]), zv = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
 #pragma unroll
@@ -406,8 +458,8 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
     a.k = k;
     a.v = v;
     const int G = c->head_dim / c->group;
-    // four tiles a block once there are blocks enough for every multiprocessor's eight (what a block does before its first value: half of what one tile takes)
-    const bool four = blocks >= 4u * 8u * 148u;
+    // four tiles a block (its start costs as much as a tile) where that leaves most multiprocessors four blocks
+    const bool four = blocks >= 2u * 8u * 148u;
     if (four) blocks = (unsigned int)((a.r.tiles + 3) / 4 * (int64_t)c->n_kv_heads * r->B);
     auto kernel = out_dtype == EESD_F32 ? (four ? kv4::pick_read<4, float>(c->head_dim, G) : kv4::pick_read<1, float>(c->head_dim, G))
                                         : (four ? kv4::pick_read<4, __nv_bfloat16>(c->head_dim, G) : kv4::pick_read<1, __nv_bfloat16>(c->head_dim, G));
