@@ -17,6 +17,7 @@
 #include <cuda_fp16.h>
 #include <limits.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -29,6 +30,7 @@ namespace kv4 {
 namespace cg = cooperative_groups;
 
 constexpr int kWarps = 8, kAttnThreads = kWarps * 32;
+constexpr int kMaxShare = 16;     // blocks of a cluster
 constexpr int kUnit = 2 * kWarps;   // runs: tiles between the places where a segment may be cut
 constexpr int kMaxGrid = 296;
 __host__ __device__ constexpr int grid_of(int nt) { return nt == 1 ? kMaxGrid : kMaxGrid / 2; }   // blocks that fit the machine's 148 multiprocessors at once
@@ -218,13 +220,12 @@ template <int D, int G, int NT, int TT> struct Shared {
     };
     uint32_t q[NT][D / 32][32][4];    // digits 0 and 1 of the queries, in operand order
     uint32_t q2[NT][D / 32][32][2];   // digit 2 (fp32 queries)
-    int2 qsum[C][D / 32];             // of a group (at first: of 32 dimensions): the sum of digits 0 and 1 together, and of digit 2
+    int2 qsum[C][G];                  // of a group: the sum of digits 0 and 1 together, and of digit 2
     float2 ml[kWarps][C];   // the warps' maxima and sums
-    float most[C][2];       // largest finite query of a column (of its halves)
-    int bad[C][2];          // whether one is not finite
     float alpha[C];         // what a unit of its scores is worth
-    float2 ml_all[C];       // the block's
-    float y[C][D];
+    // clusters: the blocks' parts of the results that this block joins: [block][its share], and their maxima and sums
+    float4 in_y[C * D / 4 + kMaxShare];
+    float2 in_ml[kMaxShare][C];
     Plan plan;              // (runs alone; last)
 };
 
@@ -239,6 +240,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
     Pair base;
     asm volatile("mov.b32 %0, 0x64006400;" : "=r"(base.low));
     asm volatile("mov.b32 %0, 0x54005400;" : "=r"(base.high));
+    if (!RUNS && a.share > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (waited for before another block's memory is written)
     pdl_trigger();
     pdl_wait();
     Place f;
@@ -256,14 +258,14 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         f.n = tiles_of(a, a.n_ctx[f.b], rows_of(a, f.b));
     }
     // What a segment begins with: its rows, the pages of the first tiles, its queries and their angles.  Asked for before the last segment's parts meet.
-    constexpr int QI = (C * HALF + kAttnThreads - 1) / kAttnThreads;
-    static_assert(C * HALF % kAttnThreads == 0 && HALF % 32 == 0, "a warp's values belong to one column");
+    constexpr int QK = HALF / 32;   // pairs of a lane in a column; a warp has the columns warp + 8 i
+    static_assert(kWarps == 8 && C == 8 * NT && HALF % 32 == 0, "");
     const int step = TT * kWarps * (RUNS ? 1 : a.share);
     struct Pages { int v[TT]; };
     struct Start {
         int b, h, pair0, n, old, tile1, first;
         Pages pages[kStages];
-        float2 q[QI], turn[QI];
+        float2 q[NT][QK], turn[NT][QK];
     };
     auto pages_of = [&](const int32_t *table, int tile, int tile1) {
         Pages p;
@@ -281,17 +283,19 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
 #pragma unroll
         for (int i = 0; i < kStages; i++) s.pages[i] = pages_of(table, s.first + i * step, s.tile1);
 #pragma unroll
-        for (int i = 0; i < QI; i++) {
-            const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF, rho = s.pair0 + c, m = rho / a.heads;
-            s.q[i] = make_float2(0.f, 0.f);
-            s.turn[i] = make_float2(1.f, 0.f);
-            if (m < s.n) {
-                const T *src = (const T *)a.q + s.b * a.qs[0] + m * a.qs[1] + (int64_t)(s.h * a.heads + rho % a.heads) * a.qs[2] + 2 * e;
-                s.q[i] = make_float2(to_f(src[0]), to_f(src[1]));
-                if (a.rope) {
-                    const int at = a.positions ? a.positions[(int64_t)s.b * a.rows + m] : s.old + m;
-                    s.turn[i] = reinterpret_cast<const float2 *>(a.rope)[(int64_t)min(max(at, 0), a.n_rope - 1) * HALF + e];
-                }
+        for (int i = 0; i < NT; i++) {
+            const int rho = s.pair0 + warp + 8 * i, m = rho / a.heads;
+            const bool there = m < s.n;
+            const T *src = (const T *)a.q + s.b * a.qs[0] + m * a.qs[1] + (int64_t)(s.h * a.heads + rho - m * a.heads) * a.qs[2] + 2 * lane;
+            const float2 *cs = nullptr;
+            if (there && a.rope) {
+                const int at = a.positions ? a.positions[(int64_t)s.b * a.rows + m] : s.old + m;
+                cs = reinterpret_cast<const float2 *>(a.rope) + (int64_t)min(max(at, 0), a.n_rope - 1) * HALF + lane;
+            }
+#pragma unroll
+            for (int k = 0; k < QK; k++) {
+                s.q[i][k] = there ? make_float2(to_f(src[64 * k]), to_f(src[64 * k + 1])) : make_float2(0.f, 0.f);
+                s.turn[i][k] = cs ? cs[32 * k] : make_float2(1.f, 0.f);
             }
         }
     };
@@ -325,64 +329,55 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         Pages next_pages = now.pages[kStages - 1];
 
         // ---- queries: turned, and as whole numbers of 16 (fp32: 24) bits under a power of two of their column, in digits of 8 bits
-        float2 qv[QI];
 #pragma unroll
-        for (int i = 0; i < QI; i++) {
-            const int idx = tid + i * kAttnThreads, c = idx / HALF, e = idx % HALF;
-            // (1, 0) turns nothing, but for what is not finite
-            qv[i] = a.rope ? turn(now.q[i].x, now.q[i].y, now.turn[i]) : now.q[i];
-            const float u = fabsf(qv[i].x), v = fabsf(qv[i].y);
-            bool bad = !(u <= -kLowest) || !(v <= -kLowest);
+        for (int i = 0; i < NT; i++) {
+            const int c = warp + 8 * i;
+            float2 qv[QK];
             float most = 0.f;
-            if (bad) qv[i] = make_float2(0.f, 0.f);   // (the column is NaN)
-            else most = fmaxf(u, v);
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < QK; k++) {
+                // ((1, 0) would turn what is not finite)
+                qv[k] = a.rope ? turn(now.q[i][k].x, now.q[i][k].y, now.turn[i][k]) : now.q[i][k];
+                const float u = fabsf(qv[k].x), v = fabsf(qv[k].y);
+                if (!(u <= -kLowest) || !(v <= -kLowest)) bad = true, qv[k] = make_float2(0.f, 0.f);   // (the column is NaN)
+                else most = fmaxf(most, fmaxf(u, v));
+            }
             most = warp_max(most);
             bad = __any_sync(0xffffffffu, bad);
-            if (lane == 0) sh.most[c][e / 32] = most, sh.bad[c][e / 32] = bad;
-        }
-        __syncthreads();
+            constexpr int kBits = F32 ? 22 : 14;
+            int ex = max((int)(__float_as_uint(most) >> 23) - 127, -100);   // floor(log2), not below -100
+            if (most * power(kBits - ex) > (F32 ? 127.f * 65536.f : 127.f * 256.f)) ex++;   // (the first digit's range)
+            if (lane == 0) sh.alpha[c] = bad ? __uint_as_float(0x7fc00000u) : a.scale2 * power(ex - kBits);
+            int2 sum = make_int2(0, 0);
 #pragma unroll
-        for (int i = 0; i < QI; i++) {
-            const int idx = tid + i * kAttnThreads, c = idx / HALF, d = idx % HALF * 2;
-            if (c < C) {
-                constexpr int kBits = F32 ? 22 : 14;
-                const float most = HALF == 64 ? fmaxf(sh.most[c][0], sh.most[c][1]) : sh.most[c][0];
-                int ex = max((int)(__float_as_uint(most) >> 23) - 127, -100);   // floor(log2), not below -100
-                if (most * power(kBits - ex) > (F32 ? 127.f * 65536.f : 127.f * 256.f)) ex++;   // (the first digit's range)
-                const int x = __float2int_rn(qv[i].x * power(kBits - ex)), y = __float2int_rn(qv[i].y * power(kBits - ex));
-                if (d == 0) sh.alpha[c] = sh.bad[c][0] || (HALF == 64 && sh.bad[c][1]) ? __uint_as_float(0x7fc00000u) : a.scale2 * power(ex - kBits);
-                // word 0 of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + 0, 2, 4, 6, word 1 the others
-                const int j = d / 32, slot = c % 8 * 4 + d % 32 / 8, byte = d % 8 / 2;
+            for (int k = 0; k < QK; k++) {
+                const int x = __float2int_rn(qv[k].x * power(kBits - ex)), y = __float2int_rn(qv[k].y * power(kBits - ex));
+                // word 0 of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + 0, 2, 4, 6, word 1 the others; the lane has dimensions 64 k + 2 lane and + 1
+                const int slot = warp * 4 + lane % 16 / 4, byte = lane % 4;
                 const int xl = (int8_t)x, yl = (int8_t)y, xh = (x - xl) >> 8, yh = (y - yl) >> 8;   // the last digit, and the others
-                int8_t *q = reinterpret_cast<int8_t *>(sh.q[c / 8][j][slot]) + byte;
+                int8_t *q = reinterpret_cast<int8_t *>(sh.q[i][2 * k + lane / 16][slot]) + byte;
                 const int xm = F32 ? (int8_t)xh : xl, ym = F32 ? (int8_t)yh : yl;
                 q[0] = (int8_t)(F32 ? (xh - xm) >> 8 : xh), q[4] = (int8_t)(F32 ? (yh - ym) >> 8 : yh);
                 q[8] = (int8_t)xm, q[12] = (int8_t)ym;
                 if (F32) {
-                    int8_t *q2 = reinterpret_cast<int8_t *>(sh.q2[c / 8][j][slot]) + byte;
+                    int8_t *q2 = reinterpret_cast<int8_t *>(sh.q2[i][2 * k + lane / 16][slot]) + byte;
                     q2[0] = (int8_t)xl, q2[4] = (int8_t)yl;
                 }
-                int first = F32 ? xh + yh : x + y, second = xl + yl;
+                // a group's sums
+                sum.x += F32 ? xh + yh : x + y, sum.y += xl + yl;
+                if (G > 1 || k == QK - 1) {
 #pragma unroll
-                for (int o = 1; o < 16; o <<= 1) {
-                    first += __shfl_xor_sync(0xffffffffu, first, o);
-                    second += __shfl_xor_sync(0xffffffffu, second, o);
+                    for (int o = 1; o < (G == J ? 16 : 32); o <<= 1) {
+                        sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
+                        sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
+                    }
+                    if (lane % (G == J ? 16 : 32) == 0) sh.qsum[c][G == J ? 2 * k + lane / 16 : G > 1 ? k : 0] = sum;
+                    sum = make_int2(0, 0);
                 }
-                if (lane % 16 == 0) sh.qsum[c][j] = make_int2(first, second);
             }
         }
         __syncthreads();
-        if (G < J) {   // 32 dimensions -> a group
-            int2 v = make_int2(0, 0);
-            if (tid < C * G)
-                for (int j = 0; j < J / G; j++) {
-                    const int2 part = sh.qsum[tid / G][tid % G * (J / G) + j];
-                    v.x += part.x, v.y += part.y;
-                }
-            __syncthreads();
-            if (tid < C * G) sh.qsum[tid / G][tid % G] = v;
-            __syncthreads();
-        }
 
         // ---- what the lane's columns (2 t, 2 t + 1 of each eight) see
         int limit[NT][2];
@@ -705,6 +700,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         }
         __syncthreads();
         float *part = a.part + (size_t)(2 * blockIdx.x + (off == 0)) * C * (D + 4);
+        const int rank = RUNS ? 0 : blockIdx.x % a.share, chunk = RUNS ? 1 : (C * (D / 4) + a.share - 1) / a.share;   // results that a block of a cluster joins
+        if (!RUNS && a.share > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         for (int idx = tid; idx < C * (D / 4); idx += kAttnThreads) {
             const int c = idx / (D / 4), d = idx % (D / 4) * 4, rho = pair0 + c;
             if (rho >= a.rows * a.heads) break;
@@ -722,31 +719,29 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             if (all) {
                 store_out<D, T>(a, b, h, rho, d, n, y, total);
             } else if (!RUNS) {
-                *reinterpret_cast<float4 *>(&sh.y[c][d]) = y;
-                if (d == 0) sh.ml_all[c] = make_float2(top, total);
+                cg::cluster_group cluster = cg::this_cluster();
+                const int to = idx / chunk, at = idx - to * chunk;
+                *cluster.map_shared_rank(&sh.in_y[rank * chunk + at], to) = y;
+                if (d == 0 || at == 0) *cluster.map_shared_rank(&sh.in_ml[rank][c], to) = make_float2(top, total);
             } else {
                 *reinterpret_cast<float4 *>(part + c * (D + 4) + d) = y;
                 if (d == 0) *reinterpret_cast<float2 *>(part + c * (D + 4) + D) = make_float2(top, total);
             }
         }
         if (!RUNS && a.share > 1) {
-            cg::cluster_group cluster = cg::this_cluster();
-            cluster.sync();
-            for (int idx = blockIdx.x % a.share * kAttnThreads + tid; idx < C * (D / 4); idx += a.share * kAttnThreads) {
-                const int c = idx / (D / 4), d = idx % (D / 4) * 4, rho = pair0 + c;
-                if (rho >= a.rows * a.heads) break;
+            cg::this_cluster().sync();   // (the last touch of another block's memory lies before it)
+            const int idx = rank * chunk + tid, c = idx / (D / 4), d = idx % (D / 4) * 4, rho = pair0 + c;
+            if (tid < chunk && idx < C * (D / 4) && rho < a.rows * a.heads) {
                 float top = kLowest, total = 0.f;
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int r = 0; r < a.share; r++) top = fmaxf(top, cluster.map_shared_rank(&sh.ml_all[c], r)->x);
+                for (int r = 0; r < a.share; r++) top = fmaxf(top, sh.in_ml[r][c].x);
                 for (int r = 0; r < a.share; r++) {
-                    const float2 ml = *cluster.map_shared_rank(&sh.ml_all[c], r);
-                    const float f1 = ex2(ml.x - top);
-                    total = fmaf(f1, ml.y, total);
-                    add4(y, f1, *reinterpret_cast<const float4 *>(cluster.map_shared_rank(&sh.y[c][d], r)));
+                    const float f1 = ex2(sh.in_ml[r][c].x - top);
+                    total = fmaf(f1, sh.in_ml[r][c].y, total);
+                    add4(y, f1, sh.in_y[r * chunk + tid]);
                 }
                 store_out<D, T>(a, b, h, rho, d, n, y, total);
             }
-            cluster.sync();   // (the others read this block's memory)
         }
         if (!RUNS) return;
         __syncthreads();
@@ -823,9 +818,10 @@ Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     Way w;
     w.nt = columns <= 8 ? 1 : 2;
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * ((columns + 8 * w.nt - 1) / (8 * w.nt));
-    w.share = 1;
-    while (w.share < 8 && segments * w.share * 2 <= grid_of(w.nt) && w.share * kWarps < tiles) w.share *= 2;
-    if (segments * tiles > 64LL * grid_of(w.nt) || tiles > 64LL * w.share * 4) w.share = 0;
+    // the fewest rounds of tiles that the machine's blocks at once allow, with the fewest blocks
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(grid_of(w.nt) / segments, 1), kMaxShare), rounds = (tiles + kWarps * most - 1) / (kWarps * most);
+    w.share = (int)((tiles + kWarps * rounds - 1) / (kWarps * rounds));
+    if (segments * tiles > 64LL * grid_of(w.nt) || rounds > 32) w.share = 0;
     return w;
 }
 
@@ -840,6 +836,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(
     if (e != cudaSuccess) return e;
     if (dev > 63 || !(done.load(std::memory_order_acquire) >> dev & 1)) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess && !RUNS) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         if (dev <= 63) done.fetch_or(1ull << dev, std::memory_order_release);
     }
