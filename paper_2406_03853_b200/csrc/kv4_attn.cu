@@ -49,6 +49,8 @@ struct AttnArgs {
     int B, rows, heads;  // heads: query heads of a key head
     int blocks;          // column blocks of a key head
     int share;           // blocks of a cluster (runs: 0)
+    bool wide;           // runs: the call may have 2^31 tiles
+    bool pairs;          // pairs of queries are aligned
     int4 *head;          // runs: of each block, the sequence and segment that it began and left to the next ones (-1: none), and what it did of the one
                          // that it found begun: 0 nothing, 1 some, 2 its end
     float *part;         // runs: [2 * grid][columns][D + 4]: outputs, maximum, sum; of what a block found begun, and of what it left
@@ -62,10 +64,9 @@ __device__ __forceinline__ int tiles_of(const AttnArgs &a, int ctx, int n) {
 
 // ---------------------------------------------------------------------------------- runs
 // A cut inside a segment lies at a multiple of kUnit tiles, and at an end where fewer than that would be left.
-__device__ __forceinline__ int64_t cut_at(int64_t off, int64_t n) {
-    if (off <= 0) return 0;
-    if (off >= n) return n;
-    const int64_t c = (off + kUnit / 2) / kUnit * kUnit;
+__device__ __forceinline__ int cut_at(int off, int n) {   // 0 <= off < n <= 2^27
+    if (off == 0) return 0;
+    const int c = (off + kUnit / 2) / kUnit * kUnit;
     return c + kUnit > n ? n : c;
 }
 struct Place {
@@ -79,12 +80,12 @@ struct Plan {
     int64_t count;                 // how many tiles it takes
     __device__ __forceinline__ int tiles(const AttnArgs &a, int b) const { return tiles_of(a, ctx[b], rows[b]); }
 };
-// The run of block `block` of `grid`, worked out by the first warp.
-__device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block, int grid) {
-    if (threadIdx.x < 32) {
+// The run of block `block` of GRID, worked out by the first warp.  T: what holds all tiles of the call.
+template <int GRID, typename T> __device__ __forceinline__ void find_run(const AttnArgs &a, Plan &p, int block) {
+    {
         const int lane = threadIdx.x;
-        const int64_t per = (int64_t)a.c.Hkv * a.blocks;
-        int64_t total = 0;
+        const T per = (T)a.c.Hkv * a.blocks;
+        T total = 0;
         for (int b = lane; b < a.B; b += 32) {
             p.ctx[b] = a.n_ctx[b];
             p.rows[b] = (uint8_t)rows_of(a, b);
@@ -96,26 +97,26 @@ __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block,
         __syncwarp();
         // lane 0 .. 31: the sequences 32 i + lane; the one whose tiles hold a run's end says where
         Place f = {a.B, 0, 0, 1};
-        int64_t at[2];
+        T at[2] = {total, total};
+        T before = 0;   // tiles of one head and column block up to the chunk
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            const int n = b0 + lane < a.B ? p.tiles(a, b0 + lane) : 0;
+            T sum = n;
 #pragma unroll
-        for (int end = 0; end < 2; end++) {
-            const int64_t raw = total * (block + end) / grid;
-            int64_t before = 0;   // tiles of one head and column block up to the chunk
-            at[end] = total;
-            for (int b0 = 0; b0 < a.B; b0 += 32) {
-                const int n = b0 + lane < a.B ? p.tiles(a, b0 + lane) : 0;
-                int64_t sum = n;
+            for (int o = 1; o < 32; o <<= 1) {
+                const T u = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += u;
+            }
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int64_t u = __shfl_up_sync(0xffffffffu, sum, o);
-                    if (lane >= o) sum += u;
-                }
-                const int64_t in = raw - (before + sum - n) * per;   // tiles past the start of the lane's sequence
+            for (int end = 0; end < 2; end++) {
+                const T raw = (T)((uint64_t)total * (uint64_t)(block + end) / GRID), in = raw - (before + sum - n) * per;   // tiles past the start of the lane's sequence
                 const bool here = n > 0 && in >= 0 && in < n * per;
-                int64_t start = 0;
+                const uint32_t who = __ballot_sync(0xffffffffu, here);
+                if (!who) continue;
+                T start = 0;
                 if (here) {
-                    int seg = (uint64_t)in >> 32 ? (int)(in / n) : (int)((uint32_t)in / (uint32_t)n);
-                    const int off = (int)(in - (int64_t)seg * n);
+                    int seg = sizeof(T) == 8 && (uint64_t)in >> 32 ? (int)(in / n) : (int)((uint32_t)in / (uint32_t)n);
+                    const int off = (int)(in - (T)seg * n);
                     int cut = (int)cut_at(off, n);
                     start = raw - off + cut;
                     int b = b0 + lane;
@@ -124,20 +125,14 @@ __device__ __forceinline__ void make_plan(const AttnArgs &a, Plan &p, int block,
                         if (++seg == per) seg = 0, b++;
                     }
                     f = Place{b, seg, cut, b < a.B ? p.tiles(a, b) : 1};
+                    if (end == 0) p.begin = f;
                 }
-                const uint32_t who = __ballot_sync(0xffffffffu, here);
-                if (who) {
-                    const int from = __ffs(who) - 1;
-                    at[end] = __shfl_sync(0xffffffffu, start, from);
-                    if (end == 0 && lane == from) p.begin = f;
-                    break;
-                }
-                before += __shfl_sync(0xffffffffu, sum, 31);
+                at[end] = __shfl_sync(0xffffffffu, start, __ffs(who) - 1);
             }
+            before += __shfl_sync(0xffffffffu, sum, 31);
         }
         if (lane == 0) p.count = at[1] - at[0];
     }
-    __syncthreads();
 }
 
 // ---------------------------------------------------------------------------------- pieces
@@ -246,7 +241,11 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
     Place f;
     int64_t left = 1;   // runs: tiles to do
     if constexpr (RUNS) {
-        make_plan(a, sh.plan, blockIdx.x, grid_of(NT));
+        if (tid < 32) {
+            if (a.wide) find_run<grid_of(NT), int64_t>(a, sh.plan, blockIdx.x);
+            else find_run<grid_of(NT), int>(a, sh.plan, blockIdx.x);
+        }
+        __syncthreads();
         f = sh.plan.begin;
         left = sh.plan.count;
         if (tid == 0) a.head[blockIdx.x] = make_int4(-1, 0, 0, 0);
@@ -262,10 +261,12 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
     static_assert(kWarps == 8 && C == 8 * NT && HALF % 32 == 0, "");
     const int step = TT * kWarps * (RUNS ? 1 : a.share);
     struct Pages { int v[TT]; };
+    using Two = std::conditional_t<F32, float2, uint32_t>;
     struct Start {
         int b, h, pair0, n, old, tile1, first;
         Pages pages[kStages];
-        float2 q[NT][QK], turn[NT][QK];
+        Two q[NT][QK];   // as they lie in memory (what would use them waits for them)
+        float2 turn[NT][QK];
     };
     auto pages_of = [&](const int32_t *table, int tile, int tile1) {
         Pages p;
@@ -294,7 +295,10 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             }
 #pragma unroll
             for (int k = 0; k < QK; k++) {
-                s.q[i][k] = there ? make_float2(to_f(src[64 * k]), to_f(src[64 * k + 1])) : make_float2(0.f, 0.f);
+                if (!there) s.q[i][k] = Two{};
+                else if (a.pairs) s.q[i][k] = *reinterpret_cast<const Two *>(src + 64 * k);
+                else if constexpr (F32) s.q[i][k] = make_float2(src[64 * k], src[64 * k + 1]);
+                else s.q[i][k] = (uint32_t)__bfloat16_as_ushort(src[64 * k]) | (uint32_t)__bfloat16_as_ushort(src[64 * k + 1]) << 16;
                 s.turn[i][k] = cs ? cs[32 * k] : make_float2(1.f, 0.f);
             }
         }
@@ -338,7 +342,9 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
 #pragma unroll
             for (int k = 0; k < QK; k++) {
                 // ((1, 0) would turn what is not finite)
-                qv[k] = a.rope ? turn(now.q[i][k].x, now.q[i][k].y, now.turn[i][k]) : now.q[i][k];
+                if constexpr (F32) qv[k] = now.q[i][k];
+                else qv[k] = make_float2(__uint_as_float(now.q[i][k] << 16), __uint_as_float(now.q[i][k] & 0xffff0000u));
+                if (a.rope) qv[k] = turn(qv[k].x, qv[k].y, now.turn[i][k]);
                 const float u = fabsf(qv[k].x), v = fabsf(qv[k].y);
                 if (!(u <= -kLowest) || !(v <= -kLowest)) bad = true, qv[k] = make_float2(0.f, 0.f);   // (the column is NaN)
                 else most = fmaxf(most, fmaxf(u, v));
@@ -921,6 +927,9 @@ int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size
     a.heads = n_heads / c->n_kv_heads;
     a.blocks = (int)(((int64_t)a.heads * r->rows + 8 * w.nt - 1) / (8 * w.nt));
     a.share = w.share;
+    a.wide = (double)r->max_pages * (c->page_tokens / 16) * r->B * c->n_kv_heads * a.blocks >= 2147483648.0;
+    const uintptr_t es = dtype == EESD_F32 ? 4 : 2;
+    a.pairs = (uintptr_t)call->q.data % (2 * es) == 0 && ((call->q.stride_b | call->q.stride_row | call->q.stride_head) & 1) == 0;
     a.head = (int4 *)call->scratch;
     a.part = (float *)(a.head + kv4::grid_of(w.nt));
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * a.blocks;
