@@ -604,12 +604,14 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  *   out = sum_p exp(x_p - max x) v_p / sum_p exp(x_p - max x),  x_p = scale * (turned q . k_p)
  * over the positions p <= at[b] - n + m or, with `visible` ([B][rows], device), over p < at[b] - n and those of the n new ones at[b] - n + j whose
  * bit j of visible[b][m] is set (a tree).  What a row does not see has no effect on it, NaN and infinities included.  A row that sees nothing and rows
- * from n on are 0.  Row m's new key is not among what it sees by itself: a tree's mask sets the row's own bit.
+ * from n on are 0.  With `visible` a row sees its own key only where its own bit is set.
  * q in dtype, out contiguous [B][rows][n_heads][head_dim] in dtype, overlapping no input.  scratch: device, 16-byte aligned, eesd_kv4_attend_scratch_bytes
  * bytes (0: it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.
  * Arithmetic: sums, maxima and exponentials are fp32.  A row and head's queries are taken as whole numbers of 24 bits (dtype EESD_BF16: 16) under a power of
  * two: off by at most 2^-22 (2^-14) of the largest; their products with codes are exact.  A softmax numerator times its value's scale is taken as two fp16 terms
- * (EESD_BF16: one): off by at most 2^-22 (2^-11) of itself, or 2^-29 of the row's largest.  A row of queries that holds a NaN or an infinity gives NaN. */
+ * (EESD_BF16: one): off by at most 2^-22 (2^-11) of itself, or 2^-29 of the row's largest.  A row of queries that holds a NaN or an infinity gives NaN.
+ * Queries whose largest is below 2^-100 are taken as if it were 2^-100; keys and values from 2^88 on may overflow.  UNSUPPORTED: rows * n_heads above 2^30,
+ * or that times B and the table's tiles above 2^50. */
 typedef struct eesd_kv4_attention {
     eesd_kv4_rows rows;
     eesd_kv4_tensor q;

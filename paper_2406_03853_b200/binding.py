@@ -906,7 +906,8 @@ class KV4Cache:
         if buffer.dim() != 1 or not buffer.is_contiguous() or buffer.numel() < self.layout.total_bytes:
             raise ValueError(f"buffer: wanted {self.layout.total_bytes} contiguous bytes")
         self.buffer, self._ptr, self._bytes = buffer, buffer.data_ptr(), buffer.numel()
-        self._scratch = {}   # (B, rows, heads, pages) -> bytes of scratch memory that attend_rows takes
+        self._scale = head_dim ** -0.5
+        self._scratch = {}   # (B, rows, heads, pages) -> bytes of scratch memory that attend_rows takes; emptied when it has grown long
 
     @property
     def device(self) -> torch.device:
@@ -914,13 +915,13 @@ class KV4Cache:
 
     def _ints(self, t, name: str, shape) -> int:
         """The address of a contiguous int32 tensor of that shape on the cache's device."""
-        if not isinstance(t, torch.Tensor) or t.dtype is not _I32 or t.shape != shape or not t.is_cuda or t.get_device() != self._index or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor) or t.dtype is not _I32 or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: wanted a contiguous tensor of torch.int32 {list(shape)} on device {self._index}")
         return t.data_ptr()
 
     def _rows(self, page_table, B: int, rows: int, at, at_name: str, n_rows, rope, positions):
         """The fields of a call's eesd_kv4_rows, its tensors checked."""
-        if not isinstance(page_table, torch.Tensor) or page_table.dtype is not _I32 or not page_table.is_cuda or page_table.get_device() != self._index:
+        if not isinstance(page_table, torch.Tensor) or page_table.dtype is not _I32 or page_table.get_device() != self._index:
             raise ValueError(f"page_table: wanted a tensor of torch.int32 on device {self._index}")
         shape = page_table.shape
         if len(shape) != 2 or shape[0] != B or shape[1] < 1:
@@ -934,7 +935,7 @@ class KV4Cache:
                 stride = s[0]
         n_rope = rope_ptr = pos_ptr = 0
         if rope is not None:
-            if not isinstance(rope, torch.Tensor) or rope.dtype is not _F32 or not rope.is_cuda or rope.get_device() != self._index:
+            if not isinstance(rope, torch.Tensor) or rope.dtype is not _F32 or rope.get_device() != self._index:
                 raise ValueError(f"rope: wanted a tensor of torch.float32 on device {self._index}")
             shape = rope.shape
             if len(shape) != 3 or shape[0] < 1 or shape[1] != self.head_dim >> 1 or shape[2] != 2 or not rope.is_contiguous():
@@ -947,7 +948,7 @@ class KV4Cache:
 
     def _tensor(self, t, name: str, heads: int = 0):
         """The fields of an eesd_kv4_tensor: [B, rows, heads, head_dim] fp32 or bf16, and its shape."""
-        if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or not t.is_cuda or t.get_device() != self._index:
+        if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or t.get_device() != self._index:   # (-1: on the CPU)
             raise ValueError(f"{name}: wanted a tensor of torch.float32 or torch.bfloat16 on device {self._index}")
         shape = t.shape
         if len(shape) != 4 or shape[3] != self.head_dim or not t.numel() or (heads and shape[2] != heads):
@@ -1021,9 +1022,12 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
             raise ValueError("scratch: wanted contiguous")
         ptr, size = scratch.data_ptr(), scratch.numel()
     else:
-        size = cache._scratch.get((B, rows, H, r[2]))
+        key = B, rows, H, r[2]
+        size = cache._scratch.get(key)
         if size is None:
-            size = cache._scratch[B, rows, H, r[2]] = L.eesd_kv4_attend_scratch_bytes(cache._desc_ptr, _kv4_rows(*r), H)
+            if len(cache._scratch) >= 4096:
+                cache._scratch.clear()
+            size = cache._scratch[key] = L.eesd_kv4_attend_scratch_bytes(cache._desc_ptr, _kv4_rows(*r), H)
         if size:
             scratch = cache.buffer.new_empty(size)
             ptr = scratch.data_ptr()
@@ -1033,6 +1037,6 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
         _check_tensor(out, "out", (q.dtype,), index)
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out: wanted contiguous, of q's shape")
-    call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, cache.head_dim ** -0.5 if scale is None else scale)
+    call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, cache._scale if scale is None else scale)
     _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, call)
     return out

@@ -817,6 +817,12 @@ template <int D, int NT, bool F32> __global__ void __launch_bounds__(kAttnThread
 }
 
 // ---------------------------------------------------------------------------------- launches
+// Whether the call's columns, segments and tiles stay in the kernels' integers (a run's ends are tiles times blocks in 64 bits).
+bool countable(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
+    const double columns = (double)r->rows * n_heads, tiles = (double)r->max_pages * (c->page_tokens / 16);
+    return columns <= 0x1p30 && tiles * columns * r->B <= 0x1p50;
+}
+
 // How a call is shared out: column tiles a block takes at once, blocks of a cluster (0: runs)
 struct Way { int nt, share; };
 Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
@@ -892,7 +898,7 @@ extern "C" {
 size_t eesd_kv4_attend_scratch_bytes(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     eesd_kv4_layout l;
     if (eesd_kv4_layout_of(c, &l) || !r || r->B < 1 || r->max_pages < 1 || r->rows < 1 || r->rows > EESD_MAX_ROWS) return 0;
-    if (n_heads < 1 || n_heads % c->n_kv_heads) return 0;
+    if (n_heads < 1 || n_heads % c->n_kv_heads || !kv4::countable(c, r, n_heads)) return 0;
     return kv4::scratch_of(c, kv4::way_of(c, r, n_heads));
 }
 
@@ -907,6 +913,7 @@ int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size
     if (!r->at || (dtype != EESD_F32 && dtype != EESD_BF16) || r->rows > EESD_MAX_ROWS || n_heads < 1 || n_heads % c->n_kv_heads) return EESD_ERR_BADARG;
     if ((st = kv4_rows_check(&call->q, dtype))) return st;
     if (!call->out || ((uintptr_t)call->out & 15) || ((uintptr_t)call->visible & 3) || !(call->scale > 0.f) || !(call->scale <= 3.402823466e38f)) return EESD_ERR_BADARG;
+    if (!kv4::countable(c, r, n_heads)) return EESD_ERR_UNSUPPORTED;
     const kv4::Way w = kv4::way_of(c, r, n_heads);
     if (const size_t need = kv4::scratch_of(c, w)) {
         if (!call->scratch || ((uintptr_t)call->scratch & 15)) return EESD_ERR_BADARG;
@@ -933,7 +940,6 @@ int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size
     a.head = (int4 *)call->scratch;
     a.part = (float *)(a.head + kv4::grid_of(w.nt));
     const int64_t segments = (int64_t)r->B * c->n_kv_heads * a.blocks;
-    if (segments * (w.share ? w.share : 1) > 0x7fffffffLL) return EESD_ERR_UNSUPPORTED;
     const bool f32 = dtype == EESD_F32;
     const int G = c->head_dim / c->group;
     cudaStream_t s = (cudaStream_t)cuda_stream;

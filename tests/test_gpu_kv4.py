@@ -449,3 +449,37 @@ def test_refusals():
               lambda: c.read(torch.zeros(1025, 1, dtype=torch.int32, device="cuda"), 1)):
         with pytest.raises(eesd.EesdError):
             f()
+
+
+@pytest.mark.parametrize("a", ["f32", "bf16"])
+@pytest.mark.parametrize("room", [0, 30000])
+def test_largest_and_smallest_keys_and_values(a, room):
+    """values of 2^87 and 2^-100, keys of 2^80 and 2^-80 with queries that bring the scores back"""
+    B, R, H, Hkv, D, n = 1, 3, 4, 2, 128, 700
+    k, v = rows(B, n, Hkv, D, torch.float32, 3)
+    v = v / v.abs().max()
+    q = torch.randn(B, R, H, D, generator=gen(4), device="cuda")
+    for ek, ev in ((80, 87), (-80, -100), (0, 87), (0, -100)):
+        c, table = new_cache(B, n, Hkv, D, 16, 64, garbage=True)
+        c.append(k * 2.0 ** ek, v * 2.0 ** ev, table, ints([0]))
+        out = check_attend(c, table, (q * 2.0 ** -ek).to(DT[a]), [n], room=room)
+        assert out.abs().max() > 2.0 ** (ev - 8)
+
+
+def test_more_segments_than_blocks_and_one_of_many_parts():
+    """runs that hold many whole segments and pieces of two; one segment that every block has a part of"""
+    D = 64
+    B, R, H, Hkv = 40, 2, 10, 5
+    lengths = [(37 * b) % 300 + 1 for b in range(B)]
+    c, table = new_cache(B, 304, Hkv, D, 16, 32)
+    k, v = rows(B, 304, Hkv, D, torch.bfloat16, 3)
+    c.append(k, v, table, ints([0] * B))
+    q = torch.randn(B, R, H, D, generator=gen(4), device="cuda")
+    check_attend(c, table, q, lengths, room=4000)
+    check_attend(c, table, q, lengths, n_rows=[b % 3 for b in range(B)], visible=ints([[1, 3]] * B), room=4000)
+    c, table = new_cache(1, 70001, 1, D, 128, 64)
+    k, v = rows(1, 70001, 1, D, torch.bfloat16, 5)
+    c.append(k, v, table, ints([0]))
+    for a in ("f32", "bf16"):
+        for rows_, heads in ((1, 3), (3, 4), (16, 3)):
+            check_attend(c, table, torch.randn(1, rows_, heads, D, generator=gen(6), device="cuda").to(DT[a]), [70001], room=1000)

@@ -93,3 +93,14 @@ def test_scratch():
         assert L.eesd_kv4_attend_scratch_bytes(p, bad.get("r", long), bad.get("H", 4)) == 0
     f = lambda s, sn: L.eesd_kv4_attend(None, p, AT, n, attention(long, 0, tensor(), 4, 0.125, 0, AT, s, sn))
     assert f(0, need) == BADARG and f(AT + 8, need) == BADARG and f(AT, need - 1) == NOMEM
+
+
+def test_attend_refuses_what_its_integers_do_not_hold():
+    append, read, attend, n, keep = calls()
+    wide = desc(heads=1)
+    big = dict(d=C.addressof(wide), n=size(wide).total_bytes)
+    assert attend(r=rows(rows=16, B=1), H=1 << 27, **big) == UNSUPPORTED            # 2^31 columns
+    assert attend(r=rows(rows=16, B=1024, pages=2 ** 31 - 1, stride=2 ** 31 - 1), H=1 << 20, **big) == UNSUPPORTED
+    assert eesd.lib().eesd_kv4_attend_scratch_bytes(big["d"], rows(rows=16, B=1), 1 << 27) == 0
+    # the largest ranges of tokens that a table may name are not refused (no scratch memory is given)
+    assert attend(r=rows(rows=1, B=1024, pages=2 ** 27, stride=2 ** 27), H=8, **big) == BADARG
