@@ -823,18 +823,27 @@ bool countable(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     return columns <= 0x1p30 && tiles * columns * r->B <= 0x1p50;
 }
 
-// How a call is shared out: column tiles a block takes at once, blocks of a cluster (0: runs)
+// How a call is shared out: column tiles a block takes at once, blocks of a cluster (0: runs).  A unit: a tile for 8 columns.
+//   clusters  as many blocks of a cluster as fit at once, less what leaves the rounds of tiles as they are.  A round of a block's warps takes 1.2 us (64 dimensions: half of it),
+//             the second kernel of the runs, with what it reads, 6 us, and a segment's start and end in a run 2.4: clusters where those are more than the
+//             rounds beyond an even share (several sequences: three quarters of it, their lengths differ).  70B shape, one row, 4097 tokens: 9.5 us, by runs
+//             13.9; 16384: 16 and 16; 32768: 26 and 21; 4 x 8192 tokens: 16 and 23; 13B shape, 13 rows, 4000 tokens: 26 and 30; 32 x 300 tokens: 31 and 38
+//   runs      two column tiles at once where there are many units and no tile stays empty: codes are read and expanded once for both (a tile 100 ns instead of 2 x 59, fp32
+//             127 instead of 2 x 76), but with one block a multiprocessor what comes before and after takes 2 us more.  16 rows x 8 heads on 32768 tokens:
+//             121 instead of 140 us; 2 rows on 4 x 8192: 31 instead of 29
 struct Way { int nt, share; };
+// clusters of so many blocks that the machine holds at once, two blocks a multiprocessor (cudaOccupancyMaxActiveClusters)
+constexpr int kFit[kMaxShare + 1] = {0, 296, 148, 93, 71, 56, 45, 37, 33, 30, 26, 21, 21, 17, 14, 14, 14};
 Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
-    const int64_t columns = (int64_t)(n_heads / c->n_kv_heads) * r->rows, tiles = (int64_t)r->max_pages * (c->page_tokens / 16);
-    Way w;
-    w.nt = columns <= 8 ? 1 : 2;
-    const int64_t segments = (int64_t)r->B * c->n_kv_heads * ((columns + 8 * w.nt - 1) / (8 * w.nt));
-    // the fewest rounds of tiles that the machine's blocks at once allow, with the fewest blocks
-    const int64_t most = std::min<int64_t>(std::max<int64_t>(grid_of(w.nt) / segments, 1), kMaxShare), rounds = (tiles + kWarps * most - 1) / (kWarps * most);
-    w.share = (int)((tiles + kWarps * rounds - 1) / (kWarps * rounds));
-    if (segments * tiles > 64LL * grid_of(w.nt) || rounds > 32) w.share = 0;
-    return w;
+    const int64_t columns = (int64_t)(n_heads / c->n_kv_heads) * r->rows, tiles = (int64_t)r->max_pages * (c->page_tokens / 16), blocks = (columns + 7) / 8;
+    const int64_t segments = (int64_t)r->B * c->n_kv_heads * blocks, units = segments * tiles;
+    int most = kMaxShare;
+    while (most > 1 && kFit[most] < segments) most--;
+    const int64_t rounds = (tiles + kWarps * most - 1) / (kWarps * most);
+    const int64_t even = units / (kWarps * grid_of(1)) * (r->B > 1 ? 3 : 4) / 4;
+    const int64_t turns = (segments + grid_of(1) - 1) / grid_of(1);   // of segments, past what fits at once
+    if (turns * rounds <= even + 640 / c->head_dim + 2 * segments / grid_of(1)) return Way{1, (int)((tiles + kWarps * rounds - 1) / (kWarps * rounds))};
+    return Way{blocks % 2 == 0 && units > 256 * grid_of(1) ? 2 : 1, 0};
 }
 
 size_t scratch_of(const eesd_kv4 *c, const Way &w) { return w.share ? 0 : (size_t)grid_of(w.nt) * (16 + 2 * 8 * w.nt * (c->head_dim + 4) * 4); }
@@ -881,8 +890,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 template <int D, int G, bool F32> cudaError_t launch_kind(cudaStream_t s, const AttnArgs &a, int nt, int64_t segments) {
-    if (nt == 1) return a.share ? launch<D, G, 1, 1, false, F32>(s, a, segments) : launch<D, G, 1, 2, true, F32>(s, a, segments);
-    return a.share ? launch<D, G, 2, 1, false, F32>(s, a, segments) : launch<D, G, 2, 2, true, F32>(s, a, segments);
+    if (a.share) return launch<D, G, 1, 1, false, F32>(s, a, segments);
+    return nt == 1 ? launch<D, G, 1, 2, true, F32>(s, a, segments) : launch<D, G, 2, 2, true, F32>(s, a, segments);
 }
 template <int D, int G> cudaError_t launch_type(cudaStream_t s, const AttnArgs &a, bool f32, int nt, int64_t segments) {
     return f32 ? launch_kind<D, G, true>(s, a, nt, segments) : launch_kind<D, G, false>(s, a, nt, segments);
