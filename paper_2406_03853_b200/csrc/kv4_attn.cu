@@ -2,17 +2,29 @@
 //
 //   x_p = scale * sum_G s_pG (q_G . (c - z)_pG),   out = sum_p (e_p s_pG) (c - z)_pG / sum_p e_p,   e_p = exp(x_p - max x)
 //
-// The integers c - z are exact in fp16, so the scales stay outside the matrix products: a key's scales multiply the groups' scores,
-// a value's the softmax numerator.  One pass over the codes with a running maximum.
+// Codes and zero points are small whole numbers, so the scales stay outside the matrix products: a key's scales multiply the groups' scores, a
+// value's the softmax numerator. One pass over the codes with a running maximum.
 //
-// A warp takes tiles of 16 tokens.  Scores are S^T[token][column] = K Q^T (m16n8k16, columns = (row, head) pairs that share the key head),
-// outputs O^T[dimension][column] = V^T P^T, with keys and values as the 16-row operand straight from their codes in registers and
-// one 8 x 8 transposition (movmatrix) between the score's accumulators and the numerators' operand.  Tiles come through a ring of asynchronous
-// copies that belongs to the warp; the warps of a block meet once, at a segment's end.
+// A warp takes tiles of 16 tokens for 8 columns (pairs of a row and a head that share the key head) or 16. Both products have the tile as their
+// 16-row operand, straight from its codes in registers:
+//   scores   S^T[token][column] = K Q^T as whole numbers (m16n8k32, bytes): the queries of a row and head become whole numbers under one power of
+//            two, in digits of 8 bits (bf16: two, fp32: three), so a group's sum and what its zero point takes off are exact, and expanding a word of
+//            codes is two operations and a shift. (With fp16 terms of the queries, five operations a word and two for each sum, and one tile a step,
+//            the 32 sequences below took 1.7 times as long.) What it costs: a query is off by 2^-15 (fp32: 2^-23) of its head's largest
+//   outputs  O^T[dimension][column] = V^T P^T (m16n8k16, fp16): numerators of 11 bits (fp32: two terms, 22 bits) by codes set into an fp16 mantissa;
+//            one 8 x 8 transposition (movmatrix) stands between a score's accumulators and the numerators' operand
+// Sums are held in 32 bits. Tiles come through a ring of asynchronous copies that belongs to the warp; the warps of a block meet once, at a segment's
+// end.
 //
-// A segment is what one key head of one sequence has to do for up to 8 NT columns.  Two ways to share the machine:
-//   clusters  the blocks of a cluster share a segment and join their parts through each other's shared memory (one launch)
-//   runs      the tiles of all segments stand in a row and are dealt out evenly, whatever the sequences' lengths; a second kernel joins what was cut
+// A segment is what one key head of one sequence has to do for 8 NT columns. Two ways to share the machine (way_of):
+//   clusters  the blocks of a cluster share a segment and push their parts into the shared memory of the block that joins them (one launch)
+//   runs      the tiles of all segments stand in a row and are dealt out evenly, whatever the sequences' lengths; a second kernel joins what was cut.
+//             Two tiles a step of a warp (TT), which hide each other's latency: the 130001 tokens below 197 us, one tile a step 215
+//
+// What bounds it (70B shape, 64 heads on 8 of 128; B200): 32 sequences of up to 8192 tokens, one row, bf16: 51 us, 180 MB, 0.54 of the copy rate;
+// 130001 tokens, 5 rows, fp32: 197 us, 21 GFLOP. A warp's unit of 16 tokens by 8 columns is 318 instructions (fp32: 423), 17 (28) of them matrix
+// instructions, at four warps a scheduler: two thirds of the issue slots, half of the ALU pipe. Short calls (one sequence of 1056 tokens, 5 rows, 13B
+// shape: 8.4 us) are launch, four dependent reads and the joining.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <limits.h>
@@ -178,6 +190,12 @@ __device__ __forceinline__ uint32_t low(uint32_t x, const Pair &base, const Pair
 __device__ __forceinline__ uint32_t high(uint32_t x, const Pair &base, const Pair &zero) {
     uint32_t r;
     asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;\n\tadd.rn.f16x2 %0, %0, %3;" : "=&r"(r) : "r"(x), "r"(base.high), "r"(zero.high));
+    return r;
+}
+// 64 + the codes in bits 4 to 7 of x's halves
+__device__ __forceinline__ uint32_t set64(uint32_t x, const Pair &base) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(r) : "r"(x), "r"(base.high));
     return r;
 }
 // -(1024 + z) and -(64 + z) of two zero points, bytes 0 and 1 of z (below 16)
@@ -401,7 +419,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         // A numerator enters the product as e * scale * unit, with a power of two for each column that puts the largest so far near 2^4: e <=
         // 2^kRise then keeps them below fp16's range, and what is dropped is below 2^-29 of the largest.  units: the largest of the lane's
         float unit[NT][2], weight[NT][2], units = 0x1p120f;
-        float oz[F32 ? 1 : G][NT][4];   // bf16: sums of numerators times zero points (all rows alike)
+        float oz[F32 ? 1 : G][NT][4];   // bf16: sums of numerators times 64 + z (all rows alike)
 #pragma unroll
         for (int i = 0; i < NT; i++) {
 #pragma unroll
@@ -620,15 +638,15 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                         ph[i][1] = transpose(ph[i][1]);
                     }
                     // zero points of tokens 2 t, 2 t + 1 and those 8 after them.  fp32: codes less their zero points, so that nothing large cancels.  bf16:
-                    // codes as they are (a nibble in fp16's lowest bits is c 2^-24), and the zero points as rows of their own, whose sums are taken
-                    // off at the end
+                    // 64 + c, and 64 + z as rows of their own, whose sums are taken off at the end: sums in fp32 of up to 79 where a group's largest value is at least
+                    // 7.5 lose 2^-20 of the largest (measured; codes as subnormal fp16 numbers, two shifts fewer, lose 2^-15.5 inside the matrix instruction)
                     Pair z[2];
                     uint32_t az[4];
 #pragma unroll
                     for (int r = 0; r < 2; r++) {
                         const uint32_t z2 = *reinterpret_cast<const uint16_t *>(at + L::VZ + gi * 16 + 8 * r + 2 * t);
                         if (F32) z[r] = zeros(z2);
-                        else az[2 * r] = az[2 * r + 1] = __byte_perm(z2, 0, 0x4140) & 0x000f000fu;
+                        else az[2 * r] = az[2 * r + 1] = set64(__byte_perm(z2, 0, 0x4140) << 4, base);
                     }
                     if constexpr (!F32) {
 #pragma unroll
@@ -640,14 +658,13 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                         uint32_t av[4];
 #pragma unroll
                         for (int r = 0; r < 2; r++) {
-                            uint32_t y = __byte_perm(vw[w][2 * r], vw[w][2 * r + 1], q < 2 ? 0x5410 : 0x7632);
-                            if (q & 1) y >>= 8;
+                            const uint32_t y = __byte_perm(vw[w][2 * r], vw[w][2 * r + 1], q < 2 ? 0x5410 : 0x7632);
                             if (F32) {
-                                av[2 * r] = low(y, base, z[r]);
-                                av[2 * r + 1] = high(y, base, z[r]);
+                                av[2 * r] = low(q & 1 ? y >> 8 : y, base, z[r]);
+                                av[2 * r + 1] = high(q & 1 ? y >> 8 : y, base, z[r]);
                             } else {
-                                av[2 * r] = y & 0x000f000fu;
-                                av[2 * r + 1] = y & 0x00f000f0u;   // (16 c 2^-24)
+                                av[2 * r] = set64(q & 1 ? y >> 4 : y << 4, base);
+                                av[2 * r + 1] = set64(q & 1 ? y >> 8 : y, base);
                             }
                         }
 #pragma unroll
@@ -686,9 +703,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                 if constexpr (!F32) {
 #pragma unroll
                     for (int r = 0; r < D / 16; r++) {
-                        const float z = oz[r * G / (D / 16)][i][k] * 0x1p24f;
-                        o[r][i][k] = fmaf(o[r][i][k], 0x1p24f, -z);
-                        o[r][i][k + 2] = fmaf(o[r][i][k + 2], 0x1p20f, -z);
+                        const float z = oz[r * G / (D / 16)][i][k];
+                        o[r][i][k] -= z, o[r][i][k + 2] -= z;
                     }
                 }
                 if (g == 0) sh.ml[warp][c] = make_float2(mx[i][k], sum[i][k]);
@@ -823,14 +839,15 @@ bool countable(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     return columns <= 0x1p30 && tiles * columns * r->B <= 0x1p50;
 }
 
-// How a call is shared out: column tiles a block takes at once, blocks of a cluster (0: runs).  A unit: a tile for 8 columns.
-//   clusters  as many blocks of a cluster as fit at once, less what leaves the rounds of tiles as they are.  A round of a block's warps takes 1.2 us (64 dimensions: half of it),
-//             the second kernel of the runs, with what it reads, 6 us, and a segment's start and end in a run 2.4: clusters where those are more than the
-//             rounds beyond an even share (several sequences: three quarters of it, their lengths differ).  70B shape, one row, 4097 tokens: 9.5 us, by runs
-//             13.9; 16384: 16 and 16; 32768: 26 and 21; 4 x 8192 tokens: 16 and 23; 13B shape, 13 rows, 4000 tokens: 26 and 30; 32 x 300 tokens: 31 and 38
-//   runs      two column tiles at once where there are many units and no tile stays empty: codes are read and expanded once for both (a tile 100 ns instead of 2 x 59, fp32
-//             127 instead of 2 x 76), but with one block a multiprocessor what comes before and after takes 2 us more.  16 rows x 8 heads on 32768 tokens:
-//             121 instead of 140 us; 2 rows on 4 x 8192: 31 instead of 29
+// How a call is shared out: column tiles a block takes at once, blocks of a cluster (0: runs). A unit: a tile for 8 columns.
+//   clusters  as many blocks of a cluster as fit at once, less what leaves the rounds of tiles as they are. A round of a block's warps takes 1.2 us
+//             (64 dimensions: half of it), and the second kernel of the runs, with what it reads, 6 us, and a segment's start and end in a run 2.4:
+//             clusters where those are more than the rounds beyond an even share (several sequences: three quarters of it, their lengths differ). 70B
+//             shape, one row, 4097 tokens: 9.5 us, by runs 13.9; 16384: 16 and 16; 32768: 26 and 21; 4 x 8192 tokens: 16 and 23; 13B shape, 13 rows,
+//             4000 tokens: 26 and 30; 32 x 300 tokens: 31 and 38
+//   runs      two column tiles at once where there are many units and no tile stays empty: codes are read and expanded once for both (a tile 100 ns
+//             instead of 2 x 59, fp32 127 instead of 2 x 76), but with one block a multiprocessor what comes before and after takes 2 us more. 16
+//             rows x 8 heads on 32768 tokens: 121 instead of 140 us; 2 rows on 4 x 8192: 31 instead of 29
 struct Way { int nt, share; };
 // clusters of so many blocks that the machine holds at once, two blocks a multiprocessor (cudaOccupancyMaxActiveClusters)
 constexpr int kFit[kMaxShare + 1] = {0, 296, 148, 93, 71, 56, 45, 37, 33, 30, 26, 21, 21, 17, 14, 14, 14};

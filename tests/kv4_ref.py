@@ -126,8 +126,9 @@ def bound(out, A, of_rows, n, D, dtype):
     """How far attend_rows may be.  Scores: whole numbers up to the scales; queries are off by half a step of 2^-22 (bf16: 2^-14) of their row's largest at most (the largest
     is at least half of 127 * 65536, or 127 * 256, steps), and up to 4 groups' sums, two conversions and products are rounded to fp32: 16 * 2^-24.  Exponentials by
     2^-22, numerators by 2^-21 (bf16: 2^-11) and each by 2^-28 of the largest product with a value (a group's largest value is at least 7.5 scales, a
-    code at most 15).  Sums over n positions take two steps per 16 of them, and 64 for joining (bf16: of codes less 8, at most 1.1 of the largest value each);
-    the result is rounded to its type."""
+    code at most 15).  Sums over n positions take two steps per 16 of them, and 64 for joining.  bf16 sums 64 + c and 64 + z, at most 79 where the largest value is at least 7.5 scales: two
+    sums of 10.5 of it, each of n / 128 + 1 steps (eight warps or more share the positions), 21 (n / 128 + 1) <= 1.1 (n / 8 + 64) up to 1800 positions, and
+    more blocks share them beyond; the result is rounded to its type."""
     S, most, Q, M = of_rows
     f32 = dtype == torch.float32
     dx = S * 2.0 ** -20 + Q * 2.0 ** (-22 if f32 else -14)

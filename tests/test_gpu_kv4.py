@@ -483,3 +483,22 @@ def test_more_segments_than_blocks_and_one_of_many_parts():
     for a in ("f32", "bf16"):
         for rows_, heads in ((1, 3), (3, 4), (16, 3)):
             check_attend(c, table, torch.randn(1, rows_, heads, D, generator=gen(6), device="cuda").to(DT[a]), [70001], room=1000)
+
+
+@pytest.mark.parametrize("a", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [16, 200, 3000])
+@pytest.mark.parametrize("room", [0, 30000])
+def test_a_large_value_leaves_what_it_does_not_touch(a, n, room):
+    """a token whose scale is far above the others', with a code that stands for 0 (and is not 0): its dimensions are the other tokens' alone"""
+    D = 128
+    k, v = rows(1, n, 1, D, torch.float32, 11)
+    q = torch.randn(1, 1, 2, D, generator=gen(12), device="cuda").to(DT[a])
+    for big in (1e2, 1e3, 1e4, 1e5):
+        v2 = v.clone()
+        v2[:, 5] *= big
+        v2[:, 5, :, :96] = 0
+        v2[:, 5, :, 96], v2[:, 5, :, 97] = 3 * big, -3 * big
+        c, table = new_cache(1, n, 1, D, 16, 128)
+        c.append(k * 0.1, v2, table, ints([0]))
+        assert c.read(table, n)[1][0, 5, 0, :96].eq(0).all()
+        check_attend(c, table, q, [n], room=room)
