@@ -502,3 +502,64 @@ def test_a_large_value_leaves_what_it_does_not_touch(a, n, room):
         c.append(k * 0.1, v2, table, ints([0]))
         assert c.read(table, n)[1][0, 5, 0, :96].eq(0).all()
         check_attend(c, table, q, [n], room=room)
+
+
+def test_tables_of_16_million_pages():
+    """more tiles than 31 bits count, most of them in pages that do not exist: the same bits as with a narrow table, and a context of 2^31 - 1 tokens"""
+    D, Hkv, page, n = 64, 2, 128, 700
+    c, table = new_cache(1, n, Hkv, D, page, 64)
+    k, v = rows(1, n, Hkv, D, torch.float32, 3)
+    c.append(k, v, table, ints([0]))
+    wide = torch.full((1, 1 << 24), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    narrow = torch.nn.functional.pad(table, (0, 30000), value=-1)
+    for a in ("f32", "bf16"):
+        q = torch.randn(1, 16, 16, D, generator=gen(4), device="cuda").to(DT[a])
+        assert torch.equal(eesd.attend_rows(q, c, wide, ints([n])), eesd.attend_rows(q, c, narrow, ints([n])))
+    # the same heads eight times: 2^31 tiles to look for
+    c16 = eesd.KV4Cache(8, 16, D, page_tokens=page, group=64)
+    t16 = ints([[5, 0, 3, 7, 1]])
+    c16.append(k.repeat(1, 1, 8, 1)[:, :640], v.repeat(1, 1, 8, 1)[:, :640], t16, ints([0]))
+    wide[:, :6] = -1
+    wide[:, :5] = t16
+    q = torch.randn(1, 1, 16, D, generator=gen(5), device="cuda")
+    got = eesd.attend_rows(q, c16, wide, ints([2 ** 31 - 1]))
+    kk, vv = c16.read(t16, 640)
+    want, A, S = ref.attend(q, kk.double(), vv.double(), [640], None, D ** -0.5)
+    assert ((got.double() - want).abs() <= ref.bound(want, A, S, 640, D, torch.float32)).all()
+    assert c16.read(wide, 3, start=ints([2 ** 31 - 4]))[0].eq(0).all()
+
+
+def test_binding_refusals():
+    c, table = new_cache(2, 64, 2, 64, 16, 32)
+    z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device="cuda")
+    k, q, at = z(2, 3, 2, 64), z(2, 3, 4, 64), ints([0, 0])
+    rope = z(80, 32, 2)
+    for kw in (dict(n_pages=0), dict(n_kv_heads=0), dict(head_dim=96), dict(page_tokens=8), dict(group=128)):
+        with pytest.raises(eesd.EesdError):
+            eesd.KV4Cache(**{**dict(n_pages=2, n_kv_heads=2, head_dim=64), **kw})
+    for bad in (z(10, dtype=torch.uint8), z(c.layout.total_bytes), z(2, c.layout.total_bytes, dtype=torch.uint8), torch.zeros(c.layout.total_bytes, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            eesd.KV4Cache(c.n_pages, 2, 64, group=32, buffer=bad)
+    shared = (dict(page_table=table.long()), dict(page_table=table.cpu()), dict(page_table=table[:1]), dict(page_table=table[0]), dict(page_table=table[:, :0]), dict(page_table=table[:1].expand(2, -1)),
+              dict(page_table=table.t().contiguous().t()), dict(page_table=None), dict(rope=rope.double()), dict(rope=rope[:, :16]), dict(rope=rope[0]), dict(rope=rope[::2]), dict(rope=rope.cpu()),
+              dict(positions=z(2, 3)), dict(positions=z(2, 2, dtype=torch.int32)), dict(n_rows=z(3, dtype=torch.int32)), dict(n_rows=[1, 1]), dict(n_rows=at.long()))
+    call = dict(k=k, v=k, page_table=table, start=at, n_rows=None, rope=None, positions=None)
+    for kw in shared + (dict(k=k.half()), dict(k=k.bfloat16()), dict(k=q), dict(v=q), dict(k=k[:, :0]), dict(k=k[..., ::2]), dict(k=k.cpu()), dict(k=k[0]), dict(v=k[:, :2]), dict(v=k[:1]), dict(v=None),
+                        dict(start=None), dict(start=at[:1]), dict(start=at.float())):
+        with pytest.raises(ValueError):
+            c.append(**{**call, **kw})
+    call = dict(q=q, cache=c, page_table=table, n_ctx=at, n_rows=None, scale=None, visible=None, rope=None, positions=None, out=None, scratch=None)
+    for kw in shared + (dict(q=q.half()), dict(q=q[:, :, :3]), dict(q=z(2, 17, 4, 64)), dict(q=z(2, 3, 4, 32)), dict(q=q.cpu()), dict(q=None), dict(cache=table), dict(n_ctx=None), dict(n_ctx=at[:1]),
+                        dict(visible=z(2, 3)), dict(visible=ints([[1, 1]] * 2)), dict(out=q.bfloat16()), dict(out=q[:1]), dict(out=z(2, 3, 64, 4).transpose(2, 3)), dict(out=q.cpu()), dict(scratch=z(64)),
+                        dict(scratch=z(64, dtype=torch.uint8)[::2])):
+        with pytest.raises(ValueError):
+            eesd.attend_rows(**{**call, **kw})
+    for kw in (dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(out=z(2 * 3 * 4 * 64 + 1)[1:].view(2, 3, 4, 64)),
+               dict(page_table=torch.nn.functional.pad(table, (0, 99999)), scratch=z(64, dtype=torch.uint8))):
+        with pytest.raises(eesd.EesdError):
+            eesd.attend_rows(**{**call, **kw})
+    for kw in (dict(page_table=table[0]), dict(page_table=None), dict(count=0), dict(start=at[:1]), dict(n_ctx=at.long()), dict(dtype=torch.float16)):
+        with pytest.raises(ValueError):
+            c.read(**{**dict(page_table=table, count=4), **kw})
+    torch.cuda.synchronize()
