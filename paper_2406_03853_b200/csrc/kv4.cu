@@ -83,8 +83,9 @@ struct AppendArgs {
 // neighbours a lane.  The tasks' extremes are found together, the tasks halved among the lanes at each exchange, so that a group's scale is worked
 // out once, beside the others' (a task by itself, every lane its scale: 57 us instead of 28 for 5100 rows of 8 heads of 128, bf16).  Codes by the reciprocal,
 // settled by the remainder (as in w4.cu).  They meet in shared memory and go out as the tile's bytes, whole where the tile is.
-// 32 MB in 28 us: the issue slots bound it (71 % used, 240 instructions a row's keys or values), not memory (4.9 us).
-template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
+// 32 MB in 27 us: the issue slots bound it (80 % used, 250 instructions a row's keys or values), not memory (4.9 us).  Six blocks a multiprocessor
+// (left to itself five, 1.5 us more; eight the same).
+template <int D, int G, typename T> __global__ void __launch_bounds__(kThreads, 6) append_kernel(const AppendArgs a) {
     constexpr int N = D / 32, GL = 32 / G;   // GL: lanes of a group
     using L = Tile<D, G>;
     __shared__ __align__(16) unsigned char tile[L::BYTES];
@@ -256,25 +257,15 @@ struct ReadArgs {
     void *k, *v;
 };
 
-template <int N, typename T> __device__ __forceinline__ void store(T *out, const float (&w)[N]) {
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (N == 4) __stcs(reinterpret_cast<float4 *>(out), make_float4(w[0], w[1], w[2], w[3]));
-        else __stcs(reinterpret_cast<float2 *>(out), make_float2(w[0], w[1]));
-    } else {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(w[0], w[1]);
-        if constexpr (N == 4) {
-            const __nv_bfloat162 q = __floats2bfloat162_rn(w[2], w[3]);
-            __stcs(reinterpret_cast<uint2 *>(out), make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q)));
-        } else {
-            __stcs(reinterpret_cast<uint32_t *>(out), *reinterpret_cast<const uint32_t *>(&p));
-        }
-    }
-}
+// Where 16-byte piece i of a tile stands in shared memory when a lane takes N neighbouring dimensions: the values' pieces that a warp reads together are 32 apart (dimensions
+// 64 apart; N = 4: also 16), in the same banks, unless the higher bits of their number change the lowest.
+template <int D, int N> __device__ __forceinline__ int piece(int i) { return i >= D / 2 && i < D ? i ^ (i - D / 2) >> (N == 8 ? 5 : 4) : i; }
 
-// One block: kTiles neighbouring tiles of a head, brought into shared memory; a warp two tokens' keys and values of each, N = D / 32 neighbours a lane.
-// 2 x 16385 tokens of 8 heads of 128 as bf16: 46 us, 174 MB, 0.58 of the copy rate; shared memory's data path (51 %) and the issue slots (60 %) come before it.
+// One block: kTiles neighbouring tiles of a head, brought into shared memory.  A lane takes N neighbouring values of a token's keys and of its values: 16 bytes of
+// what is written.  2 x 16385 tokens of 8 heads of 128 as bf16: 32 us, 174 MB, 0.83 of the copy rate (a token a warp, N = D / 32, was 110 instructions a token and
+// head, and 46 us).
 template <int D, int G, int kTiles, typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a) {
-    constexpr int N = D / 32, GL = 32 / G;
+    constexpr int N = 16 / sizeof(T), LT = D / N, TW = 32 / LT;   // lanes of a token, tokens of a warp
     using L = Tile<D, G>;
     __shared__ __align__(16) unsigned char tiles[kTiles][L::BYTES];
     __shared__ int ends[kTiles];
@@ -295,29 +286,31 @@ template <int D, int G, int kTiles, typename T> __global__ void __launch_bounds_
         const unsigned char *src = ti + j < 0 || left <= max(lo, 16 * j) || 16 * j >= hi ? nullptr : tile_at(a.c, b, h, ti + j, L::BYTES);
         if (src)
 #pragma unroll 5
-            for (int i = kTiles == 1 ? (int)threadIdx.x : lane; i < L::BYTES / 16; i += by) reinterpret_cast<uint4 *>(tiles[j])[i] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
+            for (int i = kTiles == 1 ? (int)threadIdx.x : lane; i < L::BYTES / 16; i += by)
+                reinterpret_cast<uint4 *>(tiles[j])[piece<D, N>(i)] = __ldcs(reinterpret_cast<const uint4 *>(src) + i);
         if (kTiles == 1 ? threadIdx.x == 0 : lane == 0) ends[j] = src ? (int)min((int64_t)16, left - 16 * j) : 0;   // tokens that are there
     }
     __syncthreads();
-    const int gi = lane / GL, d = lane * N;
+    const int d = lane % LT * N, gi = d / (D / G), i = d % 64 / 8;   // i: the nibble of the values' words
     const size_t row = (size_t)a.c.Hkv * D;
     const size_t at = ((size_t)((int64_t)b * a.r.rows - first) * a.c.Hkv + h) * D + d;   // of token 0
-    const int k_at = d % 32 / 8 * (D / 8) + d / 32 * 4, k_shift = 4 * (d % 8), v_at = L::V + (d / 64 * 8 + d % 8) * 64, v_shift = 4 * (d % 64 / 8);
-    // 2^23 + c (the code's nibble set into the mantissa) - (2^23 + z), times s
-    auto value = [](uint32_t word, int shift, float z, float s) { return __fmul_rn(__uint_as_float((word >> shift & 15u) | 0x4b000000u) - z, s); };
-#pragma unroll 2
-    for (int i = 0; i < 2 * kTiles; i++) {
-        const int j = i >> 1, tok = warp + 8 * (i & 1), place = 16 * j + tok;
+    const int k_at = d % 32 / 8 * (D / 8) + d / 32 * 4, k_shift = 4 * (d % 8), v_at = d / 64 * 32 + d % 8 * 4, v_shift = 4 * (i & 1);
+    const uint32_t v_bytes = 0x0400u + i / 2 * 0x0101u;   // byte i / 2 of two words, in the halves' low bytes
+#pragma unroll 1   // (2: 36 us)
+    for (int place = warp * TW + lane / LT; place < 16 * kTiles; place += TW * kThreads / 32) {
         if (place < lo || place >= hi) continue;
+        const int j = place >> 4, tok = place & 15;
         const unsigned char *tile = tiles[j];
-        float k[N], v[N];
-#pragma unroll
-        for (int n = 0; n < N; n++) k[n] = v[n] = 0.f;
+        uint4 ko = make_uint4(0, 0, 0, 0), vo = ko;   // 0 in either type
         if (tok < ends[j]) {
             const uint32_t scales = *reinterpret_cast<const uint32_t *>(tile + L::SCALES + (gi * 16 + tok) * 4);
-            const uint32_t c = *reinterpret_cast<const uint32_t *>(tile + tok * (D / 2) + k_at) >> k_shift;
-            const unsigned char *vc = tile + v_at + (tok % 8 / 2) * 16 + (tok / 8 * 2 + tok % 2) * 4;
-            if constexpr (sizeof(T) == 2 && N == 4) {
+            const uint32_t c = *reinterpret_cast<const uint32_t *>(tile + tok * (D / 2) + k_at) >> (N == 8 ? 0 : k_shift);
+            // words of the lane's dimensions, 64 bytes apart
+            const uint32_t *vc = reinterpret_cast<const uint32_t *>(tile + piece<D, N>(L::V / 16 + v_at + tok % 8 / 2) * 16) + tok / 8 * 2 + tok % 2;
+            uint32_t v2[N / 2];   // their codes, in the lowest bits of the halves
+#pragma unroll
+            for (int n = 0; n < N / 2; n++) v2[n] = __byte_perm(vc[32 * n], vc[32 * n + 16], v_bytes) >> v_shift;
+            if constexpr (sizeof(T) == 2) {
                 // two codes at a time: 128 + c (the nibble set into the mantissa of bf16's 128) - (128 + z), times s, rounded once
                 const uint32_t zk = tile[L::KZ + gi * 16 + tok] * 0x10001u | 0x43004300u, zv = tile[L::VZ + gi * 16 + tok] * 0x10001u | 0x43004300u;
                 const uint32_t sk = __byte_perm(scales, 0, 0x1010), sv = __byte_perm(scales, 0, 0x3232);
@@ -326,24 +319,21 @@ template <int D, int G, int kTiles, typename T> __global__ void __launch_bounds_
                     asm("sub.rn.bf16x2 %0, %0, %1;\n\tmul.rn.bf16x2 %0, %0, %2;" : "+r"(r) : "r"(z), "r"(s));
                     return r;
                 };
-                const uint32_t c4 = c & 0xffffu, *v4 = reinterpret_cast<const uint32_t *>(vc);
-                const size_t to = at + place * row;
-                if (a.k) __stcs(reinterpret_cast<uint2 *>((T *)a.k + to), make_uint2(pair(c4 | c4 << 12, zk, sk), pair(c4 >> 8 | c4 << 4, zk, sk)));
-                if (a.v)
-                    __stcs(reinterpret_cast<uint2 *>((T *)a.v + to),
-                           make_uint2(pair(__byte_perm(v4[0] >> v_shift, v4[16] >> v_shift, 0x5410), zv, sv), pair(__byte_perm(v4[32] >> v_shift, v4[48] >> v_shift, 0x5410), zv, sv)));
-                continue;
+                const uint32_t c0 = c & 0xffffu, c1 = c >> 16;
+                ko = make_uint4(pair(c0 | c0 << 12, zk, sk), pair(c0 >> 8 | c0 << 4, zk, sk), pair(c1 | c1 << 12, zk, sk), pair(c1 >> 8 | c1 << 4, zk, sk));
+                vo = make_uint4(pair(v2[0], zv, sv), pair(v2[1], zv, sv), pair(v2[2], zv, sv), pair(v2[3], zv, sv));
+            } else {
+                const float sk = __uint_as_float(scales << 16), sv = __uint_as_float(scales & 0xffff0000u);
+                const float zk = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]), zv = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
+                // 2^23 + c (the code's nibble set into the mantissa) - (2^23 + z), times s
+                auto value = [](uint32_t word, float z, float s) { return __float_as_uint(__fmul_rn(__uint_as_float((word & 15u) | 0x4b000000u) - z, s)); };
+                ko = make_uint4(value(c, zk, sk), value(c >> 4, zk, sk), value(c >> 8, zk, sk), value(c >> 12, zk, sk));
+                vo = make_uint4(value(v2[0], zv, sv), value(v2[0] >> 16, zv, sv), value(v2[1], zv, sv), value(v2[1] >> 16, zv, sv));
             }
-            const float sk = __uint_as_float(scales << 16), sv = __uint_as_float(scales & 0xffff0000u);
-            const float zk = __uint_as_float(0x4b000000u | tile[L::KZ + gi * 16 + tok]), zv = __uint_as_float(0x4b000000u | tile[L::VZ + gi * 16 + tok]);
-#pragma unroll
-            for (int n = 0; n < N; n++) k[n] = value(c, 4 * n, zk, sk);
-#pragma unroll
-            for (int n = 0; n < N; n++) v[n] = value(*reinterpret_cast<const uint32_t *>(vc + n * 64), v_shift, zv, sv);
         }
         const size_t to = at + place * row;
-        if (a.k) store<N>((T *)a.k + to, k);
-        if (a.v) store<N>((T *)a.v + to, v);
+        if (a.k) __stcs(reinterpret_cast<uint4 *>((T *)a.k + to), ko);
+        if (a.v) __stcs(reinterpret_cast<uint4 *>((T *)a.v + to), vo);
     }
 }
 
@@ -460,12 +450,12 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
     a.k = k;
     a.v = v;
     const int G = c->head_dim / c->group;
-    // four tiles a block (its start costs as much as a tile) where that leaves most multiprocessors four blocks: 2 x 16385 tokens of 8 heads as
-    // bf16 45.7 us, by single tiles 47.3
-    const bool four = blocks >= 2u * 8u * 148u;
-    if (four) blocks = (unsigned int)((a.r.tiles + 3) / 4 * (int64_t)c->n_kv_heads * r->B);
-    auto kernel = out_dtype == EESD_F32 ? (four ? kv4::pick_read<4, float>(c->head_dim, G) : kv4::pick_read<1, float>(c->head_dim, G))
-                                        : (four ? kv4::pick_read<4, __nv_bfloat16>(c->head_dim, G) : kv4::pick_read<1, __nv_bfloat16>(c->head_dim, G));
+    // eight tiles a block (its start costs as much as a tile) where that leaves every multiprocessor eight blocks: 2 x 16385 tokens of 8 heads as bf16 32 us, by single
+    // tiles 43; 4 x 2047 as fp32, which would be 516 blocks, takes 3 us longer by eights
+    const bool eight = blocks >= 8u * 8u * 148u;
+    if (eight) blocks = (unsigned int)((a.r.tiles + 7) / 8 * (int64_t)c->n_kv_heads * r->B);
+    auto kernel = out_dtype == EESD_F32 ? (eight ? kv4::pick_read<8, float>(c->head_dim, G) : kv4::pick_read<1, float>(c->head_dim, G))
+                                        : (eight ? kv4::pick_read<8, __nv_bfloat16>(c->head_dim, G) : kv4::pick_read<1, __nv_bfloat16>(c->head_dim, G));
     launch_k(kernel, dim3(blocks), dim3(kv4::kThreads), 0, (cudaStream_t)cuda_stream, pdl_enabled(), a);
     return cudaGetLastError() == cudaSuccess ? EESD_OK : EESD_ERR_CUDA;
 }

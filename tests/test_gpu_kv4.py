@@ -563,3 +563,21 @@ def test_binding_refusals():
         with pytest.raises(ValueError):
             c.read(**{**dict(page_table=table, count=4), **kw})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D,group", [(64, 64), (128, 32)])
+def test_long_reads_are_those_of_their_parts(D, group, dtype):
+    """many tiles, of which a block takes several: the same values as in short reads, starts inside tiles, before the first position and past the context"""
+    B, Hkv, n = 9, 2, 9000
+    c, table = new_cache(B, n, Hkv, D, 32, group, garbage=True)
+    k, v = rows(B, n, Hkv, D, torch.bfloat16, 3)
+    c.append(k, v, table, ints([0] * B))
+    table[3, 7] = -1
+    start, n_ctx = ints([0, 5, -300, 16, 4000, 8999, 15, -1, 40]), ints([9000, 8000, 777, 9000, 0, 9000, 16, 9008, 31])
+    bits = torch.int32 if dtype == torch.float32 else torch.int16   # (positions never written hold anything, NaN included)
+    for bound in (None, n_ctx):
+        got = c.read(table, n, start=start, n_ctx=bound, dtype=dtype)
+        for i in range(0, n, 500):
+            for x, y in zip(got, c.read(table, 500, start=start + i, n_ctx=bound, dtype=dtype)):
+                assert torch.equal(x[:, i:i + 500].view(bits), y.view(bits))
