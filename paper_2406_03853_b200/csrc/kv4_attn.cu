@@ -192,12 +192,6 @@ __device__ __forceinline__ uint32_t high(uint32_t x, const Pair &base, const Pai
     asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;\n\tadd.rn.f16x2 %0, %0, %3;" : "=&r"(r) : "r"(x), "r"(base.high), "r"(zero.high));
     return r;
 }
-// 64 + the codes in bits 4 to 7 of x's halves
-__device__ __forceinline__ uint32_t set64(uint32_t x, const Pair &base) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(r) : "r"(x), "r"(base.high));
-    return r;
-}
 // -(1024 + z) and -(64 + z) of two zero points, bytes 0 and 1 of z (below 16)
 __device__ __forceinline__ Pair zeros(uint32_t z) { return Pair{__byte_perm(z, 0xe4u, 0x4140), __byte_perm(z << 4, 0xd4u, 0x4140)}; }
 __device__ __forceinline__ void copy16(uint32_t dst, const unsigned char *src) {
@@ -419,13 +413,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         // A numerator enters the product as e * scale * unit, with a power of two for each column that puts the largest so far near 2^4: e <=
         // 2^kRise then keeps them below fp16's range, and what is dropped is below 2^-29 of the largest.  units: the largest of the lane's
         float unit[NT][2], weight[NT][2], units = 0x1p120f;
-        float oz[F32 ? 1 : G][NT][4];   // bf16: sums of numerators times 64 + z (all rows alike)
 #pragma unroll
         for (int i = 0; i < NT; i++) {
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-#pragma unroll
-                for (int gi = 0; gi < (F32 ? 1 : G); gi++) oz[gi][i][k] = 0.f;
 #pragma unroll
             for (int k = 0; k < 2; k++) mx[i][k] = kLowest, sum[i][k] = 0.f, unit[i][k] = units, weight[i][k] = 0.f, alpha[i][k] = sh.alpha[i * 8 + 2 * t + k];
 #pragma unroll
@@ -591,8 +580,6 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                         const float f0 = ex2(shift);
 #pragma unroll
                         for (int r = 0; r < D / 16; r++) o[r][i][k] *= f0, o[r][i][k + 2] *= f0;
-#pragma unroll
-                        for (int gi = 0; gi < (F32 ? 1 : G); gi++) oz[gi][i][k] *= f0, oz[gi][i][k + 2] *= f0;
                     }
             }
             // ---- numerators
@@ -637,21 +624,11 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                         ph[i][0] = transpose(ph[i][0]);
                         ph[i][1] = transpose(ph[i][1]);
                     }
-                    // zero points of tokens 2 t, 2 t + 1 and those 8 after them.  fp32: codes less their zero points, so that nothing large cancels.  bf16:
-                    // 64 + c, and 64 + z as rows of their own, whose sums are taken off at the end: sums in fp32 of up to 79 where a group's largest value is at least
-                    // 7.5 lose 2^-20 of the largest (measured; codes as subnormal fp16 numbers, two shifts fewer, lose 2^-15.5 inside the matrix instruction)
+                    // zero points of tokens 2 t, 2 t + 1 and those 8 after them.  Codes enter less their zero points: beside sums of 64 + c and of 64 + z, taken off
+                    // one another at the end, what the codes stand for would lose bits to sums ten times as large and more
                     Pair z[2];
-                    uint32_t az[4];
 #pragma unroll
-                    for (int r = 0; r < 2; r++) {
-                        const uint32_t z2 = *reinterpret_cast<const uint16_t *>(at + L::VZ + gi * 16 + 8 * r + 2 * t);
-                        if (F32) z[r] = zeros(z2);
-                        else az[2 * r] = az[2 * r + 1] = set64(__byte_perm(z2, 0, 0x4140) << 4, base);
-                    }
-                    if constexpr (!F32) {
-#pragma unroll
-                        for (int i = 0; i < NT; i++) mma(oz[gi][i], az, ph[i][0], ph[i][1]);
-                    }
+                    for (int r = 0; r < 2; r++) z[r] = zeros(*reinterpret_cast<const uint16_t *>(at + L::VZ + gi * 16 + 8 * r + 2 * t));
 #pragma unroll
                     for (int r16 = gi * (D / 16) / G; r16 < (gi + 1) * (D / 16) / G; r16++) {
                         const int w = r16 / 4, q = r16 % 4;   // nibbles 2 q, 2 q + 1 of the words
@@ -659,13 +636,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
 #pragma unroll
                         for (int r = 0; r < 2; r++) {
                             const uint32_t y = __byte_perm(vw[w][2 * r], vw[w][2 * r + 1], q < 2 ? 0x5410 : 0x7632);
-                            if (F32) {
-                                av[2 * r] = low(q & 1 ? y >> 8 : y, base, z[r]);
-                                av[2 * r + 1] = high(q & 1 ? y >> 8 : y, base, z[r]);
-                            } else {
-                                av[2 * r] = set64(q & 1 ? y >> 4 : y << 4, base);
-                                av[2 * r + 1] = set64(q & 1 ? y >> 8 : y, base);
-                            }
+                            av[2 * r] = low(q & 1 ? y >> 8 : y, base, z[r]);
+                            av[2 * r + 1] = high(q & 1 ? y >> 8 : y, base, z[r]);
                         }
 #pragma unroll
                         for (int i = 0; i < NT; i++) {
@@ -700,13 +672,6 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             for (int k = 0; k < 2; k++) {
                 const int c = i * 8 + 2 * t + k;
                 const float worth = 1.f / unit[i][k];
-                if constexpr (!F32) {
-#pragma unroll
-                    for (int r = 0; r < D / 16; r++) {
-                        const float z = oz[r * G / (D / 16)][i][k];
-                        o[r][i][k] -= z, o[r][i][k + 2] -= z;
-                    }
-                }
                 if (g == 0) sh.ml[warp][c] = make_float2(mx[i][k], sum[i][k]);
 #pragma unroll
                 for (int r = 0; r < D / 16; r++) sh.o[warp][c][16 * r + g] = o[r][i][k] * worth, sh.o[warp][c][16 * r + 8 + g] = o[r][i][k + 2] * worth;
