@@ -11,8 +11,9 @@
 //            two, in digits of 8 bits (bf16: two, fp32: three), so a group's sum and what its zero point takes off are exact, and expanding a word of
 //            codes is two operations and a shift. (With fp16 terms of the queries, five operations a word and two for each sum, and one tile a step,
 //            the 32 sequences below took 1.7 times as long.) What it costs: a query is off by 2^-15 (fp32: 2^-23) of its head's largest
-//   outputs  O^T[dimension][column] = V^T P^T (m16n8k16, fp16): numerators of 11 bits (fp32: two terms, 22 bits) by codes set into an fp16 mantissa;
-//            one 8 x 8 transposition (movmatrix) stands between a score's accumulators and the numerators' operand
+//   outputs  O^T[dimension][column] = V^T P^T (m16n8k16, fp16): numerators of two fp16 terms (22 bits, for bf16 rows too: with one, pairs of positions
+//            that cancel would leave errors of 2^-12 of either) by codes set into an fp16 mantissa; an 8 x 8 transposition (movmatrix) stands between a
+//            score's accumulators and the numerators' operand
 // Sums are held in 32 bits. Tiles come through a ring of asynchronous copies that belongs to the warp; the warps of a block meet once, at a segment's
 // end.
 //
@@ -617,10 +618,8 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                         }
                         ph[i][0] = pack(y[0], y[1]);
                         ph[i][1] = pack(y[2], y[3]);
-                        if (F32) {
-                            pl[i][0] = transpose(pack_rest(y[0], y[1], ph[i][0]));
-                            pl[i][1] = transpose(pack_rest(y[2], y[3], ph[i][1]));
-                        }
+                        pl[i][0] = transpose(pack_rest(y[0], y[1], ph[i][0]));
+                        pl[i][1] = transpose(pack_rest(y[2], y[3], ph[i][1]));
                         ph[i][0] = transpose(ph[i][0]);
                         ph[i][1] = transpose(ph[i][1]);
                     }
@@ -642,7 +641,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
 #pragma unroll
                         for (int i = 0; i < NT; i++) {
                             mma(o[r16][i], av, ph[i][0], ph[i][1]);
-                            if (F32) mma(o[r16][i], av, pl[i][0], pl[i][1]);
+                            mma(o[r16][i], av, pl[i][0], pl[i][1]);
                         }
                     }
                 }

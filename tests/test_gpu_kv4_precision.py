@@ -20,6 +20,34 @@ def half_step(dtype):
     return 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
 
 
+def bound(out, A, of_rows, n, dtype):
+    """How far a result may be when nothing is dearer than fp32.  A = sum p |v|, S = scale sum |q k|, Q = scale max |q| sum |k|.
+    Scores: two fp16 terms of a query leave 2^-22 of it, or 2^-25 where the largest is at least 2^14 (2^-39 of it); up to 4 groups' sums of 32 to 128 products and
+    their scales, at most 16 roundings of 2^-24.  Exponentials 2^-22, numerators' two terms 2^-22 and the product before them 2^-23, each by 2^-28 of the largest
+    product with a value.  Sums of n positions, at least 8 warps: two roundings of 2^-24 per 16 positions and 64 for joining."""
+    S, most, Q, _ = of_rows
+    dx = S * (2.0 ** -22 + 2.0 ** -20) + Q * 2.0 ** -39
+    rel = 2 * dx + 3 * 2.0 ** -22 + (n / 64 + 64) * 2.0 ** -24
+    return A * rel[..., None] * (1 + 1e-3) + (n * 2.0 ** -28 * most)[..., None] + half_step(dtype) * out.abs() + 1e-37
+
+
+def check(cache, table, q, n_ctx, room=0, scale=None, **kw):
+    D = q.shape[-1]
+    n = table.shape[1] * cache.page_tokens
+    k, v = cache.read(table, n)
+    out = eesd.attend_rows(q, cache, pad(table, room), ints(n_ctx), scale=scale, **{i: x for i, x in kw.items()})
+    qq = q.float()
+    if kw.get("rope") is not None:
+        R = q.shape[1]
+        where = kw["positions"].cpu().numpy() if kw.get("positions") is not None else np.array([[L - R + m for m in range(R)] for L in n_ctx])
+        qq = torch.from_numpy(ref.turn(qq.cpu().numpy(), kw["rope"], where)).cuda()
+    want, A, of_rows = ref.attend(qq, k.double(), v.double(), n_ctx, None, scale or D ** -0.5, kw.get("visible"))
+    tol = bound(want, A, of_rows, max(n_ctx), q.dtype)
+    off = (out.double() - want).abs()
+    assert (off <= tol).all(), (float((off / tol).nan_to_num(1e30).max()), float(off.max()))
+    return out
+
+
 @pytest.mark.parametrize("a", ["bf16", "f32"])
 def test_long_even_sums(a):
     """Equal scores over 2^18 positions, 32768 of them a warp: the sums are of what the codes stand for, and nothing larger beside it.  Values of -1, 0 and 1 times a
@@ -44,3 +72,22 @@ def test_long_even_sums(a):
     tol = 8 * 2048 * 2.0 ** -22 * (2 * parts + 16) / n + (half_step(DT[a]) + 2.0 ** -20) * want.abs()
     off = (out - want).abs()
     assert (off <= tol).all(), float((off / tol).max())
+
+
+@pytest.mark.parametrize("a", ["bf16", "f32"])
+@pytest.mark.parametrize("room", [0, 30000])
+@pytest.mark.parametrize("D,group", [(64, 64), (128, 32), (128, 128)])
+def test_numerators_that_cancel(D, group, room, a):
+    """pairs of positions with opposite values and nearly equal scores: what is left of them is far below either"""
+    B, R, H, Hkv, n = 1, 3, 4, 2, 192
+    c, table = new_cache(B, n, Hkv, D, 16, group)
+    g = gen(2)
+    v = torch.randint(-7, 8, (B, n, Hkv, D), generator=g, device="cuda").float()
+    v[..., ::32], v[..., 1::32] = 8, -7                    # (a scale of 1, and zero points that keep every value, and its opposite, as it is)
+    v[:, 1::2] = -v[:, ::2]
+    k = torch.randn(B, n, Hkv, D, generator=g, device="cuda") * 2.0 ** -13
+    c.append(k, v, table, ints([0]))
+    assert torch.equal(c.read(table, n)[1], v)
+    q = torch.randn(B, R, H, D, generator=g, device="cuda").to(DT[a])
+    out = check(c, table, q, [n], room)
+    assert out[:, -1].float().abs().mean() < 2.0 ** -10
