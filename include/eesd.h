@@ -607,13 +607,13 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  * from n on are 0.  With `visible` a row sees its own key only where its own bit is set.
  * q in dtype, out contiguous [B][rows][n_heads][head_dim] in dtype, overlapping no input.  scratch: device, 16-byte aligned, eesd_kv4_attend_scratch_bytes
  * bytes (0: it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.
- * Arithmetic: sums, maxima and exponentials are fp32.  A row and head's queries are taken as whole numbers of 24 bits (dtype EESD_BF16: 16) under a power of
- * two: off by at most 2^-22 (2^-14) of the largest; their products with codes are exact.  A softmax numerator times its value's scale is taken as two fp16 terms:
- * off by at most 2^-22 of itself, or 2^-29 of the row's largest.  The
- * order of additions follows from B, rows, n_heads, max_pages and the lengths: the same call has the same bits, a row among others or in a wider table may round otherwise.
+ * Arithmetic, of either dtype: sums, maxima and exponentials are fp32.  A turned query is taken as two fp16 terms under a power of two of its row and head: off by at
+ * most 2^-22 of itself, or 2^-39 of the largest of its row and head; codes less zero points enter exactly.  A softmax numerator times its value's scale is
+ * taken as two fp16 terms: off by at most 2^-22 of itself, or 2^-29 of the row's largest.  The order of additions follows from B, rows, n_heads, max_pages and
+ * the lengths: the same call has the same bits, a row among others or in a wider table may round otherwise.
  * A row of queries that holds a NaN or an infinity gives NaN.
- * Queries whose largest is below 2^-100 are taken as if it were 2^-100; keys and values from 2^88 on may overflow.  UNSUPPORTED: rows * n_heads above 2^30,
- * or that times B and the table's tiles above 2^50. */
+ * Scores may overflow where sums of query times key pass 2^115, results where 256 times a row's sum of numerators times values passes fp32's range.
+ * UNSUPPORTED: rows * n_heads above 2^30, or that times B and the table's tiles above 2^50. */
 typedef struct eesd_kv4_attention {
     eesd_kv4_rows rows;
     eesd_kv4_tensor q;

@@ -2,15 +2,14 @@
 //
 //   x_p = scale * sum_G s_pG (q_G . (c - z)_pG),   out = sum_p (e_p s_pG) (c - z)_pG / sum_p e_p,   e_p = exp(x_p - max x)
 //
-// Codes and zero points are small whole numbers, so the scales stay outside the matrix products: a key's scales multiply the groups' scores, a
+// Codes less zero points are small whole numbers, so the scales stay outside the matrix products: a key's scales multiply the groups' scores, a
 // value's the softmax numerator. One pass over the codes with a running maximum.
 //
 // A warp takes tiles of 16 tokens for 8 columns (pairs of a row and a head that share the key head) or 16. Both products have the tile as their
 // 16-row operand, straight from its codes in registers:
-//   scores   S^T[token][column] = K Q^T as whole numbers (m16n8k32, bytes): the queries of a row and head become whole numbers under one power of
-//            two, in digits of 8 bits (bf16: two, fp32: three), so a group's sum and what its zero point takes off are exact, and expanding a word of
-//            codes is two operations and a shift. (With fp16 terms of the queries, five operations a word and two for each sum, and one tile a step,
-//            the 32 sequences below took 1.7 times as long.) What it costs: a query is off by 2^-15 (fp32: 2^-23) of its head's largest
+//   scores   S^T[token][column] = K Q^T (m16n8k16, fp16): queries of two fp16 terms under a power of two that puts a row and head's largest at 2^14, so that
+//            each keeps 22 bits of its own down to 2^-18 of the largest; codes less their zero points, exactly. (As whole numbers of 16 or 24 bits by bytes,
+//            which takes fewer operations a code and 8 of the 32 sequences' 66 us below less, one loud channel would cost all others their bits)
 //   outputs  O^T[dimension][column] = V^T P^T (m16n8k16, fp16): numerators of two fp16 terms (22 bits, for bf16 rows too: with one, pairs of positions
 //            that cancel would leave errors of 2^-12 of either) by codes set into an fp16 mantissa; an 8 x 8 transposition (movmatrix) stands between a
 //            score's accumulators and the numerators' operand
@@ -22,13 +21,14 @@
 //   runs      the tiles of all segments stand in a row and are dealt out evenly, whatever the sequences' lengths; a second kernel joins what was cut.
 //             Two tiles a step of a warp (TT), which hide each other's latency: the 130001 tokens below 197 us, one tile a step 215
 //
-// What bounds it (70B shape, 64 heads on 8 of 128; B200): 32 sequences of up to 8192 tokens, one row, bf16: 51 us, 180 MB, 0.54 of the copy rate;
-// 130001 tokens, 5 rows, fp32: 197 us, 21 GFLOP. A warp's unit of 16 tokens by 8 columns is 318 instructions (fp32: 423), 17 (28) of them matrix
+// What bounds it (70B shape, 64 heads on 8 of 128; B200): 32 sequences of up to 8192 tokens, one row, bf16: 66 us, 180 MB, 0.42 of the copy rate;
+// 130001 tokens, 5 rows, fp32: 217 us, 21 GFLOP. A warp's unit of 16 tokens by 8 columns is 318 instructions (fp32: 423), 17 (28) of them matrix
 // instructions, at four warps a scheduler: two thirds of the issue slots, half of the ALU pipe. Short calls (one sequence of 1056 tokens, 5 rows, 13B
 // shape: 8.4 us) are launch, four dependent reads and the joining.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <limits.h>
+#include <math.h>
 
 #include <algorithm>
 #include <atomic>
@@ -58,7 +58,8 @@ struct AttnArgs {
     const void *q;
     int64_t qs[3];
     void *out;
-    float scale2;        // scale * log2(e)
+    float scale2;        // scale * log2(e), as scale2 * 2^scale_exp, 0.5 <= scale2 < 1
+    int scale_exp;
     int B, rows, heads;  // heads: query heads of a key head
     int blocks;          // column blocks of a key head
     int share;           // blocks of a cluster (runs: 0)
@@ -174,12 +175,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// bytes 0 .. 15 by digits -128 .. 127
-__device__ __forceinline__ void imma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 // c - z of two codes, exactly: the low nibbles of x's bytes 0 and 2 set into the mantissa of 1024, or the high ones into that of 64, less what the zero
 // point makes of it.  (The two bases in registers: with mask and base both known the compiler would take two operations for one.)
 struct Pair { uint32_t low, high; };
@@ -193,7 +188,9 @@ __device__ __forceinline__ uint32_t high(uint32_t x, const Pair &base, const Pai
     asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;\n\tadd.rn.f16x2 %0, %0, %3;" : "=&r"(r) : "r"(x), "r"(base.high), "r"(zero.high));
     return r;
 }
-// -(1024 + z) and -(64 + z) of two zero points, bytes 0 and 1 of z (below 16)
+// -(1024 + z) and -(64 + z) twice, of a zero point below 16
+__device__ __forceinline__ Pair zero_twice(uint32_t z) { return Pair{__byte_perm(z, 0xe4u, 0x4040), __byte_perm(z << 4, 0xd4u, 0x4040)}; }
+// the same of two zero points, bytes 0 and 1 of z
 __device__ __forceinline__ Pair zeros(uint32_t z) { return Pair{__byte_perm(z, 0xe4u, 0x4140), __byte_perm(z << 4, 0xd4u, 0x4140)}; }
 __device__ __forceinline__ void copy16(uint32_t dst, const unsigned char *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -226,11 +223,9 @@ template <int D, int G, int NT, int TT> struct Shared {
         unsigned char ring[kWarps][STAGES][TT * Tile<D, G>::BYTES];
         float o[kWarps][C][D + 4];   // the warps' outputs
     };
-    uint32_t q[NT][D / 32][32][4];    // digits 0 and 1 of the queries, in operand order
-    uint32_t q2[NT][D / 32][32][2];   // digit 2 (fp32 queries)
-    int2 qsum[C][G];                  // of a group: the sum of digits 0 and 1 together, and of digit 2
+    uint32_t q[NT][D / 32][2][32][4]; // the queries' terms, in operand order
     float2 ml[kWarps][C];   // the warps' maxima and sums
-    float alpha[C];         // what a unit of its scores is worth
+    float2 alpha[C];        // what a unit of its scores is worth, as two factors
     // clusters: the blocks' parts of the results that this block joins: [block][its share], and their maxima and sums
     float4 in_y[C * D / 4 + kMaxShare];
     float2 in_ml[kMaxShare][C];
@@ -345,7 +340,7 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
         for (int i = 0; i < kStages - 1; i++) fetch(i, first + i * step, now.pages[i]);
         Pages next_pages = now.pages[kStages - 1];
 
-        // ---- queries: turned, and as whole numbers of 16 (fp32: 24) bits under a power of two of their column, in digits of 8 bits
+        // ---- queries: turned, and as two fp16 terms under a power of two of their column
 #pragma unroll
         for (int i = 0; i < NT; i++) {
             const int c = warp + 8 * i;
@@ -364,36 +359,21 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             }
             most = warp_max(most);
             bad = __any_sync(0xffffffffu, bad);
-            constexpr int kBits = F32 ? 22 : 14;
-            int ex = max((int)(__float_as_uint(most) >> 23) - 127, -100);   // floor(log2), not below -100
-            if (most * power(kBits - ex) > (F32 ? 127.f * 65536.f : 127.f * 256.f)) ex++;   // (the first digit's range)
-            if (lane == 0) sh.alpha[c] = bad ? __uint_as_float(0x7fc00000u) : a.scale2 * power(ex - kBits);
-            int2 sum = make_int2(0, 0);
+            // The largest comes to 2^14 .. 2^15 (subnormal ones to less), in two factors since one may pass fp32's range.  A score is (sum * first) * a key's scale * second, first
+            // being kept from where sums (below 2^26) by the largest or the least scales would leave fp32's range; it takes all but at the ends
+            const int ex = most == 0.f ? 0 : max((int)(__float_as_uint(most) >> 23) - 127, -126), up = 14 - ex;
+            const float up0 = power(up >> 1), up1 = power(up - (up >> 1));
+            const int worth = a.scale_exp - up, first = min(max(worth, -60), 40), rest = min(max(worth - first, -126), 127);
+            if (lane == 0) sh.alpha[c] = make_float2(bad ? __uint_as_float(0x7fc00000u) : a.scale2 * power(first), power(rest));
 #pragma unroll
             for (int k = 0; k < QK; k++) {
-                const int x = __float2int_rn(qv[k].x * power(kBits - ex)), y = __float2int_rn(qv[k].y * power(kBits - ex));
-                // word 0 of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + 0, 2, 4, 6, word 1 the others; the lane has dimensions 64 k + 2 lane and + 1
-                const int slot = warp * 4 + lane % 16 / 4, byte = lane % 4;
-                const int xl = (int8_t)x, yl = (int8_t)y, xh = (x - xl) >> 8, yh = (y - yl) >> 8;   // the last digit, and the others
-                int8_t *q = reinterpret_cast<int8_t *>(sh.q[i][2 * k + lane / 16][slot]) + byte;
-                const int xm = F32 ? (int8_t)xh : xl, ym = F32 ? (int8_t)yh : yl;
-                q[0] = (int8_t)(F32 ? (xh - xm) >> 8 : xh), q[4] = (int8_t)(F32 ? (yh - ym) >> 8 : yh);
-                q[8] = (int8_t)xm, q[12] = (int8_t)ym;
-                if (F32) {
-                    int8_t *q2 = reinterpret_cast<int8_t *>(sh.q2[i][2 * k + lane / 16][slot]) + byte;
-                    q2[0] = (int8_t)xl, q2[4] = (int8_t)yl;
-                }
-                // a group's sums
-                sum.x += F32 ? xh + yh : x + y, sum.y += xl + yl;
-                if (G > 1 || k == QK - 1) {
-#pragma unroll
-                    for (int o = 1; o < (G == J ? 16 : 32); o <<= 1) {
-                        sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
-                        sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
-                    }
-                    if (lane % (G == J ? 16 : 32) == 0) sh.qsum[c][G == J ? 2 * k + lane / 16 : G > 1 ? k : 0] = sum;
-                    sum = make_int2(0, 0);
-                }
+                // word w of lane 4 (c % 8) + t holds dimensions 32 j + 8 t + w and + 4; the lane has dimensions 64 k + 2 lane and + 1
+                const float x = qv[k].x * up0 * up1, y = qv[k].y * up0 * up1;
+                const uint32_t h = pack(x, y), l = pack_rest(x, y, h);
+                const int j = 2 * k + lane / 16, slot = warp * 4 + lane % 16 / 4, word = lane % 2 * 2, half = lane % 4 / 2;
+                uint16_t *qh = reinterpret_cast<uint16_t *>(sh.q[i][j][0][slot]) + 2 * word + half, *ql = reinterpret_cast<uint16_t *>(sh.q[i][j][1][slot]) + 2 * word + half;
+                qh[0] = (uint16_t)h, qh[2] = (uint16_t)(h >> 16);
+                ql[0] = (uint16_t)l, ql[2] = (uint16_t)(l >> 16);
             }
         }
         __syncthreads();
@@ -411,19 +391,26 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
             }
 
         float o[D / 16][NT][4], mx[NT][2], sum[NT][2], alpha[NT][2];
+        bool apart = false;   // some column's second factor is not 1
         // A numerator enters the product as e * scale * unit, with a power of two for each column that puts the largest so far near 2^4: e <=
         // 2^kRise then keeps them below fp16's range, and what is dropped is below 2^-29 of the largest.  units: the largest of the lane's
         float unit[NT][2], weight[NT][2], units = 0x1p120f;
 #pragma unroll
         for (int i = 0; i < NT; i++) {
 #pragma unroll
-            for (int k = 0; k < 2; k++) mx[i][k] = kLowest, sum[i][k] = 0.f, unit[i][k] = units, weight[i][k] = 0.f, alpha[i][k] = sh.alpha[i * 8 + 2 * t + k];
+            for (int k = 0; k < 2; k++) {
+                mx[i][k] = kLowest, sum[i][k] = 0.f, unit[i][k] = units, weight[i][k] = 0.f;
+                const float2 worth = sh.alpha[i * 8 + 2 * t + k];
+                alpha[i][k] = worth.x;
+                apart |= worth.y != 1.f;
+            }
 #pragma unroll
             for (int r = 0; r < D / 16; r++)
 #pragma unroll
                 for (int k = 0; k < 4; k++) o[r][i][k] = 0.f;
         }
 
+        apart = __any_sync(0xffffffffu, apart);
         int stage = 0;
         for (int tile = first; tile < tile1; tile += step, stage = (stage + 1) % kStages) {
             wait_copies<kStages - 2>();
@@ -451,66 +438,58 @@ template <int D, int G, int NT, int TT, bool RUNS, bool F32> __global__ void __l
                 }
 #pragma unroll
             for (int gi = 0; gi < G; gi++) {
-                int acc[TT][NT][F32 ? 3 : 2][4];
+                float acc[TT][NT][4];
+                float ks[TT][2];
+                Pair z[TT][2];
+#pragma unroll
+                for (int u = 0; u < TT; u++) {
+#pragma unroll
+                    for (int r = 0; r < 2; r++) {
+                        const uint32_t word = reinterpret_cast<const uint32_t *>(src + u * L::BYTES + L::SCALES)[gi * 16 + g + 8 * r];
+                        ks[u][r] = __uint_as_float(word << 16);
+                        vs[u][gi][r] = __uint_as_float(word & 0xffff0000u);
+                        z[u][r] = zero_twice(src[u * L::BYTES + L::KZ + gi * 16 + g + 8 * r]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; i++)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) acc[u][i][k] = 0.f;
+                }
+#pragma unroll
+                for (int j = gi * J / G; j < (gi + 1) * J / G; j++) {
+#pragma unroll
+                    for (int u = 0; u < TT; u++) {
+                        const uint32_t w0 = kw[u][0][j], w1 = kw[u][1][j], x0 = w0 >> 8, x1 = w1 >> 8;
+                        const uint32_t c0[4] = {low(w0, base, z[u][0]), low(w1, base, z[u][1]), high(w0, base, z[u][0]), high(w1, base, z[u][1])};
+                        const uint32_t c1[4] = {low(x0, base, z[u][0]), low(x1, base, z[u][1]), high(x0, base, z[u][0]), high(x1, base, z[u][1])};
+#pragma unroll
+                        for (int i = 0; i < NT; i++) {
+                            const uint4 qh = *reinterpret_cast<const uint4 *>(sh.q[i][j][0][lane]), ql = *reinterpret_cast<const uint4 *>(sh.q[i][j][1][lane]);
+                            mma(acc[u][i], c0, ql.x, ql.y);
+                            mma(acc[u][i], c1, ql.z, ql.w);
+                            mma(acc[u][i], c0, qh.x, qh.y);
+                            mma(acc[u][i], c1, qh.z, qh.w);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int u = 0; u < TT; u++)
 #pragma unroll
                     for (int i = 0; i < NT; i++)
 #pragma unroll
-                        for (int p = 0; p < (F32 ? 3 : 2); p++)
-#pragma unroll
-                            for (int k = 0; k < 4; k++) acc[u][i][p][k] = 0;
-#pragma unroll
-                for (int j = gi * J / G; j < (gi + 1) * J / G; j++) {
-#pragma unroll
-                    for (int u = 0; u < TT; u++) {
-                        const uint32_t w0 = kw[u][0][j], w1 = kw[u][1][j], w[4] = {w0 & 0x0f0f0f0fu, w1 & 0x0f0f0f0fu, w0 >> 4 & 0x0f0f0f0fu, w1 >> 4 & 0x0f0f0f0fu};
-#pragma unroll
-                        for (int i = 0; i < NT; i++) {
-                            const uint4 q = *reinterpret_cast<const uint4 *>(sh.q[i][j][lane]);
-                            imma(acc[u][i][0], w, q.x, q.y);
-                            imma(acc[u][i][1], w, q.z, q.w);
-                            if constexpr (F32) {
-                                const uint2 q2 = *reinterpret_cast<const uint2 *>(sh.q2[i][j][lane]);
-                                imma(acc[u][i][2], w, q2.x, q2.y);
-                            }
+                        for (int k = 0; k < 4; k++) {
+                            const float v = acc[u][i][k] * alpha[i][k & 1];
+                            x[u][i][k] = gi ? fmaf(v, ks[u][k >> 1], x[u][i][k]) : v * ks[u][k >> 1];
                         }
-                    }
-                }
-                int2 qs[NT][2];
+            }
+            if (apart) {
 #pragma unroll
-                for (int i = 0; i < NT; i++)
-#pragma unroll
-                    for (int k = 0; k < 2; k++) qs[i][k] = sh.qsum[i * 8 + 2 * t + k][gi];
-#pragma unroll
-                for (int u = 0; u < TT; u++) {
-                    float ks[2];
-                    int z[2];
-#pragma unroll
-                    for (int r = 0; r < 2; r++) {
-                        const uint32_t word = reinterpret_cast<const uint32_t *>(src + u * L::BYTES + L::SCALES)[gi * 16 + g + 8 * r];
-                        ks[r] = __uint_as_float(word << 16);
-                        vs[u][gi][r] = __uint_as_float(word & 0xffff0000u);
-                        z[r] = src[u * L::BYTES + L::KZ + gi * 16 + g + 8 * r];
-                    }
+                for (int u = 0; u < TT; u++)
 #pragma unroll
                     for (int i = 0; i < NT; i++)
 #pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            // sums of q c less the zero point's part: whole numbers until here
-                            const int first = acc[u][i][0][k] * 256 + acc[u][i][1][k] - z[k >> 1] * qs[i][k & 1].x;
-                            float v = (float)first;
-                            if constexpr (F32) v = fmaf(v, 256.f, (float)(acc[u][i][2][k] - z[k >> 1] * qs[i][k & 1].y));
-                            x[u][i][k] = gi ? fmaf(v, ks[k >> 1], x[u][i][k]) : v * ks[k >> 1];
-                        }
-                }
+                        for (int k = 0; k < 4; k++) x[u][i][k] *= sh.alpha[i * 8 + 2 * t + (k & 1)].y;
             }
-#pragma unroll
-            for (int u = 0; u < TT; u++)
-#pragma unroll
-                for (int i = 0; i < NT; i++)
-#pragma unroll
-                    for (int k = 0; k < 4; k++) x[u][i][k] *= alpha[i][k & 1];
             // ---- masks
             uint32_t hidden = 0;   // bit 4 (u NT + i) + k
             const bool masked = old - tile * 16 < 16 * TT || here != (1u << TT) - 1;
@@ -918,7 +897,7 @@ int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size
     a.q = call->q.data;
     a.qs[0] = call->q.stride_b, a.qs[1] = call->q.stride_row, a.qs[2] = call->q.stride_head;
     a.out = call->out;
-    a.scale2 = call->scale * 1.4426950408889634f;
+    a.scale2 = (float)frexp((double)call->scale * 1.4426950408889634, &a.scale_exp);
     a.B = r->B;
     a.rows = r->rows;
     a.heads = n_heads / c->n_kv_heads;

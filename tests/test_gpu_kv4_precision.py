@@ -91,3 +91,80 @@ def test_numerators_that_cancel(D, group, room, a):
     q = torch.randn(B, R, H, D, generator=g, device="cuda").to(DT[a])
     out = check(c, table, q, [n], room)
     assert out[:, -1].float().abs().mean() < 2.0 ** -10
+
+
+@pytest.mark.parametrize("a", ["bf16", "f32"])
+@pytest.mark.parametrize("room", [0, 30000])
+@pytest.mark.parametrize("D,group,R,H", [(64, 32, 1, 2), (128, 32, 5, 8), (128, 64, 16, 2), (128, 128, 3, 4)])
+def test_queries_with_a_loud_channel(D, group, R, H, room, a):
+    """one channel of the queries far above the others, where the keys are nothing (or little): the others keep their own bits"""
+    Hkv, n = 2, 500
+    k, v = rows(1, n, Hkv, D, torch.float32, 5)
+    for loud, there in ((100.0, 0.0), (2.0 ** 14, 0.0), (1000.0, 1e-4), (2.0 ** 17, 0.0)):
+        k2 = k.clone()
+        k2[..., 5] *= there
+        c, table = new_cache(1, n, Hkv, D, 16, group)
+        c.append(k2, v, table, ints([0]))
+        q = torch.randn(1, R, H, D, generator=gen(6), device="cuda")
+        q[..., 5] *= loud
+        check(c, table, q.to(DT[a]), [n], room)
+
+
+@pytest.mark.parametrize("a", ["bf16", "f32"])
+@pytest.mark.parametrize("room", [0, 30000])
+def test_loud_channels_turned(a, room):
+    """a pair of loud channels under rotary angles, plain queries beside it"""
+    D, n, R, H, Hkv = 128, 700, 4, 8, 2
+    rope = rope_table(n, D)
+    k, v = rows(1, n, Hkv, D, torch.float32, 7)
+    k[..., 64:66] = 0
+    c, table = new_cache(1, n, Hkv, D, 16, 64)
+    c.append(k, v, table, ints([0]), rope=rope)
+    q = torch.randn(1, R, H, D, generator=gen(8), device="cuda")
+    q[..., 64:66] *= 3000
+    check(c, table, q.to(DT[a]), [n], room, rope=rope)
+
+
+@pytest.mark.parametrize("a", ["bf16", "f32"])
+@pytest.mark.parametrize("room", [0, 30000])
+@pytest.mark.parametrize("ek,eq", [(100, -100), (124, -124), (123, -140), (-100, 100), (-115, 118), (60, -58), (-130, 110)])
+def test_keys_over_the_whole_range(ek, eq, room, a):
+    """keys that the cache holds have scores wherever queries times keys are numbers"""
+    R, H, Hkv, D, n = 3, 4, 2, 128, 300
+    k, v = rows(1, n, Hkv, D, torch.float32, 9)
+    c, table = new_cache(1, n, Hkv, D, 16, 64)
+    c.append((k.double() * 2.0 ** (ek - 4)).float(), v, table, ints([0]))
+    q = (torch.randn(1, R, H, D, generator=gen(10), device="cuda").double() * 2.0 ** (eq + 4)).to(DT[a])
+    out = check(c, table, q, [n], room)
+    assert out.isfinite().all()
+
+
+@pytest.mark.parametrize("room", [0, 30000])
+@pytest.mark.parametrize("es", [-120, -60, 60, 120])
+def test_scales_over_the_whole_range(es, room):
+    """a scale far from 1 with queries that bring the scores back"""
+    R, H, Hkv, D, n = 3, 4, 2, 64, 300
+    k, v = rows(1, n, Hkv, D, torch.float32, 11)
+    c, table = new_cache(1, n, Hkv, D, 16, 64)
+    c.append(k, v, table, ints([0]))
+    q = torch.randn(1, R, H, D, generator=gen(12), device="cuda") * 2.0 ** -es
+    check(c, table, q, [n], room, scale=2.0 ** es / 8)
+
+
+@pytest.mark.parametrize("room", [0, 30000])
+@pytest.mark.parametrize("R,H,Hkv", [(13, 8, 8), (16, 64, 8), (2, 3, 1)])
+def test_trees_of_bf16_rows(R, H, Hkv, room):
+    """a chain with a sibling each, turned by their depths"""
+    B, D, n = 2, 128, 260
+    c, table = new_cache(B, n, Hkv, D, 32, 64)
+    rope = rope_table(n, D)
+    k, v = rows(B, n, Hkv, D, torch.bfloat16, 3)
+    depth = [(m + 1) // 2 for m in range(R)]
+    n_ctx = [n, 200]
+    positions = ints([[L - R + d for d in depth] for L in n_ctx])
+    chain = lambda m: sum(1 << j for j in range(m) if (j % 2 == 1 or j == 0) and depth[j] < depth[m]) | 1 << m
+    visible = ints([[chain(m) for m in range(R)]] * B)
+    c.append(k, v, table, ints([0] * B), rope=rope)
+    c.append(k[:, :R], v[:, :R], table, ints([L - R for L in n_ctx]), rope=rope, positions=positions)
+    q = torch.randn(B, R, H, D, generator=gen(4), device="cuda").to(torch.bfloat16)
+    check(c, table, q, n_ctx, room, visible=visible, rope=rope, positions=positions)
