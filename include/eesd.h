@@ -613,7 +613,7 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  * the lengths: the same call has the same bits, a row among others or in a wider table may round otherwise.
  * A row of queries that holds a NaN or an infinity gives NaN.
  * Scores may overflow where sums of query times key pass 2^115, results where 256 times a row's sum of numerators times values passes fp32's range.
- * UNSUPPORTED: rows * n_heads above 2^30, or that times B and the table's tiles above 2^50. */
+ * UNSUPPORTED: rows * n_heads above 2^30, that times B and the table's tiles above 2^50, or 2^31 blocks (of up to 8 columns of a key head). */
 typedef struct eesd_kv4_attention {
     eesd_kv4_rows rows;
     eesd_kv4_tensor q;

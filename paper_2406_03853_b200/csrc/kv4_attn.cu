@@ -806,6 +806,12 @@ Way way_of(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
     return Way{blocks % 2 == 0 && units > 256 * grid_of(1) ? 2 : 1, 0};
 }
 
+// Whether a launch holds the clusters' blocks.
+bool launchable(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads, const Way &w) {
+    const int64_t blocks = ((int64_t)(n_heads / c->n_kv_heads) * r->rows + 7) / 8;
+    return (double)r->B * c->n_kv_heads * blocks * w.share <= 2147483647.0;
+}
+
 size_t scratch_of(const eesd_kv4 *c, const Way &w) { return w.share ? 0 : (size_t)grid_of(w.nt) * (16 + 2 * 8 * w.nt * (c->head_dim + 4) * 4); }
 
 template <int D, int G, int NT, int TT, bool RUNS, bool F32> cudaError_t launch(cudaStream_t s, const AttnArgs &a, int64_t segments) {
@@ -884,6 +890,7 @@ int eesd_kv4_attend(void *cuda_stream, const eesd_kv4 *c, const void *pool, size
     if (!call->out || ((uintptr_t)call->out & 15) || ((uintptr_t)call->visible & 3) || !(call->scale > 0.f) || !(call->scale <= 3.402823466e38f)) return EESD_ERR_BADARG;
     if (!kv4::countable(c, r, n_heads)) return EESD_ERR_UNSUPPORTED;
     const kv4::Way w = kv4::way_of(c, r, n_heads);
+    if (!kv4::launchable(c, r, n_heads, w)) return EESD_ERR_UNSUPPORTED;
     if (const size_t need = kv4::scratch_of(c, w)) {
         if (!call->scratch || ((uintptr_t)call->scratch & 15)) return EESD_ERR_BADARG;
         if (call->scratch_bytes < need) return EESD_ERR_NOMEM;
