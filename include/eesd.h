@@ -596,7 +596,7 @@ int eesd_kv4_append(void *cuda_stream, const eesd_kv4 *c, void *pool, size_t poo
                     const eesd_kv4_tensor *v);
 /* eesd_kv4_read: the values at positions at[b] + m (at NULL: 0 + m), m < rows, into k and v (either may be NULL), contiguous
  * [B][rows][n_kv_heads][head_dim] in out_dtype; 0 where the position does not exist or is not below n_ctx[b] (NULL: no such bound). r's n_rows, rope
- * and positions are not looked at. */
+ * and positions are not used, but checked as in the other calls: NULL, or aligned (rope: with n_rope >= 1). */
 int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t pool_bytes, const eesd_kv4_rows *r, const int32_t *n_ctx, int out_dtype, void *k,
                   void *v);
 /* eesd_kv4_attend: rows <= EESD_MAX_ROWS query rows of each sequence, the last n = n_rows[b] positions of its at[b] tokens (which are in the
