@@ -995,6 +995,17 @@ class KV4Cache:
         return both.unbind()
 
 
+def _apart(t: torch.Tensor, name: str, *others) -> None:
+    """ValueError where the bytes of contiguous t lie on those between the first and the last of another tensor (None: left out)."""
+    lo = t.data_ptr()
+    hi = lo + t.nbytes
+    for o in others:
+        if o is not None:
+            at = o.data_ptr()
+            if at < hi and lo < at + (1 + sum((n - 1) * s for n, s in zip(o.shape, o.stride()))) * o.element_size():
+                raise ValueError(f"{name}: lies on what the call reads or writes elsewhere")
+
+
 def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ctx: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
                 scale: Optional[float] = None, visible: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
                 positions: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -1002,7 +1013,8 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
     n_ctx[b] tokens, whose keys and values are in the cache already; returns [B, rows, heads, head_dim] of q's type, rows past n_rows[b] 0.
     A row sees the positions up to its own, or with visible [B, rows] int32 those before the new rows and the new rows whose bit is set (its own
     among them).  scale: 1 / sqrt(head_dim) where left out.  rope, positions: as in KV4Cache.append, for the queries.  n_ctx, n_rows, visible, positions and
-    page_table are read on the device.  out, scratch: contiguous, made for the call when left out; calls that may overlap need their own."""
+    page_table are read on the device.  out, scratch: contiguous, made for the call when left out; they lie apart from each other and from what the call
+    reads (q too), and calls that may overlap need their own."""
     if not isinstance(cache, KV4Cache):
         raise ValueError("cache: wanted a KV4Cache")
     qt, B, rows, H = cache._tensor(q, "q")
@@ -1020,6 +1032,7 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
         _check_tensor(scratch, "scratch", (_U8,), index)
         if not scratch.is_contiguous():
             raise ValueError("scratch: wanted contiguous")
+        _apart(scratch, "scratch", q, cache.buffer, page_table, n_ctx, n_rows, visible, rope, positions)
         ptr, size = scratch.data_ptr(), scratch.numel()
     else:
         key = B, rows, H, r[2]
@@ -1037,6 +1050,7 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
         _check_tensor(out, "out", (q.dtype,), index)
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out: wanted contiguous, of q's shape")
+        _apart(out, "out", q, cache.buffer, page_table, n_ctx, n_rows, visible, rope, positions, scratch)
     call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, cache._scale if scale is None else scale)
     _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, call)
     return out
