@@ -893,6 +893,9 @@ class KV4Cache:
     are not written and not seen.  Storage: one uint8 tensor of `page_bytes` * n_pages bytes (`buffer`; the caller's own where given)."""
 
     def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int = 16, group: int = 64, device="cuda", buffer: Optional[torch.Tensor] = None):
+        for name, n in (("n_pages", n_pages), ("n_kv_heads", n_kv_heads), ("head_dim", head_dim), ("page_tokens", page_tokens), ("group", group)):
+            if not -1 << 31 <= n < 1 << 31:   # (a C record would take its low 32 bits)
+                raise ValueError(f"{name}: {n}")
         self.n_pages, self.n_kv_heads, self.head_dim, self.page_tokens, self.group = n_pages, n_kv_heads, head_dim, page_tokens, group
         self._desc, self.layout = KV4Desc(n_pages, n_kv_heads, head_dim, page_tokens, group), KV4Layout()
         self._desc_ptr = C.addressof(self._desc)
@@ -984,8 +987,8 @@ class KV4Cache:
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or not page_table.shape[0]:
             raise ValueError("page_table: wanted [B, pages]")
         B = page_table.shape[0]
-        if count < 1:
-            raise ValueError("count: at least one position")
+        if not 1 <= count < 1 << 31:
+            raise ValueError("count: 1 to 2^31 - 1 positions")
         r = self._rows(page_table, B, count, start, "start", None, None, None)
         n = None if n_ctx is None else self._ints(n_ctx, "n_ctx", (B,))
         both = self.buffer.new_empty((2, B, count, self.n_kv_heads, self.head_dim), dtype=dtype)
@@ -1051,6 +1054,10 @@ def attend_rows(q: torch.Tensor, cache: KV4Cache, page_table: torch.Tensor, n_ct
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out: wanted contiguous, of q's shape")
         _apart(out, "out", q, cache.buffer, page_table, n_ctx, n_rows, visible, rope, positions, scratch)
-    call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, cache._scale if scale is None else scale)
+    if scale is None:
+        scale = cache._scale
+    elif scale > 3.4028234e38:
+        scale = float("inf")   # (refused as such: past fp32 the record does not hold it)
+    call = _kv4_attention(*r, *qt, vis, out.data_ptr(), ptr, size, _DTYPES[q.dtype], H, scale)
     _call(L.eesd_kv4_attend, "eesd_kv4_attend", index, cache._desc_ptr, cache._ptr, cache._bytes, call)
     return out
