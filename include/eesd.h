@@ -609,8 +609,8 @@ int eesd_kv4_read(void *cuda_stream, const eesd_kv4 *c, const void *pool, size_t
  * bytes (0: it may be NULL), contents irrelevant; calls that may overlap on the GPU need their own.
  * Arithmetic, of either dtype: sums, maxima and exponentials are fp32.  A turned query is taken as two fp16 terms under a power of two of its row and head: off by at
  * most 2^-22 of itself, or 2^-39 of the largest of its row and head; codes less zero points enter exactly.  A softmax numerator times its value's scale is
- * taken as two fp16 terms: off by at most 2^-22 of itself, or 2^-29 of the row's largest.  The order of additions follows from B, rows, n_heads, max_pages and
- * the lengths: the same call has the same bits, a row among others or in a wider table may round otherwise.
+ * taken as two fp16 terms: off by at most 2^-22 of itself, or 2^-29 of the row's largest, or 2^-145.  The order of additions follows from B, rows, n_heads,
+ * max_pages and the lengths: the same call has the same bits, a row among others or in a wider table may round otherwise.
  * A row of queries that holds a NaN or an infinity gives NaN.
  * Scores may overflow where sums of query times key pass 2^115, results where 256 times a row's sum of numerators times values passes fp32's range.
  * UNSUPPORTED: rows * n_heads above 2^30, that times B and the table's tiles above 2^50, or 2^31 blocks (of up to 8 columns of a key head). */

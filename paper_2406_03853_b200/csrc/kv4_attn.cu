@@ -19,11 +19,12 @@
 // A segment is what one key head of one sequence has to do for 8 NT columns. Two ways to share the machine (way_of):
 //   clusters  the blocks of a cluster share a segment and push their parts into the shared memory of the block that joins them (one launch)
 //   runs      the tiles of all segments stand in a row and are dealt out evenly, whatever the sequences' lengths; a second kernel joins what was cut.
-//             Two tiles a step of a warp (TT), which hide each other's latency: the 130001 tokens below 197 us, one tile a step 215
+//             Two tiles a step of a warp (TT), which hide each other's latency: the 130001 tokens below 217 us, one tile a step 228 (and none of the
+//             spills, 152 to 232 bytes a thread with heads of 128, that two take at 128 registers)
 //
 // What bounds it (70B shape, 64 heads on 8 of 128; B200): 32 sequences of up to 8192 tokens, one row, bf16: 66 us, 180 MB, 0.42 of the copy rate;
-// 130001 tokens, 5 rows, fp32: 217 us, 21 GFLOP. A warp's unit of 16 tokens by 8 columns is 318 instructions (fp32: 423), 17 (28) of them matrix
-// instructions, at four warps a scheduler: two thirds of the issue slots, half of the ALU pipe. Short calls (one sequence of 1056 tokens, 5 rows, 13B
+// 130001 tokens, 5 rows, fp32: 217 us, 21 GFLOP. A warp's unit of 16 tokens by 8 columns is 413 instructions (two groups a head: 439), 32 of them matrix
+// instructions, at four warps a scheduler: 57 to 64 % of the issue slots, 43 to 47 % of the ALU pipe. Short calls (one sequence of 1056 tokens, 5 rows, 13B
 // shape: 8.4 us) are launch, four dependent reads and the joining.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -786,11 +787,11 @@ bool countable(const eesd_kv4 *c, const eesd_kv4_rows *r, int n_heads) {
 //   clusters  as many blocks of a cluster as fit at once, less what leaves the rounds of tiles as they are. A round of a block's warps takes 1.2 us
 //             (64 dimensions: half of it), and the second kernel of the runs, with what it reads, 6 us, and a segment's start and end in a run 2.4:
 //             clusters where those are more than the rounds beyond an even share (several sequences: three quarters of it, their lengths differ). 70B
-//             shape, one row, 4097 tokens: 9.5 us, by runs 13.9; 16384: 16 and 16; 32768: 26 and 21; 4 x 8192 tokens: 16 and 23; 13B shape, 13 rows,
-//             4000 tokens: 26 and 30; 32 x 300 tokens: 31 and 38
-//   runs      two column tiles at once where there are many units and no tile stays empty: codes are read and expanded once for both (a tile 100 ns
-//             instead of 2 x 59, fp32 127 instead of 2 x 76), but with one block a multiprocessor what comes before and after takes 2 us more. 16
-//             rows x 8 heads on 32768 tokens: 121 instead of 140 us; 2 rows on 4 x 8192: 31 instead of 29
+//             shape, one row, 4097 tokens: 9.8 us, by runs 14.1; 16384: 17.1 and 17.0; 32768: 29 and 23; 4 x 8192 tokens: 18 and 25; 13B shape, 13 rows,
+//             4000 tokens: 23 and 27; 32 x 300 tokens of the 70B shape: 8.6 and 11.8. (Near the border it errs: 2 rows on 4 x 8192 31, by runs 35)
+//   runs      two column tiles at once where there are many units and no tile stays empty: codes are read and expanded once for both (a tile takes a
+//             multiprocessor 160 ns instead of 2 x 99), but with one block a multiprocessor what comes before and after takes 2 us more. 16
+//             rows x 8 heads on 32768 tokens: 143 instead of 176 us; 2 rows on 4 x 8192: 34 and 35
 struct Way { int nt, share; };
 // clusters of so many blocks that the machine holds at once, two blocks a multiprocessor (cudaOccupancyMaxActiveClusters)
 constexpr int kFit[kMaxShare + 1] = {0, 296, 148, 93, 71, 56, 45, 37, 33, 30, 26, 21, 21, 17, 14, 14, 14};
